@@ -43,7 +43,17 @@ enum {
   BAKLAVA_ENOMEM = 6       /* a host-side allocation of the library failed                          */
 };
 
-enum { BAKLAVA_BF16 = 0, BAKLAVA_F32 = 1 };
+/*
+ * Element types.  BAKLAVA_MXFP4 is a type of cache rows only (the context's dtype): K and V are held in 4 bits, and
+ * queries, new rows and prompts of such a context are bf16.  A row of D elements is D/2 bytes of E2M1 codes (element 2i in
+ * the low half of byte i; a code is sign, two exponent bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6) and D/32
+ * scales, one E8M0 byte (2^(byte - 127)) for every 32 elements, in a plane of their own (baklava_desc.kv_scale).
+ * Rows are rounded when they enter a cache: the scale is 2^e with e = floor(log2(a)) - 2, a the largest magnitude of the
+ * 32, or one more where a exceeds 1.75 * 2^floor(log2(a)); e stays within -125 .. 125; an element becomes the nearest code,
+ * ties to the one with mantissa bit 0, magnitudes above 6 the code of 6.  32 elements of which one is infinite or NaN take
+ * the scale byte 255: all of them are NaN from then on.  Relative error of N(0, 1) values: 0.112 (2-norm).
+ */
+enum { BAKLAVA_BF16 = 0, BAKLAVA_F32 = 1, BAKLAVA_MXFP4 = 2 };
 enum { BAKLAVA_POLICY_SCORE = 0, BAKLAVA_POLICY_STREAMING = 1 };
 
 /* Static text for a status code. */
@@ -128,7 +138,8 @@ int baklava_plan_schedule(const int64_t* off_host, const int32_t* cap_host, int3
  * Device.
  *
  * Calls that only enqueue kernels on the caller's stream (safe inside a stream capture):
- * baklava_reset, baklava_append, baklava_decode_attn, baklava_append_decode_attn (its token
+ * baklava_reset, baklava_append, baklava_append_prompt (its first rows are then those of the capture),
+ * baklava_read_rows, baklava_qk_norm_rope, baklava_prompt_attn, baklava_decode_attn, baklava_append_decode_attn (its token
  * position and its capacity check are then those of the capture; baklava_append_decode_attn_replay
  * is the variant made for replay), baklava_flush_scores, baklava_compact, and the one-time passes
  * further down.  Set-up calls that synchronise or copy synchronously and therefore must stay
@@ -142,12 +153,13 @@ typedef struct baklava_ctx baklava_ctx;
 
 typedef struct {
   int32_t L, Hq, Hkv, D, batch;
-  int32_t dtype;          /* BAKLAVA_BF16 or BAKLAVA_F32: element type of k, v and of q / k_new / v_new */
+  int32_t dtype;          /* BAKLAVA_BF16 or BAKLAVA_F32: element type of k, v and of q / k_new / v_new;
+                             BAKLAVA_MXFP4: 4-bit rows, q / k_new / v_new bf16                       */
   int32_t sink, recent;   /* rows at the front / back of a cache that eviction never removes        */
   int32_t policy;         /* BAKLAVA_POLICY_*                                                        */
   int32_t track_scores;   /* 1: attention calls add each token's attention weights to `score`; see
                              baklava_flush_scores for when the plane is up to date                  */
-  void* k;                /* DEVICE [total_tokens, D] row-major, 16-byte aligned                     */
+  void* k;                /* DEVICE [total_tokens, D] row-major, 16-byte aligned (MXFP4: D/2 bytes)  */
   void* v;                /* DEVICE [total_tokens, D]                                                */
   float* score;           /* DEVICE [total_tokens] accumulated attention per cached token            */
   int32_t* pos;           /* DEVICE [total_tokens] original sequence position of each cached token   */
@@ -157,6 +169,8 @@ typedef struct {
   const int32_t* budget;  /* DEVICE [L*Hkv]; one that is not below a cache's capacity: it never evicts */
   void* workspace;        /* DEVICE scratch, 256-byte aligned, baklava_workspace_bytes() bytes       */
   size_t workspace_bytes;
+  void* kv_scale;         /* BAKLAVA_MXFP4 only (not looked at otherwise): DEVICE uint8 [total_tokens, D/16], 8-byte
+                             aligned: the scales of a row's key, D/32 bytes, then those of its value */
 } baklava_desc;
 
 /*
@@ -177,7 +191,7 @@ size_t baklava_workspace_bytes(const baklava_desc* desc, const int32_t* cap_host
  * keeps a host mirror of the lengths so that no call reads anything back from the device);
  * len_host may be NULL for all-empty caches, in which case the caller must have zeroed desc->len
  * or call baklava_reset.  Writes the work-item table into the workspace with a synchronous copy.
- * Supported shapes: D in {64, 128}; Hq a multiple of Hkv with Hq/Hkv <= 16 (<= 8 for F32);
+ * Supported shapes: D in {64, 128}; Hq a multiple of Hkv with Hq/Hkv <= 16 (<= 8 for F32 and for BF16 with D = 64);
  * sink, recent >= 0.
  * The arena must be packed the way baklava_layout lays it out: off_host[c] = sum of the capacities
  * of the caches before c (workspace planes that run parallel to the arena use the same offsets).
@@ -194,11 +208,11 @@ enum {
   BAKLAVA_OPT_CHUNK_TOKENS = 1, /* shortest run of rows per split-K work item for launches over part of
                                    the layers (multiple of 64, >= 256); the item target below may
                                    lengthen it                                                        */
-  BAKLAVA_OPT_KERNEL = 2,       /* 0 = automatic (MFMA kernel for bf16; for F32 the vector-ALU kernel up to
+  BAKLAVA_OPT_KERNEL = 2,       /* 0 = automatic (MFMA kernel for bf16 and MXFP4; for F32 the vector-ALU kernel up to
                                    four query heads per KV head, an fp32 MFMA kernel from five on), 1 =
-                                   vector-ALU kernel, 2 = MFMA kernel with recorded scores (bf16, D=128;
-                                   EINVAL otherwise, also at D=64 and for F32, where automatic choice
-                                   takes an MFMA kernel)                                              */
+                                   vector-ALU kernel (not for MXFP4), 2 = MFMA kernel with recorded scores (bf16,
+                                   D=128; EINVAL otherwise, also at D=64, for F32 and for MXFP4, where
+                                   automatic choice takes an MFMA kernel)                             */
   BAKLAVA_OPT_TIME_KERNEL = 3,  /* time every attention partial-kernel launch with a pair of HIP events
                                    (baklava_profile_read): 1 = recorded on the stream before and
                                    after the launch, 2 = carried by the kernel's own dispatch (bf16
@@ -245,7 +259,7 @@ int baklava_set_lengths(baklava_ctx* ctx, const int32_t* len_host, void* stream)
  * Appends the current token's key and value row to every cache of layers
  * [layer_begin, layer_begin + layer_count) -- the concatenations [K'; K_t], [V'; V_t] of Eq. 7.
  * The row's score starts at 0 and its pos is token_pos.
- * k_new, v_new DEVICE [layer_count, batch, Hkv, D] in the context's dtype, 16-byte aligned.
+ * k_new, v_new DEVICE [layer_count, batch, Hkv, D] in the context's dtype (bf16 for MXFP4), 16-byte aligned.
  * Errors: EINVAL, ECAPACITY (some cache of the range is full; nothing is enqueued).
  */
 int baklava_append(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count, const void* k_new,
@@ -255,7 +269,7 @@ int baklava_append(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count, c
  * Single-query attention over the reduced caches (Eq. 7, i.e. Eq. 1 with one query row per
  * head and the evicted rows absent) for layers [layer_begin, layer_begin + layer_count):
  *   out[hq] = softmax(q[hq] . K_c^T / sqrt(D)) V_c,  c = the cache of KV head hq / G.
- * q   DEVICE [layer_count, batch, Hq, D] in the context's dtype, 16-byte aligned.
+ * q   DEVICE [layer_count, batch, Hq, D] in the context's dtype (bf16 for MXFP4), 16-byte aligned.
  * out DEVICE [layer_count, batch, Hq, D] fp32, fully overwritten.
  * With track_scores, score[j] += sum over the G query heads of the softmax weight of row j; the
  * addition may be deferred to a later attention call over the same layer (baklava_flush_scores).
@@ -309,8 +323,8 @@ int baklava_sync_lengths(baklava_ctx* ctx, void* stream);
  * range holds every weight up to the latest call; without it the plane lacks at most the weights
  * of the calls on record, never anything else.  baklava_compact does this itself before it ranks
  * rows; baklava_reset and baklava_set_lengths drop what is on record.  Only calls over bf16 rows of 128
- * elements that take the MFMA kernel are recorded; all others (fp32, rows of 64 elements, BAKLAVA_OPT_KERNEL
- * = 1) add their weights before they end, so that the plane is current.  The rows a recorded call
+ * elements that take the MFMA kernel and calls over MXFP4 rows are recorded; all others (fp32, bf16 rows of 64 elements,
+ * BAKLAVA_OPT_KERNEL = 1) add their weights before they end, so that the plane is current.  The rows a recorded call
  * attended must keep their places until its weights are added: the library's own calls see to
  * that; a caller that rewrites arena rows itself calls baklava_set_lengths afterwards.
  * No-op without track_scores.  Enqueues kernels on `stream`, does not synchronise.
@@ -324,7 +338,7 @@ int baklava_flush_scores(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_co
  * `sink` rows, the last `recent` rows, and the budget - sink - recent middle rows with the
  * largest score (equal scores: the older row wins; scores compare as fp32, -0 == +0; NaN
  * scores are not supported).  POLICY_STREAMING keeps the sink rows and the budget - sink most
- * recent ones.  K, V, score and pos rows are moved in place; len <- min(len, budget).
+ * recent ones.  K, V, score and pos rows (and scales) are moved in place; len <- min(len, budget).
  * kept_idx_out DEVICE int32 [total_tokens] or NULL: for each cache in range, entries
  * off[c] .. off[c] + new_len - 1 receive the old cache-local row index of each surviving row.
  * Rows at index >= new_len are unspecified afterwards.
@@ -428,6 +442,87 @@ int baklava_alloc_two_level(const double* layer_importance, const double* head_i
 int baklava_prefill_scores(const void* q, const void* k, const float* lse, const int64_t* row_off,
                            int32_t batch, int32_t Hq, int32_t Hkv, int32_t T, int32_t D, int32_t dtype,
                            float* score_out, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Prompts: rows of queries and keys before they are used, attention over whole prompts, and prompts into and out of
+ * the caches.
+ * ------------------------------------------------------------------------------------------ */
+
+/*
+ * Rows of D elements by sequence, token and head, anywhere in DEVICE memory: row (b, t, h), t counted inside sequence b,
+ * starts at element  S_b + t * token_stride + h * head_stride  of `data`, where S_b = b * seq_stride, or, with
+ * seq_stride == 0 (packed: the tokens of all sequences in a row), token_stride times the tokens of the sequences before b.
+ * [tokens, H, D] is {0, H*D, D}, a part of a fused projection {0, width, D}, [batch, H, T, D] {H*T*D, D, T*D}.
+ * Strides are in elements, >= 0 and whole 16-byte pieces, token_stride below 2^24; `data` is 16-byte aligned.  A stride that
+ * no token, head or sequence multiplies is not looked at.  Rows that are written must not overlap.
+ */
+typedef struct {
+  void* data;
+  int64_t seq_stride, token_stride, head_stride;
+} baklava_rows;
+
+/*
+ * Queries and keys as attention takes them: every row is normed (root mean square over its D elements) and rotated by its
+ * token's position, in one pass and with one rounding, at the end:
+ *   n = x * w / sqrt(mean(x^2) + eps);   pair i of the first rot_dim elements: (a, b) <- (a cos - b sin, a sin + b cos),
+ *   angle = pos[axis_of_pair[i]] * inv_freq[i]
+ * Pair i is elements (i, i + rot_dim/2), or (2i, 2i+1) with interleaved != 0; elements from rot_dim on are not rotated.
+ * Angles are formed and reduced in 64 bits.  Tokens: n_seq sequences of T each, T at most 2^26 (packed rows: the sequences
+ * in a row).
+ * q, k rows (of Hq and Hkv heads) in `dtype` (BAKLAVA_BF16 or BAKLAVA_F32); q_out, k_out the same, and may be q and k
+ * themselves (the same struct values).  Hq or Hkv may be 0: those rows are not looked at.
+ * q_weight, k_weight DEVICE [D] in `dtype`, 16-byte aligned, or NULL: these rows are not normed.
+ * pos DEVICE int32 [n_axes, n_seq * T]; axis_of_pair HOST uint8 [rot_dim/2], each < n_axes, or NULL (axis 0);
+ * inv_freq HOST double [rot_dim/2], finite.  rot_dim even, 0 .. D; 0: no rotation, the three are not looked at.
+ * D in {64, 128}; n_axes 1 .. 8; eps >= 0.  Enqueues one kernel on `stream`; deterministic.
+ * Errors: EINVAL (null, misaligned, bad shape, stride, dtype, eps or frequency), EHIP.
+ */
+int baklava_qk_norm_rope(const baklava_rows* q, const baklava_rows* k, int32_t n_seq, int32_t T, int32_t Hq, int32_t Hkv,
+                         int32_t D, int32_t dtype, const void* q_weight, const void* k_weight, float eps,
+                         const int32_t* pos, int32_t n_axes, const uint8_t* axis_of_pair, const double* inv_freq,
+                         int32_t rot_dim, int32_t interleaved, const baklava_rows* q_out, const baklava_rows* k_out,
+                         void* stream);
+
+/*
+ * Causal attention over whole prompts of different lengths (Eq. 1 with the mask of autoregressive inference, logits scaled
+ * by 1/sqrt(D)); query head h reads KV head h / (Hq/Hkv).  Sequence b has q_len[b] query tokens and kv_len[b] keys; its
+ * queries are the last of its tokens: query t sees keys 0 .. kv_len[b] - q_len[b] + t.  A query that sees none (fewer keys
+ * than queries) gets an output of zeros and lse = -inf.  Lengths may be 0.
+ * q, out rows of Hq heads; k, v rows of Hkv heads (S_b by q_len for q and out, by kv_len for k and v when packed); bf16.
+ * lse NULL or fp32 "rows of one element" (strides in floats, any >= 0; 4-byte aligned): row (b, t, h) receives the log2 of
+ * the sum over the visible keys of 2^(q.k log2(e)/sqrt(D)), as baklava_prefill_scores takes it.  Padded places of out and lse (past a
+ * sequence's length) are not written.
+ * q_len HOST int32 [n_seq]; kv_len HOST int32 [n_seq] or NULL (= q_len).  D in {64, 128}; dtype BAKLAVA_BF16.  fp32
+ * accumulation; the softmax weights enter the second product as bf16.  Enqueues one kernel for every 128 sequences on
+ * `stream`; deterministic.
+ * Errors: EINVAL (null, misaligned, bad shape, stride or length), EHIP.
+ */
+int baklava_prompt_attn(const baklava_rows* q, const baklava_rows* k, const baklava_rows* v, int32_t n_seq,
+                        const int32_t* q_len, const int32_t* kv_len, int32_t Hq, int32_t Hkv, int32_t D, int32_t dtype,
+                        const baklava_rows* out, const baklava_rows* lse, void* stream);
+
+/*
+ * Appends a prompt (or the next part of one) to the caches of one layer: the n_tok[b] rows of sequence b, head h go behind
+ * the live rows of cache (layer, b, h), rounded to 4 bits if the context holds MXFP4 rows.  Positions are pos0[b],
+ * pos0[b] + 1, ...; scores are taken from `scores`, or 0.
+ * k, v rows of Hkv heads in the context's dtype (bf16 for MXFP4); n_tok HOST int32 [batch], 0 .. 2^29 each; pos0 HOST int32
+ * [batch] or NULL (0); scores NULL or fp32 rows of one element, as lse above (read).
+ * The host mirror of the lengths says where the rows go (see baklava_sync_lengths) and is advanced; a replay of a captured
+ * call writes the rows that the capture found, and sets the same lengths.
+ * Enqueues one kernel for at most 128 sequences of 512 caches on `stream`.
+ * Errors: EINVAL, ECAPACITY (some cache has no room; nothing is enqueued), EHIP.
+ */
+int baklava_append_prompt(baklava_ctx* ctx, int32_t layer, const baklava_rows* k, const baklava_rows* v,
+                          const int32_t* n_tok, const int32_t* pos0, const baklava_rows* scores, void* stream);
+
+/*
+ * The last n rows of every cache of the layer range as values: k_out, v_out DEVICE [caches of the range, n, D], 16-byte
+ * aligned, in the context's dtype (bf16 for MXFP4, exactly what the codes stand for).  Of a cache of fewer rows the places
+ * in front are zero.  n 1 .. 2^29.  Live lengths are read on the device.
+ * Errors: EINVAL, EHIP.
+ */
+int baklava_read_rows(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count, int32_t n, void* k_out, void* v_out,
+                      void* stream);
 
 /*
  * Algorithm 1, step 2, with the normalisation of "Head Importance Heuristic" (host only): the

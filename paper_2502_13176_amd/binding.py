@@ -17,7 +17,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libbaklava.so")
 
 OK, EINVAL, EINFEASIBLE, ECAPACITY, EHIP, ESTATE, ENOMEM = range(7)
-BF16, F32 = 0, 1
+BF16, F32, MXFP4 = 0, 1, 2
 POLICY_SCORE, POLICY_STREAMING = 0, 1
 OPT_CHUNK_TOKENS, OPT_KERNEL, OPT_TIME_KERNEL, OPT_CHUNK_TOKENS_WHOLE, OPT_TARGET_ITEMS, OPT_TARGET_ITEMS_WHOLE = 1, 2, 3, 4, 5, 6
 OPT_TRACK_SCORES, OPT_TILED_SELECT_ROWS = 7, 8
@@ -32,6 +32,7 @@ EXPORTS = [
     "baklava_stream_probe", "baklava_profile_workspace_bytes", "baklava_profile_similarity", "baklava_kv_importance", "baklava_prefill_scores", "baklava_layer_workspace_bytes", "baklava_layer_similarity",
     "baklava_alloc_two_level", "baklava_layer_similarity_static", "baklava_append_decode_attn_replay",
     "baklava_sync_lengths", "baklava_flush_scores",
+    "baklava_qk_norm_rope", "baklava_prompt_attn", "baklava_append_prompt", "baklava_read_rows",
 ]
 
 
@@ -48,8 +49,13 @@ class Desc(C.Structure):
         ("track_scores", C.c_int32),
         ("k", C.c_void_p), ("v", C.c_void_p), ("score", C.c_void_p), ("pos", C.c_void_p),
         ("off", C.c_void_p), ("cap", C.c_void_p), ("len", C.c_void_p), ("budget", C.c_void_p),
-        ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("kv_scale", C.c_void_p),
     ]
+
+
+class Rows(C.Structure):
+    """baklava_rows: rows by sequence, token and head (strides in elements, seq_stride 0: packed)."""
+    _fields_ = [("data", C.c_void_p), ("seq_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
 class WorkItem(C.Structure):
@@ -113,6 +119,14 @@ def lib() -> C.CDLL:
     L.baklava_prefill_scores.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
                                          C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]
     L.baklava_kv_importance.argtypes = [f64p, C.c_int32, C.c_int32, C.c_int32, f64p]
+    rowsp = C.POINTER(Rows)
+    L.baklava_qk_norm_rope.argtypes = [rowsp, rowsp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                                       C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_int32, C.POINTER(C.c_uint8), f64p,
+                                       C.c_int32, C.c_int32, rowsp, rowsp, C.c_void_p]
+    L.baklava_prompt_attn.argtypes = [rowsp, rowsp, rowsp, C.c_int32, i32p, i32p, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                                      rowsp, rowsp, C.c_void_p]
+    L.baklava_append_prompt.argtypes = [C.c_void_p, C.c_int32, rowsp, rowsp, i32p, i32p, rowsp, C.c_void_p]
+    L.baklava_read_rows.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
     for name in EXPORTS:
         if name not in ("baklava_strerror", "baklava_workspace_bytes", "baklava_profile_workspace_bytes",
                         "baklava_layer_workspace_bytes"):
@@ -223,10 +237,14 @@ class Arena:
         self.budget_host = _i32(budget)
         self.off_host, self.cap_host, self.total_tokens = layout(budget, L, Hkv, batch, slack)
         self.n_caches = L * batch * Hkv
-        tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
+        if dtype not in ("bf16", "f32", "mxfp4"):
+            raise ValueError("dtype must be bf16, f32 or mxfp4")
+        mx = dtype == "mxfp4"  # rows of D / 2 bytes of codes, their scales in a plane of their own
+        tdt = torch.uint8 if mx else torch.bfloat16 if dtype == "bf16" else torch.float32
         dev = self.device
-        self.k = torch.zeros((self.total_tokens, D), dtype=tdt, device=dev)
-        self.v = torch.zeros((self.total_tokens, D), dtype=tdt, device=dev)
+        self.k = torch.zeros((self.total_tokens, D // 2 if mx else D), dtype=tdt, device=dev)
+        self.v = torch.zeros_like(self.k)
+        self.kv_scale = torch.full((self.total_tokens, D // 16), 2, dtype=torch.uint8, device=dev) if mx else None
         self.score = torch.zeros((self.total_tokens,), dtype=torch.float32, device=dev)
         self.pos = torch.zeros((self.total_tokens,), dtype=torch.int32, device=dev)
         self.off = torch.from_numpy(self.off_host).to(dev)
@@ -236,7 +254,7 @@ class Arena:
 
         d = Desc()
         d.L, d.Hq, d.Hkv, d.D, d.batch = L, Hq, Hkv, D, batch
-        d.dtype = BF16 if dtype == "bf16" else F32
+        d.dtype = MXFP4 if mx else BF16 if dtype == "bf16" else F32
         d.sink, d.recent, d.policy, d.track_scores = sink, recent, policy, int(bool(track_scores))
         ws_bytes = lib().baklava_workspace_bytes(C.byref(d), _p(self.cap_host, C.c_int32),
                                                  _p(self.budget_host, C.c_int32))
@@ -245,6 +263,7 @@ class Arena:
         # the library does not rely on the workspace's initial contents; tests fill it with 0xFF bytes
         self.workspace = torch.full((ws_bytes,), int(workspace_fill), dtype=torch.uint8, device=dev)
         d.k, d.v = self.k.data_ptr(), self.v.data_ptr()
+        d.kv_scale = self.kv_scale.data_ptr() if mx else None
         d.score, d.pos = self.score.data_ptr(), self.pos.data_ptr()
         d.off, d.cap, d.len, d.budget = (self.off.data_ptr(), self.cap.data_ptr(), self.len.data_ptr(),
                                          self.budget.data_ptr())
@@ -301,6 +320,34 @@ class Arena:
     def flush_scores(self, layer_begin: int, layer_count: int, stream=None) -> None:
         _check(lib().baklava_flush_scores(self.ctx, layer_begin, layer_count, _stream_ptr(stream)),
                "baklava_flush_scores")
+
+    def append_prompt(self, layer: int, k, v, lens: Sequence[int], pos0: Optional[Sequence[int]] = None, scores=None,
+                      stream=None) -> None:
+        """baklava_append_prompt: k, v [tokens, Hkv, D] (the sequences of `lens` tokens in a row) or [batch, Hkv, T, D]
+        (padded), of any strides with contiguous rows; scores [Hkv, tokens] or [batch, Hkv, T] fp32, or None (zeros)."""
+        if len(lens) != self.batch or (pos0 is not None and len(pos0) != self.batch):
+            raise ValueError("one length (and position) per sequence expected")
+        dt = self.torch.float32 if self.dtype == "f32" else self.torch.bfloat16
+        kr, vr = (_rows(t, name, lens, self.Hkv, self.D, dt) for t, name in ((k, "k"), (v, "v")))
+        sr = _lse_rows(scores, "scores", lens, self.Hkv) if scores is not None else None
+        n = _i32(lens)
+        p0 = _i32(pos0) if pos0 is not None else None
+        _check(lib().baklava_append_prompt(self.ctx, int(layer), C.byref(kr), C.byref(vr), _p(n, C.c_int32),
+                                           _p(p0, C.c_int32) if p0 is not None else None,
+                                           C.byref(sr) if sr is not None else None, _stream_ptr(stream)),
+               "baklava_append_prompt")
+
+    def read_rows(self, layer_begin: int, layer_count: int, n: int, stream=None):
+        """baklava_read_rows: the last n rows of every cache of the range as values, (k, v) [caches, n, D]."""
+        if n < 1 or layer_count < 1:
+            raise ValueError("at least one row of one layer expected")
+        dt = self.torch.float32 if self.dtype == "f32" else self.torch.bfloat16
+        shape = (layer_count * self.batch * self.Hkv, n, self.D)
+        k, v = (self.torch.empty(shape, dtype=dt, device=self.device) for _ in range(2))
+        _check(lib().baklava_read_rows(self.ctx, int(layer_begin), int(layer_count), int(n), k.data_ptr(), v.data_ptr(),
+                                       _stream_ptr(stream)), "baklava_read_rows")
+        _hold_until_stream_passes((k, v), stream)
+        return k, v
 
     def decode_attn(self, layer_begin: int, layer_count: int, q, out, stream=None) -> None:
         _check(lib().baklava_decode_attn(self.ctx, layer_begin, layer_count, q.data_ptr(), out.data_ptr(),
@@ -432,3 +479,154 @@ def layer_similarity_static(x_in, x_out, sim, cos=None, stream=None) -> None:
     _check(lib().baklava_layer_similarity_static(x_in.data_ptr(), x_out.data_ptr(), n_seq, T, hidden, BF16,
                                                  cos.data_ptr() if cos is not None else None, sim.data_ptr(),
                                                  _stream_ptr(stream)), "baklava_layer_similarity_static")
+
+
+# ---------------------------------------------------------------------------
+# prompts
+# ---------------------------------------------------------------------------
+
+def _on_device(t, name: str):
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be a tensor on the current GPU")
+
+
+def _rows(t, name: str, lens, heads: int, D: int, dtype) -> Rows:
+    """Rows of D elements: [tokens, heads, D] packed, or [batch, heads, T, D]."""
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: {dtype} expected")
+    if t.dim() == 3:
+        ok = t.shape[0] >= sum(lens) and t.shape[1] == heads
+        st = (0, t.stride(0), t.stride(1))
+    elif t.dim() == 4:
+        ok = t.shape[0] == len(lens) and t.shape[1] == heads and t.shape[2] >= max(lens, default=0)
+        st = (t.stride(0), t.stride(2), t.stride(1))
+        if t.shape[0] > 1 and st[0] == 0:
+            raise ValueError(f"{name}: sequences must not share their memory")
+    else:
+        ok = False
+    if not ok or t.shape[-1] != D:
+        raise ValueError(f"{name} must be [tokens, {heads}, {D}] or [batch, {heads}, T, {D}] and hold all tokens")
+    if t.stride(-1) != 1:
+        raise ValueError(f"{name}: contiguous rows expected")
+    _on_device(t, name)
+    return Rows(t.data_ptr(), *st)
+
+
+def _lse_rows(t, name: str, lens, heads: int) -> Rows:
+    """One fp32 value per token and head: [heads, tokens] packed, or [batch, heads, T]."""
+    import torch
+    if t.dtype != torch.float32:
+        raise ValueError(f"{name}: float32 expected")
+    if t.dim() == 2:
+        ok = t.shape[0] == heads and t.shape[1] >= sum(lens)
+        st = (0, t.stride(1), t.stride(0))
+    else:
+        ok = t.dim() == 3 and t.shape[0] == len(lens) and t.shape[1] == heads and t.shape[2] >= max(lens, default=0)
+        st = (t.stride(0), t.stride(2), t.stride(1)) if ok else (0, 0, 0)
+        if ok and t.shape[0] > 1 and st[0] == 0:
+            raise ValueError(f"{name}: sequences must not share their memory")
+    if not ok:
+        raise ValueError(f"{name} must be [{heads}, tokens] or [batch, {heads}, T] and hold all tokens")
+    _on_device(t, name)
+    return Rows(t.data_ptr(), *st)
+
+
+def prompt_attn(q, k, v, lens: Sequence[int], kv_lens: Optional[Sequence[int]] = None, out=None, lse=None,
+                want_lse: bool = False, stream=None):
+    """baklava_prompt_attn on torch device tensors (bf16): q [tokens, Hq, D], k and v [keys, Hkv, D] (the sequences in a row)
+    or q [batch, Hq, T, D], k and v [batch, Hkv, T', D] (padded); lens query tokens and kv_lens keys of every sequence.
+    Returns out (like q; places past a sequence's length are not written), and with want_lse or lse given also lse (fp32
+    [Hq, tokens] or [batch, Hq, T])."""
+    import torch
+    if q.dim() not in (3, 4) or k.dim() not in (3, 4) or k.shape != v.shape:
+        raise ValueError("q, k, v of three or four dimensions expected, k and v alike")
+    if len(lens) == 0 or (kv_lens is not None and len(kv_lens) != len(lens)):
+        raise ValueError("one length per sequence expected")
+    if min(lens) < 0 or (kv_lens is not None and min(kv_lens) < 0):
+        raise ValueError("lengths must not be negative")
+    Hq, Hkv, D = q.shape[1], k.shape[1], q.shape[-1]
+    keys = lens if kv_lens is None else kv_lens
+    rows = [_rows(t, name, n, h, D, torch.bfloat16) for t, name, n, h in ((q, "q", lens, Hq), (k, "k", keys, Hkv), (v, "v", keys, Hkv))]
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.empty((Hq, q.shape[0]) if q.dim() == 3 else q.shape[:3], dtype=torch.float32, device=q.device)
+    rows.append(_rows(out, "out", lens, Hq, D, torch.bfloat16))
+    rows.append(_lse_rows(lse, "lse", lens, Hq) if lse is not None else None)
+    n_q, n_k = _i32(lens), _i32(kv_lens) if kv_lens is not None else None
+    _check(lib().baklava_prompt_attn(*(C.byref(r) for r in rows[:3]), len(lens), _p(n_q, C.c_int32),
+                                     _p(n_k, C.c_int32) if n_k is not None else None, Hq, Hkv, D, BF16, C.byref(rows[3]),
+                                     C.byref(rows[4]) if lse is not None else None, _stream_ptr(stream)), "baklava_prompt_attn")
+    _hold_until_stream_passes((out, lse), stream)
+    return (out, lse) if lse is not None else out
+
+
+def qk_norm_rope(q, k, pos, inv_freq: Sequence[float], q_weight=None, k_weight=None, eps: float = 1e-6,
+                 sections: Optional[Sequence[int]] = None, axis_of_pair: Optional[Sequence[int]] = None,
+                 interleaved: bool = False, q_out=None, k_out=None, stream=None):
+    """baklava_qk_norm_rope on torch device tensors: q [tokens, Hq, D], k [tokens, Hkv, D] or [batch, H, T, D] (either may be
+    None), bf16 or fp32, of any strides with contiguous rows; pos int32 [tokens] or [axes, tokens] ([axes, batch, T] in any
+    shape of as many values); inv_freq one frequency per pair of rotated elements (empty: no rotation, pos is not looked at).
+    The axis of every pair is given by axis_of_pair, or by sections: pairs of axis 0, of axis 1, ...  Weights [D] or None (not
+    normed).  q_out, k_out may be q and k.  Returns (q_out, k_out)."""
+    import torch
+    given = [t for t in (q, k) if t is not None]
+    if not given or any(t.dim() not in (3, 4) or t.dim() != given[0].dim() for t in given):
+        raise ValueError("q or k of three or four dimensions expected, both alike")
+    t0 = given[0]
+    if t0.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("bf16 or fp32 tensors expected")
+    D, padded = t0.shape[-1], t0.dim() == 4
+    n_seq, T = (t0.shape[0], t0.shape[2]) if padded else (1, t0.shape[0])
+    for t in given:
+        if ((t.shape[0], t.shape[2]) if padded else (1, t.shape[0])) != (n_seq, T):
+            raise ValueError("q and k must hold the same tokens")
+    if n_seq * T == 0:
+        return tuple(None if t is None else o if o is not None else torch.empty_like(t) for t, o in ((q, q_out), (k, k_out)))
+    freq = np.ascontiguousarray(inv_freq, dtype=np.float64)
+    axes = 1
+    if freq.size:
+        if pos.dtype != torch.int32 or not pos.is_contiguous() or pos.numel() == 0 or pos.numel() % (n_seq * T):
+            raise ValueError("pos must be a contiguous int32 tensor with one value per axis and token")
+        _on_device(pos, "pos")
+        axes = pos.numel() // (n_seq * T)
+    if sections is not None:
+        if axis_of_pair is not None or sum(sections) != freq.size or len(sections) > axes or min(sections, default=0) < 0:
+            raise ValueError("sections must add up to the number of pairs, at most one for each axis")
+        axis_of_pair = [a for a, n in enumerate(sections) for _ in range(n)]
+    ax = None
+    if axis_of_pair is not None:
+        if len(axis_of_pair) != freq.size or any(not 0 <= a < axes for a in axis_of_pair):
+            raise ValueError("axis_of_pair must name an axis for every pair")
+        ax = np.ascontiguousarray(axis_of_pair, dtype=np.uint8)
+    lens = [T] * n_seq
+    ptr, outs, heads = [], [], []
+    for t, name, w, o in ((q, "q", q_weight, q_out), (k, "k", k_weight, k_out)):
+        if t is None:
+            if w is not None or o is not None:
+                raise ValueError(f"no {name} given")
+            ptr.append((None, None, None))
+            outs.append(None)
+            heads.append(0)
+            continue
+        if w is not None:
+            if w.dtype != t.dtype or w.shape != (D,) or not w.is_contiguous():
+                raise ValueError(f"{name}_weight must be a contiguous [{D}] tensor of the rows' type")
+            _on_device(w, f"{name}_weight")
+        r = _rows(t, name, lens, t.shape[1], D, t0.dtype)
+        if o is None:
+            o = torch.empty(t.shape, dtype=t.dtype, device=t.device)
+        elif o.shape != t.shape:
+            raise ValueError(f"{name}_out must have the shape of {name}")
+        ptr.append((C.byref(r), w.data_ptr() if w is not None else None, C.byref(_rows(o, f"{name}_out", lens, t.shape[1], D, t0.dtype))))
+        outs.append(o)
+        heads.append(t.shape[1])
+    _check(lib().baklava_qk_norm_rope(ptr[0][0], ptr[1][0], n_seq, T, heads[0], heads[1], D,
+                                      BF16 if t0.dtype == torch.bfloat16 else F32, ptr[0][1], ptr[1][1], float(eps),
+                                      pos.data_ptr() if freq.size else None, axes,
+                                      _p(ax, C.c_uint8) if ax is not None else None, _p(freq, C.c_double), 2 * freq.size,
+                                      int(bool(interleaved)), ptr[0][2], ptr[1][2], _stream_ptr(stream)),
+           "baklava_qk_norm_rope")
+    _hold_until_stream_passes(outs, stream)
+    return outs[0], outs[1]

@@ -1,6 +1,7 @@
 // C-ABI entry points of libbaklava (device part): context, split-K schedule, launches.
 #include <algorithm>
 #include <cmath>
+#include <cstddef>
 #include <cstring>
 #include <memory>
 #include <new>
@@ -30,6 +31,9 @@ constexpr int kDefaultChunkWhole = 256;   // launches over the whole model: shor
 constexpr int kWholeItemsPerCu = 5;       // launches over many caches aim at this many work items per compute unit
 constexpr int kShortestRun = 64;          // where those would leave compute units idle (see build_schedule)
 constexpr int kMostFillItems = 256;       // most work items such short runs are cut for: one per compute unit (sizes the workspace)
+constexpr int32_t kMostPromptTokens = 1 << 29;      // of a sequence
+constexpr int32_t kMostRopeTokens = 1 << 26;        // of a sequence: a grid dimension holds fewer than 2^32 threads
+constexpr int64_t kMostTokenStride = 1 << 24;       // offsets inside a tile of rows stay below 2^32 bytes
 constexpr int kMaxChunk = 1 << 22; // row offsets inside a work item stay below 2^32 bytes
 inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
@@ -53,7 +57,7 @@ bool shape_ok(const baklava_desc* d) {
   if (!d) return false;
   if (d->L <= 0 || d->Hq <= 0 || d->Hkv <= 0 || d->batch <= 0) return false;
   if (d->D != 64 && d->D != 128) return false;
-  if (d->dtype != BAKLAVA_BF16 && d->dtype != BAKLAVA_F32) return false;
+  if (d->dtype != BAKLAVA_BF16 && d->dtype != BAKLAVA_F32 && d->dtype != BAKLAVA_MXFP4) return false;
   if (d->Hq % d->Hkv) return false;
   const int G = d->Hq / d->Hkv;
   if (G > 16 || (d->dtype == BAKLAVA_F32 && G > 8)) return false;
@@ -64,14 +68,18 @@ bool shape_ok(const baklava_desc* d) {
   return true;
 }
 
-// Scores are deferred over bf16 rows of 128 elements only (see decode_impl).
-bool keeps_records(const baklava_desc* d) { return d->dtype == BAKLAVA_BF16 && d->D == 128; }
+// Scores are deferred over bf16 rows of 128 elements and over 4-bit rows only (see decode_impl).
+bool keeps_records(const baklava_desc* d) { return d->dtype == BAKLAVA_MXFP4 || (d->dtype == BAKLAVA_BF16 && d->D == 128); }
+
+// Bytes of a row of queries (and of new rows), and of a cached row.
+int32_t query_row_bytes(const baklava_desc* d) { return d->D * (d->dtype == BAKLAVA_F32 ? 4 : 2); }
+int32_t cache_row_bytes(const baklava_desc* d) { return d->dtype == BAKLAVA_MXFP4 ? d->D / 2 : query_row_bytes(d); }
 
 WorkspacePlan plan_workspace(const baklava_desc* d, const int32_t* cap) {
   WorkspacePlan w{};
   const int64_t n_caches = (int64_t)d->L * d->batch * d->Hkv;
   const int G = d->Hq / d->Hkv;
-  const size_t row_bytes = (size_t)d->D * (d->dtype == BAKLAVA_BF16 ? 2 : 4);
+  const size_t row_bytes = (size_t)query_row_bytes(d);
   int64_t total_tokens = 0;
   for (int64_t c = 0; c < n_caches; ++c) total_tokens += cap[c];
   // runs of at least kSizingChunk rows, or the shorter ones of the layers that those would not fill the chip with
@@ -127,7 +135,7 @@ struct baklava_ctx {
   int64_t n_caches, total_tokens;
   int32_t cpl;  // caches per layer
   int32_t G;
-  int32_t row_bytes;
+  int32_t row_bytes;  // of a cached row
   std::vector<int64_t> off;
   std::vector<int32_t> cap, len, budget;
   std::vector<int32_t> order_all, order_layer;  // caches, longest first (whole model / inside each layer)
@@ -337,8 +345,8 @@ bool range_ok(const baklava_ctx* ctx, int32_t lb, int32_t lc) {
 }
 
 // The weights of the calls on record go to the score plane now (see DecodeParams): a pass over the
-// K rows of the layer range, after which the records are empty.  Only the MFMA attention kernel over rows of
-// 128 elements leaves calls on record.
+// K rows of the layer range, after which the records are empty.  Only the MFMA attention kernel over bf16 rows of
+// 128 elements and the one over 4-bit rows leave calls on record.
 int flush_records(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count, hipStream_t s) {
   if (!ctx->d.track_scores || !keeps_records(&ctx->d)) return BAKLAVA_OK;
   const int64_t c0 = (int64_t)layer_begin * ctx->cpl;
@@ -359,10 +367,13 @@ int flush_records(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count, hi
                                             sc.max_split.begin() + layer_begin + layer_count) <= kMostTickets;
   p.flush_ticket = self_clear ? reinterpret_cast<int32_t*>(ctx->ws + ctx->plan.flush_ticket) : nullptr;
   p.G = ctx->G; p.lag_gp_log2 = ctx->lag_gp_log2;
+  p.kv_scale = reinterpret_cast<uint8_t*>(ctx->d.kv_scale);
   p.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)ctx->d.D));
   const int32_t longest = *std::max_element(sc.max_count.begin() + layer_begin,
                                             sc.max_count.begin() + layer_begin + layer_count);
-  if (!hip_ok(launch_score_flush_mfma(p, i1 - i0, longest, s))) return BAKLAVA_EHIP;
+  if (!hip_ok(ctx->d.dtype == BAKLAVA_MXFP4 ? launch_score_flush_mxfp4(p, ctx->d.D, i1 - i0, longest, s)
+                                            : launch_score_flush_mfma(p, i1 - i0, longest, s)))
+    return BAKLAVA_EHIP;
   if (!self_clear && !hip_ok(launch_fill_i32(p.lag_cnt + c0 * ctx->G, 0, (c1 - c0) * ctx->G, s))) return BAKLAVA_EHIP;
   return BAKLAVA_OK;
 }
@@ -403,9 +414,10 @@ int decode_impl(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count, cons
   hipStream_t s = (hipStream_t)stream;
   const bool use_mfma = ctx->kernel_pref == 2 || (ctx->kernel_pref == 0 && ctx->d.dtype == BAKLAVA_BF16);
   const bool track = ctx->track_on;
-  // Scores are deferred over rows of 128 elements only: those of 64 have always been current when a call
-  // returns, and callers read them, set them or declare new lengths between calls without a flush.
-  const bool defer = track && use_mfma && ctx->d.D == 128;
+  // Scores are deferred over bf16 rows of 128 elements only: those of 64 have always been current when a call
+  // returns, and callers read them, set them or declare new lengths between calls without a flush.  4-bit rows always.
+  const bool mx = ctx->d.dtype == BAKLAVA_MXFP4;
+  const bool defer = track && (mx || (use_mfma && ctx->d.D == 128));
   // Other calls add their weights right away; weights an earlier call left pending come first, so that the
   // scores grow in the order of the calls.
   if (track && !defer) {
@@ -446,7 +458,8 @@ int decode_impl(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count, cons
                                             sc.max_count.begin() + layer_begin + layer_count);
   p.fused_append = fused ? 1 : 0;
   p.token_pos = token_pos;
-  p.row_bytes = ctx->row_bytes;
+  p.row_bytes = query_row_bytes(&ctx->d);
+  p.kv_scale = reinterpret_cast<uint8_t*>(ctx->d.kv_scale);
   p.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)ctx->d.D));
   hipEvent_t ev0 = nullptr, ev1 = nullptr;
   if (ctx->time_kernel) {
@@ -460,7 +473,8 @@ int decode_impl(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count, cons
     if (!(ctx->time_kernel == 2 && use_mfma) && !hip_ok(hipEventRecord(ev0, s))) return BAKLAVA_EHIP;
   }
   const bool on_dispatch = ctx->time_kernel == 2 && use_mfma;
-  hipError_t e = use_mfma ? launch_decode_mfma(p, ctx->d.D, i1 - i0, longest, i1 - i0 <= ctx->n_cus, s,
+  hipError_t e = mx ? launch_decode_mxfp4(p, ctx->d.D, i1 - i0, longest, i1 - i0 <= ctx->n_cus, s)
+               : use_mfma ? launch_decode_mfma(p, ctx->d.D, i1 - i0, longest, i1 - i0 <= ctx->n_cus, s,
                                                on_dispatch ? ev0 : nullptr, on_dispatch ? ev1 : nullptr)
                : ctx->kernel_pref == 0 && f32_on_matrix_cores(ctx)
                           ? launch_decode_mfma_f32(p, ctx->d.D, i1 - i0, longest, i1 - i0 <= ctx->n_cus, s)
@@ -512,6 +526,7 @@ extern "C" int baklava_create(const baklava_desc* desc, const int64_t* off_host,
       !desc->budget || !desc->workspace)
     return BAKLAVA_EINVAL;
   if (((uintptr_t)desc->k | (uintptr_t)desc->v) & 15) return BAKLAVA_EINVAL;
+  if (desc->dtype == BAKLAVA_MXFP4 && (!desc->kv_scale || ((uintptr_t)desc->kv_scale & 7))) return BAKLAVA_EINVAL;
   if ((uintptr_t)desc->workspace & 255) return BAKLAVA_EINVAL;
   const int64_t n_caches = (int64_t)desc->L * desc->batch * desc->Hkv;
   const int64_t m = (int64_t)desc->L * desc->Hkv;
@@ -530,12 +545,13 @@ extern "C" int baklava_create(const baklava_desc* desc, const int64_t* off_host,
   }
   baklava_ctx* ctx = new (std::nothrow) baklava_ctx();
   if (!ctx) return BAKLAVA_ENOMEM;
-  ctx->d = *desc;
+  // (a caller of bf16 or fp32 rows may have been built with the description as it ended before kv_scale)
+  std::memcpy(&ctx->d, desc, desc->dtype == BAKLAVA_MXFP4 ? sizeof(baklava_desc) : offsetof(baklava_desc, kv_scale));
   ctx->n_caches = n_caches;
   ctx->total_tokens = packed;
   ctx->cpl = desc->batch * desc->Hkv;
   ctx->G = desc->Hq / desc->Hkv;
-  ctx->row_bytes = desc->D * (desc->dtype == BAKLAVA_BF16 ? 2 : 4);
+  ctx->row_bytes = cache_row_bytes(desc);
   ctx->lag_gp_log2 = ctx->G <= 4 ? 2 : ctx->G <= 8 ? 3 : 4;
   ctx->off.assign(off_host, off_host + n_caches);
   ctx->cap.assign(cap_host, cap_host + n_caches);
@@ -614,6 +630,7 @@ extern "C" int baklava_create(const baklava_desc* desc, const int64_t* off_host,
     if (st != BAKLAVA_OK) { delete ctx; return st; }
   }
   if (desc->dtype == BAKLAVA_BF16 && !hip_ok(prepare_decode_mfma())) { delete ctx; return BAKLAVA_EHIP; }
+  if (desc->dtype == BAKLAVA_MXFP4 && !hip_ok(prepare_decode_mxfp4())) { delete ctx; return BAKLAVA_EHIP; }
   if (desc->dtype == BAKLAVA_F32 && !hip_ok(prepare_decode_mfma_f32())) { delete ctx; return BAKLAVA_EHIP; }
   const int chunk = ctx->layer_one_wave ? kDefaultChunk : kDefaultChunkWhole;
   const int chunk_layer = slow_rows(ctx) ? kDefaultChunkWhole : chunk;  // (see build_schedule)
@@ -654,7 +671,7 @@ extern "C" int baklava_set_option(baklava_ctx* ctx, int32_t option, int64_t valu
     case BAKLAVA_OPT_KERNEL:
       if (value < 0 || value > 2) return BAKLAVA_EINVAL;
       if (value == 2 && !(ctx->d.dtype == BAKLAVA_BF16 && ctx->d.D == 128)) return BAKLAVA_EINVAL;
-      if (value == 1 && ctx->G > 8) return BAKLAVA_EINVAL;
+      if (value == 1 && (ctx->G > 8 || ctx->d.dtype == BAKLAVA_MXFP4)) return BAKLAVA_EINVAL;
       ctx->kernel_pref = (int32_t)value;
       return BAKLAVA_OK;
     case BAKLAVA_OPT_TILED_SELECT_ROWS: {
@@ -749,7 +766,10 @@ extern "C" int baklava_append(baklava_ctx* ctx, int32_t layer_begin, int32_t lay
   p.k_new = k_new; p.v_new = v_new;
   p.token_pos_dev = nullptr;
   p.cache_begin = (int32_t)c0; p.token_pos = token_pos; p.row_bytes = ctx->row_bytes;
-  if (!hip_ok(launch_append(p, (int)(c1 - c0), (hipStream_t)stream))) return BAKLAVA_EHIP;
+  p.kv_scale = reinterpret_cast<uint8_t*>(ctx->d.kv_scale);
+  if (!hip_ok(ctx->d.dtype == BAKLAVA_MXFP4 ? launch_append_mx(p, ctx->d.D, (int)(c1 - c0), (hipStream_t)stream)
+                                            : launch_append(p, (int)(c1 - c0), (hipStream_t)stream)))
+    return BAKLAVA_EHIP;
   for (int64_t c = c0; c < c1; ++c) ctx->len[c] += 1;
   return BAKLAVA_OK;
 }
@@ -815,6 +835,7 @@ extern "C" int baklava_compact(baklava_ctx* ctx, int32_t layer_begin, int32_t la
   p.Hkv = ctx->d.Hkv; p.batch = ctx->d.batch;
   p.sink = ctx->d.sink; p.recent = ctx->d.recent; p.policy = ctx->d.policy;
   p.row_bytes = ctx->row_bytes;
+  p.kv_scale = reinterpret_cast<uint8_t*>(ctx->d.kv_scale);
   p.write_identity = kept_idx_out ? 1 : 0;
   p.move_ticket = reinterpret_cast<int32_t*>(ctx->ws + ctx->plan.move_ticket);
   p.move_flags = reinterpret_cast<int32_t*>(ctx->ws + ctx->plan.move_flags);
@@ -898,6 +919,198 @@ extern "C" int baklava_prefill_scores(const void* q, const void* k, const float*
   if (((uintptr_t)lse | (uintptr_t)score_out) & 3 || ((uintptr_t)row_off & 7)) return BAKLAVA_EINVAL;
   if ((int64_t)batch * Hkv * (((int64_t)T + 127) / 128) > INT32_MAX) return BAKLAVA_EINVAL;
   if (!hip_ok(launch_prefill_scores(q, k, lse, row_off, batch, Hq, Hkv, T, score_out, (hipStream_t)stream)))
+    return BAKLAVA_EHIP;
+  return BAKLAVA_OK;
+}
+
+namespace {
+
+// Whether rows of `heads` heads can be addressed: `unit` elements are a 16-byte piece (or one element), `wide` bytes an
+// element.  Strides that no row index multiplies are not looked at.
+bool rows_ok(const baklava_rows* r, int32_t n_seq, int64_t most_tokens, int32_t heads, int unit, int align) {
+  if (!r || !r->data || ((uintptr_t)r->data & (align - 1))) return false;
+  if (r->seq_stride < 0 || r->token_stride < 0 || r->head_stride < 0) return false;
+  if (n_seq > 1 && r->seq_stride % unit) return false;
+  if ((most_tokens > 1 || (n_seq > 1 && !r->seq_stride)) && (r->token_stride % unit || r->token_stride >= kMostTokenStride)) return false;
+  return !(heads > 1 && r->head_stride % unit);
+}
+// ... and written: rows apart from each other where there are several.
+bool written_rows_ok(const baklava_rows* r, int32_t n_seq, int64_t most_tokens, int32_t heads, int unit, int align, int row) {
+  if (!rows_ok(r, n_seq, most_tokens, heads, unit, align)) return false;
+  const bool packed = n_seq > 1 && !r->seq_stride;
+  if ((most_tokens > 1 || packed) && r->token_stride < row) return false;
+  if (heads > 1 && r->head_stride < row) return false;
+  return !(n_seq > 1 && r->seq_stride && r->seq_stride < row);
+}
+
+Rows device_rows(const baklava_rows* r, int64_t num, int64_t den) {
+  if (!r) return Rows{nullptr, 0, 0, 0};
+  return Rows{r->data, r->seq_stride * num / den, r->token_stride * num / den, r->head_stride * num / den};
+}
+
+}  // namespace
+
+extern "C" int baklava_qk_norm_rope(const baklava_rows* q, const baklava_rows* k, int32_t n_seq, int32_t T, int32_t Hq,
+                                    int32_t Hkv, int32_t D, int32_t dtype, const void* q_weight, const void* k_weight,
+                                    float eps, const int32_t* pos, int32_t n_axes, const uint8_t* axis_of_pair,
+                                    const double* inv_freq, int32_t rot_dim, int32_t interleaved, const baklava_rows* q_out,
+                                    const baklava_rows* k_out, void* stream) {
+  if (n_seq <= 0 || T <= 0 || T > kMostRopeTokens || Hq < 0 || Hkv < 0 || (int64_t)Hq + Hkv <= 0 || (int64_t)Hq + Hkv > INT32_MAX / 1024) return BAKLAVA_EINVAL;
+  if ((D != 64 && D != 128) || (dtype != BAKLAVA_BF16 && dtype != BAKLAVA_F32)) return BAKLAVA_EINVAL;
+  if (rot_dim < 0 || rot_dim > D || rot_dim % 2 || !(eps >= 0.f) || std::isinf(eps)) return BAKLAVA_EINVAL;
+  const int unit = dtype == BAKLAVA_BF16 ? 8 : 4;
+  if (Hq > 0 && (!rows_ok(q, n_seq, T, Hq, unit, 16) || !written_rows_ok(q_out, n_seq, T, Hq, unit, 16, D))) return BAKLAVA_EINVAL;
+  if (Hkv > 0 && (!rows_ok(k, n_seq, T, Hkv, unit, 16) || !written_rows_ok(k_out, n_seq, T, Hkv, unit, 16, D))) return BAKLAVA_EINVAL;
+  if (((uintptr_t)q_weight | (uintptr_t)k_weight) & 15) return BAKLAVA_EINVAL;
+  RopeParams p{};
+  p.q = Hq > 0 ? device_rows(q, 1, 1) : Rows{};
+  p.k = Hkv > 0 ? device_rows(k, 1, 1) : Rows{};
+  p.q_out = Hq > 0 ? device_rows(q_out, 1, 1) : Rows{};
+  p.k_out = Hkv > 0 ? device_rows(k_out, 1, 1) : Rows{};
+  for (Rows* r : {&p.q, &p.k, &p.q_out, &p.k_out})
+    if (!r->seq) r->seq = r->tok * T;  // packed: sequences of T tokens in a row
+  p.q_weight = q_weight; p.k_weight = k_weight;
+  p.eps = eps;
+  p.n_seq = n_seq; p.T = T; p.Hq = Hq; p.Hkv = Hkv;
+  p.rot = rot_dim;
+  if (rot_dim > 0) {
+    if (!pos || ((uintptr_t)pos & 3) || !inv_freq || n_axes < 1 || n_axes > 8) return BAKLAVA_EINVAL;
+    for (int i = 0; i < rot_dim / 2; ++i) {
+      if (!std::isfinite(inv_freq[i])) return BAKLAVA_EINVAL;
+      if (axis_of_pair && axis_of_pair[i] >= n_axes) return BAKLAVA_EINVAL;
+      p.turns[i] = (double)((long double)inv_freq[i] * 0.159154943091895335768883763372514362034459645740456448747667344L);  // 1 / (2 pi)
+      p.axis[i] = axis_of_pair ? axis_of_pair[i] : 0;
+    }
+    p.pos = pos;
+  }
+  if (!hip_ok(launch_qk_norm_rope(p, dtype, D, interleaved != 0, (hipStream_t)stream))) return BAKLAVA_EHIP;
+  return BAKLAVA_OK;
+}
+
+extern "C" int baklava_prompt_attn(const baklava_rows* q, const baklava_rows* k, const baklava_rows* v, int32_t n_seq,
+                                   const int32_t* q_len, const int32_t* kv_len, int32_t Hq, int32_t Hkv, int32_t D,
+                                   int32_t dtype, const baklava_rows* out, const baklava_rows* lse, void* stream) {
+  if (!q_len || n_seq <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || dtype != BAKLAVA_BF16) return BAKLAVA_EINVAL;
+  if (D != 64 && D != 128) return BAKLAVA_EINVAL;
+  const int32_t* const k_len = kv_len ? kv_len : q_len;
+  int64_t n_q = 0, n_k = 0, tiles = 0;
+  int32_t most_q = 0, most_k = 0;
+  const int tile = prompt_tile_tokens();
+  for (int32_t b = 0; b < n_seq; ++b) {
+    if (q_len[b] < 0 || k_len[b] < 0 || q_len[b] > kMostPromptTokens || k_len[b] > kMostPromptTokens) return BAKLAVA_EINVAL;
+    n_q += q_len[b];
+    n_k += k_len[b];
+    tiles += (q_len[b] + tile - 1) / tile;
+    most_q = std::max(most_q, q_len[b]);
+    most_k = std::max(most_k, k_len[b]);
+  }
+  if (n_q > INT32_MAX || n_k > INT32_MAX || tiles * Hq > INT32_MAX / 1024) return BAKLAVA_EINVAL;
+  if (n_q == 0) return BAKLAVA_OK;
+  if (!rows_ok(q, n_seq, most_q, Hq, 8, 16) || !written_rows_ok(out, n_seq, most_q, Hq, 8, 16, D)) return BAKLAVA_EINVAL;
+  if (n_k > 0 && (!rows_ok(k, n_seq, most_k, Hkv, 8, 16) || !rows_ok(v, n_seq, most_k, Hkv, 8, 16))) return BAKLAVA_EINVAL;
+  if (lse && !written_rows_ok(lse, n_seq, most_q, Hq, 1, 4, 1)) return BAKLAVA_EINVAL;
+  try {
+    // Sequences with most work first: a launch's last workgroups should be short ones.
+    std::vector<PromptParams::Seq> seq;
+    seq.reserve(n_seq);
+    int32_t q_first = 0, k_first = 0;
+    for (int32_t b = 0; b < n_seq; ++b) {
+      if (q_len[b] > 0) seq.push_back(PromptParams::Seq{b, q_first, k_first, q_len[b], k_len[b], 0});
+      q_first += q_len[b];
+      k_first += k_len[b];
+    }
+    std::stable_sort(seq.begin(), seq.end(), [](const PromptParams::Seq& a, const PromptParams::Seq& b) { return a.k_len > b.k_len; });
+    PromptParams p{};
+    p.q = device_rows(q, 2, 1); p.out = device_rows(out, 2, 1);
+    p.k = n_k > 0 ? device_rows(k, 2, 1) : Rows{};
+    p.v = n_k > 0 ? device_rows(v, 2, 1) : Rows{};
+    p.lse = device_rows(lse, 4, 1);
+    p.Hq = Hq; p.Hkv = Hkv;
+    p.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)D));
+    for (size_t at = 0; at < seq.size(); at += kPromptSeqs) {
+      p.n_seq = (int32_t)std::min<size_t>(kPromptSeqs, seq.size() - at);
+      int32_t end = 0;
+      for (int32_t i = 0; i < p.n_seq; ++i) {
+        p.seq[i] = seq[at + i];
+        end += (p.seq[i].q_len + tile - 1) / tile;
+        p.seq[i].tile_end = end;
+      }
+      if (!hip_ok(launch_prompt_attn(p, D, end, (hipStream_t)stream))) return BAKLAVA_EHIP;
+    }
+  } catch (const std::bad_alloc&) {
+    return BAKLAVA_ENOMEM;
+  }
+  return BAKLAVA_OK;
+}
+
+extern "C" int baklava_append_prompt(baklava_ctx* ctx, int32_t layer, const baklava_rows* k, const baklava_rows* v,
+                                     const int32_t* n_tok, const int32_t* pos0, const baklava_rows* scores, void* stream) {
+  if (!ctx || !n_tok || !range_ok(ctx, layer, 1)) return BAKLAVA_EINVAL;
+  const int32_t batch = ctx->d.batch, Hkv = ctx->d.Hkv;
+  const int64_t c0 = (int64_t)layer * ctx->cpl;
+  int64_t total = 0;
+  int32_t most = 0;
+  for (int32_t b = 0; b < batch; ++b) {
+    if (n_tok[b] < 0 || n_tok[b] > kMostPromptTokens) return BAKLAVA_EINVAL;
+    if (pos0 && (int64_t)pos0[b] + n_tok[b] > (int64_t)INT32_MAX + 1) return BAKLAVA_EINVAL;
+    total += n_tok[b];
+    most = std::max(most, n_tok[b]);
+  }
+  if (total > INT32_MAX) return BAKLAVA_EINVAL;
+  if (total == 0) return BAKLAVA_OK;
+  const int unit = ctx->d.dtype == BAKLAVA_F32 ? 4 : 8;
+  if (!rows_ok(k, batch, most, Hkv, unit, 16) || !rows_ok(v, batch, most, Hkv, unit, 16)) return BAKLAVA_EINVAL;
+  if (scores && !rows_ok(scores, batch, most, Hkv, 1, 4)) return BAKLAVA_EINVAL;
+  for (int32_t b = 0; b < batch; ++b)
+    for (int32_t h = 0; h < Hkv; ++h)
+      if (n_tok[b] > ctx->cap[c0 + b * Hkv + h] - ctx->len[c0 + b * Hkv + h]) return BAKLAVA_ECAPACITY;
+  PromptRowsParams p{};
+  p.k = device_rows(k, 1, unit); p.v = device_rows(v, 1, unit);
+  p.scores = device_rows(scores, 1, 1);
+  p.k_plane = ctx->d.k; p.v_plane = ctx->d.v;
+  p.kv_scale = reinterpret_cast<uint8_t*>(ctx->d.kv_scale);
+  p.score = ctx->d.score; p.pos = ctx->d.pos; p.off = ctx->d.off; p.len = ctx->d.len;
+  p.Hkv = Hkv;
+  const int32_t heads = std::min(Hkv, kPromptCaches);
+  const int32_t seqs = std::min(kPromptSeqs, kPromptCaches / heads);
+  int32_t first = 0;
+  for (int32_t b0 = 0; b0 < batch; b0 += seqs) {
+    const int32_t nb = std::min(seqs, batch - b0);
+    int32_t longest = 0;
+    for (int32_t i = 0; i < nb; ++i) {
+      p.seq[i] = PromptRowsParams::Seq{n_tok[b0 + i], first, pos0 ? pos0[b0 + i] : 0};
+      first += n_tok[b0 + i];
+      longest = std::max(longest, n_tok[b0 + i]);
+    }
+    for (int32_t h0 = 0; h0 < Hkv; h0 += heads) {
+      const int32_t nh = std::min(heads, Hkv - h0);
+      p.cache0 = (int32_t)(c0 + (int64_t)b0 * Hkv);
+      p.head0 = h0; p.seq0 = b0;
+      for (int32_t i = 0; i < nb; ++i)
+        for (int32_t h = 0; h < nh; ++h) p.start[i * nh + h] = ctx->len[c0 + (int64_t)(b0 + i) * Hkv + h0 + h];
+      if (!hip_ok(launch_append_prompt(p, query_row_bytes(&ctx->d) / 16, ctx->d.dtype == BAKLAVA_MXFP4, nh, nb, longest,
+                                       (hipStream_t)stream)))
+        return BAKLAVA_EHIP;
+    }
+  }
+  for (int32_t b = 0; b < batch; ++b)
+    for (int32_t h = 0; h < Hkv; ++h) ctx->len[c0 + b * Hkv + h] += n_tok[b];
+  return BAKLAVA_OK;
+}
+
+extern "C" int baklava_read_rows(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count, int32_t n, void* k_out,
+                                 void* v_out, void* stream) {
+  if (!ctx || !k_out || !v_out || !range_ok(ctx, layer_begin, layer_count)) return BAKLAVA_EINVAL;
+  if (n < 1 || n > kMostPromptTokens || (((uintptr_t)k_out | (uintptr_t)v_out) & 15)) return BAKLAVA_EINVAL;
+  ReadRowsParams p;
+  p.k_plane = ctx->d.k; p.v_plane = ctx->d.v;
+  p.kv_scale = reinterpret_cast<const uint8_t*>(ctx->d.kv_scale);
+  p.off = ctx->d.off; p.len = ctx->d.len;
+  p.k_out = k_out; p.v_out = v_out;
+  p.cache0 = layer_begin * ctx->cpl;
+  p.n = n;
+  if (!hip_ok(launch_read_rows(p, query_row_bytes(&ctx->d) / 16, ctx->d.dtype == BAKLAVA_MXFP4, layer_count * ctx->cpl,
+                               (hipStream_t)stream)))
     return BAKLAVA_EHIP;
   return BAKLAVA_OK;
 }

@@ -123,8 +123,9 @@ struct DecodeParams {
   int64_t logit_stride;
   int32_t fused_append;            // 1: every cache of the range first receives its new row
   int32_t token_pos;
-  int32_t row_bytes;
+  int32_t row_bytes;               // of a query row, and of a cache row unless it has 4-bit elements
   float scale_log2e;               // log2(e) / sqrt(D)
+  uint8_t* kv_scale;               // 4-bit rows: [total_tokens, D / 16] scale bytes, K's before V's
 };
 
 // Score pass over the K rows alone (bf16 rows of 128 elements on the vector kernel), behind the combine kernel:
@@ -155,6 +156,73 @@ struct AppendParams {
   int32_t cache_begin;
   int32_t token_pos;
   int32_t row_bytes;
+  uint8_t* kv_scale;             // 4-bit rows only
+};
+
+// Rows by sequence, token and head (baklava_rows).
+struct Rows {
+  void* data;
+  int64_t seq, tok, head;  // seq == 0: packed
+#ifdef __HIPCC__
+  // offset of the first row of sequence b, `first` tokens behind the first of all
+  __device__ __forceinline__ int64_t begin(int b, int first) const { return seq ? b * seq : first * tok; }
+#endif
+};
+
+struct RopeParams {
+  Rows q, k, q_out, k_out;  // strides in elements
+  const void* q_weight;     // [D] or null: not normed
+  const void* k_weight;
+  const int32_t* pos;       // [axes, n_seq * T]
+  float eps;
+  int32_t n_seq, T, Hq, Hkv;
+  int32_t rot;              // elements that are rotated
+  int32_t tok;              // tokens per workgroup
+  int32_t seq0;             // first sequence of the launch
+  double turns[64];         // frequency of every pair, in turns per position
+  uint8_t axis[64];         // its axis
+};
+
+constexpr int kPromptSeqs = 128;  // sequences per launch: their records travel with the kernel's arguments
+struct PromptParams {
+  Rows q, k, v, out, lse;   // strides in bytes
+  int32_t Hq, Hkv, n_seq;
+  float scale_log2e;
+  struct Seq {
+    int32_t b, q_first, k_first;  // sequence, tokens and keys in front of it (packed rows)
+    int32_t q_len, k_len;
+    int32_t tile_end;             // tiles of the sequences up to and with this one
+  } seq[kPromptSeqs];
+};
+
+constexpr int kPromptCaches = 512;
+struct PromptRowsParams {
+  Rows k, v;                // strides in 16-byte pieces
+  Rows scores;              // in floats; data null: zeros
+  void* k_plane;
+  void* v_plane;
+  uint8_t* kv_scale;
+  float* score;
+  int32_t* pos;
+  const int64_t* off;
+  int32_t* len;
+  int32_t cache0, Hkv;      // cache of sequence 0 of the launch, head 0
+  int32_t head0, seq0;
+  struct Seq {
+    int32_t n, first, pos0;
+  } seq[kPromptSeqs];
+  int32_t start[kPromptCaches];  // [sequence][head of the launch] live rows
+};
+
+struct ReadRowsParams {
+  const void* k_plane;
+  const void* v_plane;
+  const uint8_t* kv_scale;
+  const int64_t* off;
+  const int32_t* len;
+  void* k_out;
+  void* v_out;
+  int32_t cache0, n;
 };
 
 constexpr int kLengthsPerLaunch = 512;
@@ -187,6 +255,7 @@ struct CompactParams {
   int32_t* tile_hist;      // [all tiles][4 passes][256] digit counters, indexed by first_tile + tile
   SelState* sel_state;     // [long caches][4] state after pass 0..3
   int32_t long_rows;       // caches with more capacity than this are ranked tile by tile
+  uint8_t* kv_scale;       // 4-bit rows only
 };
 
 // Records a failed HIP call for baklava_last_hip_error() (per host thread).
@@ -202,6 +271,10 @@ hipError_t launch_decode_mfma(const DecodeParams& p, int D, int n_items, int max
 hipError_t prepare_decode_mfma();
 hipError_t launch_decode_mfma_f32(const DecodeParams& p, int D, int n_items, int max_count, bool one_wave, hipStream_t s);
 hipError_t prepare_decode_mfma_f32();
+// 4-bit rows: attention, and the flush of its records
+hipError_t launch_decode_mxfp4(const DecodeParams& p, int D, int n_items, int max_count, bool one_wave, hipStream_t s);
+hipError_t launch_score_flush_mxfp4(const DecodeParams& p, int D, int n_items, int max_count, hipStream_t s);
+hipError_t prepare_decode_mxfp4();
 // the weights of the calls on record, from the K rows alone, after which the records are empty where flush_ticket is not
 // null (bf16, D = 128; needs only the lag_*, flush_ticket, k, score, items, G and scale fields, and all work items of a
 // cache in the launch)
@@ -221,6 +294,13 @@ hipError_t launch_finish(const DecodeParams& p, int D, int n_multi, int most_spl
 // max_count: the largest row count of a work item in the launched range (or a bound on it)
 hipError_t launch_score_pass(const ScoreParams& p, int n_items, int max_count, hipStream_t s);
 hipError_t launch_append(const AppendParams& p, int n_caches, hipStream_t s);
+hipError_t launch_append_mx(const AppendParams& p, int D, int n_caches, hipStream_t s);  // 4-bit rows
+hipError_t launch_qk_norm_rope(const RopeParams& p, int dtype, int D, bool interleaved, hipStream_t s);
+hipError_t launch_prompt_attn(const PromptParams& p, int D, int n_tiles, hipStream_t s);
+int prompt_tile_tokens();  // query tokens per workgroup
+// pieces: 16-byte pieces of a row as the caller holds it; most: tokens of the longest sequence
+hipError_t launch_append_prompt(const PromptRowsParams& p, int pieces, bool mx, int n_heads, int n_seq, int most, hipStream_t s);
+hipError_t launch_read_rows(const ReadRowsParams& p, int pieces, bool mx, int n_caches, hipStream_t s);
 hipError_t launch_set_lengths(const LengthsParams& p, hipStream_t s);
 hipError_t launch_fill_i32(int32_t* dst, int32_t value, int64_t n, hipStream_t s);
 // n_wide: caches of the range with more than kNarrowRows rows of capacity; sorted: they come first in p.order

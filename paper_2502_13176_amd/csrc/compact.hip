@@ -822,9 +822,11 @@ template <int PIECES, int ROWS>
 struct MoveTile {
   static_assert(ROWS <= kMoveThreads && ROWS >= kMoveRowsMin, "a thread per score, a flag per tile");
   static constexpr int kPerPlane = ROWS * PIECES / kMoveThreads;  // pieces per thread and plane
+  static constexpr int kScaleWords = PIECES <= 4 ? PIECES / 2 : 0;  // 4-bit rows: words of scales per row
   uint4 kb[kPerPlane], vb[kPerPlane];
   float sc;
   int ps;
+  uint32_t mx[kScaleWords ? kScaleWords : 1];
 
   // Destination rows p0 .. e of the cache at `off`; ends with a barrier behind which the workgroup has read all of them.
   __device__ __forceinline__ void load(const CompactParams& p, int64_t off, int p0, int e) {
@@ -845,6 +847,9 @@ struct MoveTile {
       const int src = kept[p0 + tid];
       sc = p.score[off + src];
       ps = p.pos[off + src];
+#pragma unroll
+      for (int i = 0; i < kScaleWords; ++i)
+        mx[i] = reinterpret_cast<const uint32_t*>(p.kv_scale)[(off + src) * kScaleWords + i];
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wavefront's rows are here
     __syncthreads();                                  // and those of the others
@@ -866,6 +871,9 @@ struct MoveTile {
     if (tid < e - p0) {
       p.score[off + p0 + tid] = sc;
       p.pos[off + p0 + tid] = ps;
+#pragma unroll
+      for (int i = 0; i < kScaleWords; ++i)
+        reinterpret_cast<uint32_t*>(p.kv_scale)[(off + p0 + tid) * kScaleWords + i] = mx[i];
     }
   }
 };
@@ -1014,6 +1022,8 @@ hipError_t launch_compact_move(const CompactParams& p, int c0, int n_caches, con
     const int n_short = before[at + n].short_caches - before[at].short_caches;
     if (n_tiles == 0 && n_short == 0) continue;  // no cache has more rows than its budget
     switch (p.row_bytes / 16) {
+      case 2: launch_move<2>(p, c0 + at, n, n_tiles, n_short, n_cus, s); break;
+      case 4: launch_move<4>(p, c0 + at, n, n_tiles, n_short, n_cus, s); break;
       case 8: launch_move<8>(p, c0 + at, n, n_tiles, n_short, n_cus, s); break;
       case 16: launch_move<16>(p, c0 + at, n, n_tiles, n_short, n_cus, s); break;
       case 32: launch_move<32>(p, c0 + at, n, n_tiles, n_short, n_cus, s); break;
