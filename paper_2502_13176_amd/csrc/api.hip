@@ -177,6 +177,12 @@ namespace {
 // (three) 66.7 / 65.3 and 82.1 / 80.3; D = 64, 64 18.1 / 15.3 and 29.6 / 24.1; fp32, D = 128, 64 53.3 / 47.0 and 68.9 / 55.8;
 // 128 caches of 65536 rows (four) 632 / 627 and 733 / 724, with two 628 and 736; 256 of 8192 rows with four instead of five
 // 160 / 163 (one head) and 165 / 165, with two 197.
+// 4-bit rows: one round of workgroups, which are of eight wavefronts; two to a compute unit where there is enough to read
+// (one alone keeps too few loads in flight), one where each more work item costs more than it gives.  us per call with one /
+// two / five, attention alone, four heads, D = 128: 8 caches of 32768 rows 14.6 / 14.8 / 18.6, 64 of 10000 22.0 / 22.3 / 26.4, of
+// 32768 60.6 / 52.4 / 61.2, 256 of 2000 16.5 / 18.6 / 24.2, of 8192 54.1 / 54.2 / 57.1.
+int mx_items_per_cu(int64_t rows, int64_t cus) { return rows <= 2560 * cus ? 1 : 2; }
+
 int whole_items_per_cu(int64_t n_caches, int64_t rows, int64_t cus) {
   if (4 * n_caches <= 2 * cus) return rows <= 2 * cus * 8192 ? 2 : 4;
   if (4 * n_caches <= 3 * cus) return 3;
@@ -371,7 +377,7 @@ int flush_records(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count, hi
   p.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)ctx->d.D));
   const int32_t longest = *std::max_element(sc.max_count.begin() + layer_begin,
                                             sc.max_count.begin() + layer_begin + layer_count);
-  if (!hip_ok(ctx->d.dtype == BAKLAVA_MXFP4 ? launch_score_flush_mxfp4(p, ctx->d.D, i1 - i0, longest, s)
+  if (!hip_ok(ctx->d.dtype == BAKLAVA_MXFP4 ? launch_score_flush_mxfp4(p, ctx->d.D, i1 - i0, s)
                                             : launch_score_flush_mfma(p, i1 - i0, longest, s)))
     return BAKLAVA_EHIP;
   if (!self_clear && !hip_ok(launch_fill_i32(p.lag_cnt + c0 * ctx->G, 0, (c1 - c0) * ctx->G, s))) return BAKLAVA_EHIP;
@@ -456,6 +462,8 @@ int decode_impl(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count, cons
   p.logit_stride = ctx->total_tokens;
   const int32_t longest = *std::max_element(sc.max_count.begin() + layer_begin,
                                             sc.max_count.begin() + layer_begin + layer_count);
+  const int32_t most_split = *std::max_element(sc.max_split.begin() + layer_begin,
+                                               sc.max_split.begin() + layer_begin + layer_count);
   p.fused_append = fused ? 1 : 0;
   p.token_pos = token_pos;
   p.row_bytes = query_row_bytes(&ctx->d);
@@ -473,7 +481,7 @@ int decode_impl(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count, cons
     if (!(ctx->time_kernel == 2 && use_mfma) && !hip_ok(hipEventRecord(ev0, s))) return BAKLAVA_EHIP;
   }
   const bool on_dispatch = ctx->time_kernel == 2 && use_mfma;
-  hipError_t e = mx ? launch_decode_mxfp4(p, ctx->d.D, i1 - i0, longest, i1 - i0 <= ctx->n_cus, s)
+  hipError_t e = mx ? launch_decode_mxfp4(p, ctx->d.D, i1 - i0, s)
                : use_mfma ? launch_decode_mfma(p, ctx->d.D, i1 - i0, longest, i1 - i0 <= ctx->n_cus, s,
                                                on_dispatch ? ev0 : nullptr, on_dispatch ? ev1 : nullptr)
                : ctx->kernel_pref == 0 && f32_on_matrix_cores(ctx)
@@ -484,8 +492,6 @@ int decode_impl(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count, cons
     if (!on_dispatch && !hip_ok(hipEventRecord(ev1, s))) return BAKLAVA_EHIP;
     ctx->ev_used += 1;
   }
-  const int32_t most_split = *std::max_element(sc.max_split.begin() + layer_begin,
-                                               sc.max_split.begin() + layer_begin + layer_count);
   if (from_logits) {
     if (!hip_ok(launch_finish(p, ctx->d.D, m1 - m0, most_split, i1 - i0, longest, s))) return BAKLAVA_EHIP;
   } else {
@@ -575,6 +581,10 @@ extern "C" int baklava_create(const baklava_desc* desc, const int64_t* off_host,
     ctx->target_items = ctx->layer_one_wave ? cus : kWholeItemsPerCu * cus;
     ctx->n_cus = cus;
     ctx->target_items_whole = whole_items_per_cu(n_caches, packed, cus) * cus;
+    if (desc->dtype == BAKLAVA_MXFP4) {
+      ctx->target_items = mx_items_per_cu(packed / desc->L, cus) * cus;
+      ctx->target_items_whole = mx_items_per_cu(packed, cus) * cus;
+    }
   }
   ctx->time_kernel = 0;
   ctx->track_on = desc->track_scores != 0;
@@ -630,7 +640,6 @@ extern "C" int baklava_create(const baklava_desc* desc, const int64_t* off_host,
     if (st != BAKLAVA_OK) { delete ctx; return st; }
   }
   if (desc->dtype == BAKLAVA_BF16 && !hip_ok(prepare_decode_mfma())) { delete ctx; return BAKLAVA_EHIP; }
-  if (desc->dtype == BAKLAVA_MXFP4 && !hip_ok(prepare_decode_mxfp4())) { delete ctx; return BAKLAVA_EHIP; }
   if (desc->dtype == BAKLAVA_F32 && !hip_ok(prepare_decode_mfma_f32())) { delete ctx; return BAKLAVA_EHIP; }
   const int chunk = ctx->layer_one_wave ? kDefaultChunk : kDefaultChunkWhole;
   const int chunk_layer = slow_rows(ctx) ? kDefaultChunkWhole : chunk;  // (see build_schedule)

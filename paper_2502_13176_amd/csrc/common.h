@@ -272,9 +272,8 @@ hipError_t prepare_decode_mfma();
 hipError_t launch_decode_mfma_f32(const DecodeParams& p, int D, int n_items, int max_count, bool one_wave, hipStream_t s);
 hipError_t prepare_decode_mfma_f32();
 // 4-bit rows: attention, and the flush of its records
-hipError_t launch_decode_mxfp4(const DecodeParams& p, int D, int n_items, int max_count, bool one_wave, hipStream_t s);
-hipError_t launch_score_flush_mxfp4(const DecodeParams& p, int D, int n_items, int max_count, hipStream_t s);
-hipError_t prepare_decode_mxfp4();
+hipError_t launch_decode_mxfp4(const DecodeParams& p, int D, int n_items, hipStream_t s);
+hipError_t launch_score_flush_mxfp4(const DecodeParams& p, int D, int n_items, hipStream_t s);
 // the weights of the calls on record, from the K rows alone, after which the records are empty where flush_ticket is not
 // null (bf16, D = 128; needs only the lag_*, flush_ticket, k, score, items, G and scale fields, and all work items of a
 // cache in the launch)

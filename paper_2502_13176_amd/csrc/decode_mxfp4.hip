@@ -1,6 +1,6 @@
 // Decode attention over ragged caches of 4-bit rows (BAKLAVA_MXFP4), up to 16 query heads per KV head.
 //
-// The two products of a slab of 32 rows are those of the bf16 kernel (v_mfma_f32_16x16x32_bf16):
+// The two products of 32 rows are those of the bf16 kernel (v_mfma_f32_16x16x32_bf16):
 //
 //   S^T[row, g]  = K[row, :] . Q[g, :]          O^T[d, g] += V^T[d, rows] . P^T[rows, g]
 //
@@ -15,9 +15,6 @@
 #include "decode_tail.h"
 #include "mxfp4.h"
 
-#include <algorithm>
-#include <type_traits>
-
 namespace baklava {
 
 namespace {
@@ -27,7 +24,8 @@ typedef float floatx4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
-constexpr int kSlab = 32;   // rows per wavefront iteration, two tiles of 16
+constexpr int kTiles = 2;             // tiles of 16 rows per wavefront iteration
+constexpr int kSlab = 16 * kTiles;
 constexpr int kWaves = 8;
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLowest = -3.402823466e38f;
@@ -40,7 +38,6 @@ struct Shape {
   static constexpr int kBlocks = D / 16;
   static constexpr int kQRow = D * 2;              // bytes of a query row
   static constexpr int kVStride = D * 2 + 32;      // bytes between staged V rows
-  static constexpr int kStatic = kWaves * kSlab * kVStride;
 };
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -98,14 +95,14 @@ __device__ __forceinline__ void load_record(const DecodeParams& p, int c, int G,
   }
 }
 
-// Weights of the recorded calls for the 32 rows of a slab; on return lane l < 32 holds that of row l.
+// Weights of the recorded calls for the rows of a slab; on return lane l < kSlab holds that of row l.
 template <int D>
-__device__ __forceinline__ float record_weights(const floatx4_t (&sp)[kSets][2], const Record<D>& r, float cs, int row_first,
+__device__ __forceinline__ float record_weights(const floatx4_t (&sp)[kSets][kTiles], const Record<D>& r, float cs, int row_first,
                                                 int lane) {
   const int n16 = lane & 15;
-  float w[2];
+  float w[kTiles];
 #pragma unroll
-  for (int T = 0; T < 2; ++T) {
+  for (int T = 0; T < kTiles; ++T) {
     w[T] = 0.f;
 #pragma unroll
     for (int e = 0; e < kSets; ++e) {
@@ -117,7 +114,10 @@ __device__ __forceinline__ float record_weights(const floatx4_t (&sp)[kSets][2],
     w[T] += __shfl_xor(w[T], 16);
     w[T] += __shfl_xor(w[T], 32);
   }
-  return (lane & 16) ? w[1] : w[0];
+  float mine = w[0];
+#pragma unroll
+  for (int T = 1; T < kTiles; ++T) mine = lane >> 4 == T ? w[T] : mine;
+  return mine;
 }
 
 // The new row of a fused append, rounded, into slot n_old (see append_new_row).
@@ -136,90 +136,144 @@ __device__ __forceinline__ void append_new_row_mx(const DecodeParams& p, const I
   __syncthreads();
 }
 
-// One slab of a plane: two tiles of 16 rows with the scale of each lane's elements.
+// One slab of a plane: tiles of 16 rows with the scale of each lane's elements.
 template <int D>
 struct Slab {
-  Codes<Shape<D>::kWords> c[2];
-  uint32_t s[2];
+  Codes<Shape<D>::kWords> c[kTiles];
+  uint32_t s[kTiles];
 };
 
+// plane, scale: this lane's place in the first row of the first tile of the work item
 template <int D>
-__device__ __forceinline__ void load_slab(Slab<D>& b, const unsigned char* plane, const uint8_t* scale, int t0, int row, int piece,
-                                          int last) {
+__device__ __forceinline__ void load_slab(Slab<D>& b, const unsigned char* plane, const uint8_t* scale, int t0, int row, int cnt) {
+  if (t0 + kSlab <= cnt) {
 #pragma unroll
-  for (int T = 0; T < 2; ++T) {
-    const uint32_t r = (uint32_t)min(t0 + T * 16 + row, last);
-    load_codes(b.c[T], plane + r * (uint32_t)Shape<D>::kBytes + piece * (D / 8));
-    b.s[T] = scale[r * (uint32_t)(D / 16) + (D == 128 ? piece : piece / 2)];
+    for (int T = 0; T < kTiles; ++T) {
+      load_codes(b.c[T], plane + (uint32_t)t0 * Shape<D>::kBytes + T * 16 * Shape<D>::kBytes);
+      b.s[T] = scale[(uint32_t)t0 * (D / 16) + T * 16 * (D / 16)];
+    }
+  } else {  // rows past the last one repeat it: they weigh nothing
+#pragma unroll
+    for (int T = 0; T < kTiles; ++T) {
+      const int r = min(t0 + T * 16, cnt - 1 - row);
+      load_codes(b.c[T], plane + r * Shape<D>::kBytes);
+      b.s[T] = scale[r * (D / 16)];
+    }
   }
 }
 
+// The weights of the recorded calls for rows [0, cnt) of a work item whose first row is row `start` of its cache: K alone is
+// read, scores are read with it, and the new ones wait in LDS (this wavefront's `slots` slabs at `ring`), so that they are
+// written together.
+template <int D>
+__device__ __forceinline__ void add_recorded(const DecodeParams& p, const Item& it, int cnt, int pending, float* ring, int slots) {
+  using S = Shape<D>;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n16 = lane & 15, jg = lane >> 4;
+  Record<D> rec;
+  load_record<D>(p, it.c, p.G, pending, n16, jg, rec);
+  const unsigned char* Kb = reinterpret_cast<const unsigned char*>(p.k) + (it.row0 + n16) * S::kBytes + jg * (D / 8);
+  const uint8_t* Sb = p.kv_scale + (it.row0 + n16) * (D / 16) + (D == 128 ? jg : jg / 2);
+  float* const sc_base = p.score + it.row0;
+  const float cs = p.scale_log2e;
+  Slab<D> kr;
+  float sc_cur = 0.f;
+  int ring_n = 0, ring_t0 = 0;
+  auto flush_ring = [&]() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    for (int i = lane; i < ring_n * kSlab; i += 64) {
+      const int r = ring_t0 + i / kSlab * (kWaves * kSlab) + i % kSlab;
+      if (r < cnt) sc_base[r] = ring[i];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();  // the area may be written again
+    ring_n = 0;
+  };
+  int t0 = wave * kSlab;
+  if (t0 < cnt) {
+    load_slab<D>(kr, Kb, Sb, t0, n16, cnt);
+    if (lane < kSlab) sc_cur = sc_base[min(t0 + lane, cnt - 1)];
+  }
+  for (; t0 < cnt; t0 += kWaves * kSlab) {
+    const int tn = t0 + kWaves * kSlab;
+    floatx4_t sp[kSets][kTiles];
+#pragma unroll
+    for (int T = 0; T < kTiles; ++T) {
+#pragma unroll
+      for (int e = 0; e < kSets; ++e) sp[e][T] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+      const float scale = mx_scale(kr.s[T]);
+#pragma unroll
+      for (int c = 0; c < S::kChunks; ++c) {
+        const bf16x8_t a = as_bf16x8(mx_values(kr.c[T].w[c], scale));
+#pragma unroll
+        for (int e = 0; e < kSets; ++e) sp[e][T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(rec.q[e][c], a, sp[e][T], 0, 0, 0);
+      }
+    }
+    const float sc_old = sc_cur;
+    if (tn < cnt) {
+      load_slab<D>(kr, Kb, Sb, tn, n16, cnt);
+      if (lane < kSlab) sc_cur = sc_base[min(tn + lane, cnt - 1)];
+    }
+    const float wr = record_weights<D>(sp, rec, cs, it.start + t0, lane);
+    if (ring_n == 0) ring_t0 = t0;
+    if (lane < kSlab) ring[ring_n * kSlab + lane] = sc_old + wr;
+    if (++ring_n == slots) flush_ring();
+  }
+  if (ring_n > 0) flush_ring();
+}
+
 template <int D, bool TRACK>
-__global__ __launch_bounds__(64 * kWaves, 2) void decode_partial_mxfp4(DecodeParams p) {
+__global__ __launch_bounds__(64 * kWaves, 4) void decode_partial_mxfp4(DecodeParams p) {
   using S = Shape<D>;
   constexpr int kVStride = S::kVStride;
   __shared__ __attribute__((aligned(16))) unsigned char lds[kWaves * kSlab * kVStride];
-  extern __shared__ __attribute__((aligned(16))) float lds_ring[];  // new scores that wait ([32] per slab and wavefront)
 
   const Item it = p.items[blockIdx.x];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n16 = lane & 15, jg = lane >> 4;
   const int G = p.G;
+  const int v_row = lane >> 2, v_piece = lane & 3;
+  const unsigned char* Kb = reinterpret_cast<const unsigned char*>(p.k) + (it.row0 + n16) * S::kBytes + jg * (D / 8);
+  const unsigned char* Vb = reinterpret_cast<const unsigned char*>(p.v) + (it.row0 + v_row) * S::kBytes + v_piece * (D / 8);
+  const uint8_t* KSb = p.kv_scale + (it.row0 + n16) * (D / 16) + (D == 128 ? jg : jg / 2);
+  const uint8_t* VSb = p.kv_scale + (it.row0 + v_row) * (D / 16) + D / 32 + (D == 128 ? v_piece : v_piece / 2);
+  // The first slab is requested before the cache's length is known (its rows lie within the capacity); a slab that turns out
+  // not to be made of old rows alone is requested again.
+  Slab<D> kr, vr;
+  int t0 = wave * kSlab;
+  if (t0 + kSlab <= it.count) {
+    load_slab<D>(kr, Kb, KSb, t0, n16, it.count);
+    load_slab<D>(vr, Vb, VSb, t0, v_row, it.count);
+  }
   const int n_old = p.len[it.c];
   const int64_t off_c = it.row0 - it.start;
   const int add = (p.fused_append && n_old < p.cap[it.c]) ? 1 : 0;
   const int n = n_old + add;
   const int token_pos = p.token_pos_dev ? *p.token_pos_dev : p.token_pos;
   const int pending = TRACK ? p.lag_cnt[(int64_t)it.c * G] : 0;
-  const bool apply = TRACK && pending >= p.lag_batch;
-  Record<D> rec;
-  if (TRACK && apply) load_record<D>(p, it.c, G, pending, n16, jg, rec);
   if (p.fused_append) {
     if (add) append_new_row_mx<D>(p, it, n_old, off_c, token_pos);
     else if (it.start == 0 && threadIdx.x == 0) *p.status = 1;
   }
   int cnt = min(it.start + it.count, n) - it.start;
   if (cnt < 0) cnt = 0;
-  const int64_t row0 = it.row0;
-  const unsigned char* Kb = reinterpret_cast<const unsigned char*>(p.k) + row0 * S::kBytes;
-  const unsigned char* Vb = reinterpret_cast<const unsigned char*>(p.v) + row0 * S::kBytes;
-  const uint8_t* Sb = p.kv_scale + row0 * (D / 16);
   unsigned char* myl = lds + wave * (kSlab * kVStride);
-  const int64_t qrow0 = (int64_t)(it.c - p.cache_begin) * G;
+  // A full record: its weights are added first, by a pass over the K rows of their own, which the attention then finds in a
+  // cache.  (In one pass the record's operands and results are live beside everything else: 216 registers instead of 128.)
+  if (TRACK && pending >= p.lag_batch) add_recorded<D>(p, it, cnt, pending, reinterpret_cast<float*>(myl), kVStride / 4);
 
+  const int64_t qrow0 = (int64_t)(it.c - p.cache_begin) * G;
   floatx4_t o[S::kBlocks];
 #pragma unroll
   for (int b = 0; b < S::kBlocks; ++b) o[b] = floatx4_t{0.f, 0.f, 0.f, 0.f};
   float m_run = kLowest;  // running max of head n16, log2 units (see the bf16 kernel)
   float l_part = 0.f;
   const float cs = p.scale_log2e;
-  const int last = cnt - 1;  // rows past it repeat it and weigh nothing
-  const int v_row = lane >> 2, v_piece = lane & 3;
-  Slab<D> kr, vr;
-
-  float* const sc_base = p.score + row0;
-  float sc_cur = 0.f;
-  float* const ring = lds_ring + wave * p.ring_slots * kSlab;
-  int ring_n = 0, ring_t0 = 0;
-  auto flush_ring = [&]() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    for (int sidx = lane >> 5; sidx < ring_n; sidx += 2) {
-      const int r = ring_t0 + sidx * (kWaves * kSlab) + (lane & 31);
-      if (r < cnt) sc_base[r] = ring[sidx * kSlab + (lane & 31)];
-    }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    ring_n = 0;
-  };
-
-  auto stream_rows = [&](auto apply_tag) {
-  constexpr bool APPLY = decltype(apply_tag)::value;
-  int t0 = wave * kSlab;
-  if (t0 < cnt) {
-    load_slab<D>(kr, Kb, Sb, t0, n16, jg, last);
-    if (APPLY && lane < kSlab) sc_cur = sc_base[min(t0 + lane, last)];
+  if (t0 < cnt && t0 + kSlab > min(it.count, n_old - it.start)) {
+    load_slab<D>(kr, Kb, KSb, t0, n16, cnt);
+    load_slab<D>(vr, Vb, VSb, t0, v_row, cnt);
   }
   bf16x8_t qb[S::kChunks];  // B operand: lane (g, jg), chunk c holds Q[g][jg D / 4 + 8 c .. + 8]
 #pragma unroll
@@ -229,64 +283,45 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_partial_mxfp4(DecodePar
       raw = *reinterpret_cast<const uint4*>(reinterpret_cast<const unsigned char*>(p.q) + (qrow0 + n16) * S::kQRow + jg * (D / 2) + c * 16);
     qb[c] = as_bf16x8(raw);
   }
-  if (t0 < cnt) load_slab<D>(vr, Vb, Sb + D / 32, t0, v_row, v_piece, last);
 
   for (; t0 < cnt; t0 += kWaves * kSlab) {
     const int tn = t0 + kWaves * kSlab;
     // ---- S^T = K Q^T ---------------------------------------------------------------------------
-    floatx4_t s[2], sp[kSets][2];
+    floatx4_t s[kTiles];
 #pragma unroll
-    for (int T = 0; T < 2; ++T) {
+    for (int T = 0; T < kTiles; ++T) {
       s[T] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int e = 0; e < kSets; ++e) sp[e][T] = floatx4_t{0.f, 0.f, 0.f, 0.f};
       const float scale = mx_scale(kr.s[T]);
 #pragma unroll
-      for (int c = 0; c < S::kChunks; ++c) {
-        const bf16x8_t a = as_bf16x8(mx_values(kr.c[T].w[c], scale));
-        s[T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qb[c], s[T], 0, 0, 0);
-        if (APPLY) {
-#pragma unroll
-          for (int e = 0; e < kSets; ++e) sp[e][T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(rec.q[e][c], a, sp[e][T], 0, 0, 0);
-        }
-      }
+      for (int c = 0; c < S::kChunks; ++c)
+        s[T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(mx_values(kr.c[T].w[c], scale)), qb[c], s[T], 0, 0, 0);
     }
-    load_slab<D>(kr, Kb, Sb, tn, n16, jg, last);  // past the end every row clamps to the last live row: harmless re-reads
-    const float sc_old = sc_cur;
-    if (APPLY && lane < kSlab) sc_cur = sc_base[min(tn + lane, last)];
+    if (tn < cnt) load_slab<D>(kr, Kb, KSb, tn, n16, cnt);
 
     // ---- V rows as bf16 in LDS -------------------------------------------------------------------
 #pragma unroll
-    for (int T = 0; T < 2; ++T) {
+    for (int T = 0; T < kTiles; ++T) {
       const float scale = mx_scale(vr.s[T]);
 #pragma unroll
       for (int c = 0; c < S::kWords; ++c)
         *reinterpret_cast<uint4*>(myl + (T * 16 + v_row) * kVStride + v_piece * (D / 2) + c * 16) = mx_values(vr.c[T].w[c], scale);
     }
-    load_slab<D>(vr, Vb, Sb + D / 32, tn, v_row, v_piece, last);
+    if (tn < cnt) load_slab<D>(vr, Vb, VSb, tn, v_row, cnt);
 
     // ---- online softmax on the accumulator layout ------------------------------------------------
-    float x[8];
-#pragma unroll
-    for (int T = 0; T < 2; ++T)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[T * 4 + i] = s[T][i] * cs;
     if (t0 + kSlab > cnt) {
 #pragma unroll
-      for (int T = 0; T < 2; ++T)
+      for (int T = 0; T < kTiles; ++T)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (t0 + T * 16 + jg * 4 + i >= cnt) x[T * 4 + i] = kNegInf;
+          if (t0 + T * 16 + jg * 4 + i >= cnt) s[T][i] = kNegInf;
     }
-    if (APPLY) {
-      const float wr = record_weights<D>(sp, rec, cs, it.start + t0, lane);
-      if (ring_n == 0) ring_t0 = t0;
-      if (lane < kSlab) ring[ring_n * kSlab + lane] = sc_old + wr;
-      if (++ring_n == p.ring_slots) flush_ring();
-    }
-    float mx = x[0];
+    float mx = s[0][0];
 #pragma unroll
-    for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
+    for (int T = 0; T < kTiles; ++T)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[T][i]);
+    mx *= cs;
     if (__any(mx > m_run)) {
       mx = fmaxf(mx, __shfl_xor(mx, 16));
       mx = fmaxf(mx, __shfl_xor(mx, 32));
@@ -297,43 +332,41 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_partial_mxfp4(DecodePar
 #pragma unroll
       for (int b = 0; b < S::kBlocks; ++b) o[b] *= alpha;
     }
-    u32x4_t ph, pm;
-    bf16x8_t pl;
-#pragma unroll
-    for (int e = 0; e < 8; e += 2) {  // three terms: 8 bits, the next 8, and the rest
-      const float p0 = fast_exp2(x[e] - m_run), p1 = fast_exp2(x[e + 1] - m_run);
-      l_part += p0 + p1;
-      const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
-      ph[e / 2] = (u0 >> 16) | (u1 & 0xffff0000u);
-      const float r0 = p0 - __uint_as_float(u0 & 0xffff0000u), r1 = p1 - __uint_as_float(u1 & 0xffff0000u);
-      const uint32_t w0 = __float_as_uint(r0), w1 = __float_as_uint(r1);
-      pm[e / 2] = (w0 >> 16) | (w1 & 0xffff0000u);
-      pl[e] = (__bf16)(r0 - __uint_as_float(w0 & 0xffff0000u));
-      pl[e + 1] = (__bf16)(r1 - __uint_as_float(w1 & 0xffff0000u));
-    }
-
-    // ---- O^T += V^T P^T (transposed reads as in the bf16 kernel) ---------------------------------
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    const unsigned char* tr0 = myl + (jg * 4 + (n16 >> 2)) * kVStride + (n16 & 3) * 8;
+    // ---- O^T += V^T P^T, 32 rows at a time (transposed reads as in the bf16 kernel) ---------------
 #pragma unroll
-    for (int b = 0; b < S::kBlocks; ++b) {
-      typedef __attribute__((address_space(3))) s16x4_t* lds_ptr_t;
-      const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(tr0 + b * 32));
-      const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(tr0 + 16 * kVStride + b * 32));
-      const bf16x8_t a = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-      o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8_t, ph), o[b], 0, 0, 0);
-      o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8_t, pm), o[b], 0, 0, 0);
-      o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pl, o[b], 0, 0, 0);
+    for (int u = 0; u < kTiles / 2; ++u) {
+      u32x4_t ph, pm;
+      bf16x8_t pl;
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {  // three terms: 8 bits, the next 8, and the rest
+        const float p0 = fast_exp2(fmaf(s[2 * u + e / 4][e % 4], cs, -m_run)), p1 = fast_exp2(fmaf(s[2 * u + e / 4][e % 4 + 1], cs, -m_run));
+        l_part += p0 + p1;
+        const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
+        ph[e / 2] = (u0 >> 16) | (u1 & 0xffff0000u);
+        const float r0 = p0 - __uint_as_float(u0 & 0xffff0000u), r1 = p1 - __uint_as_float(u1 & 0xffff0000u);
+        const uint32_t w0 = __float_as_uint(r0), w1 = __float_as_uint(r1);
+        pm[e / 2] = (w0 >> 16) | (w1 & 0xffff0000u);
+        pl[e] = (__bf16)(r0 - __uint_as_float(w0 & 0xffff0000u));
+        pl[e + 1] = (__bf16)(r1 - __uint_as_float(w1 & 0xffff0000u));
+      }
+      const unsigned char* tr0 = myl + (u * 32 + jg * 4 + (n16 >> 2)) * kVStride + (n16 & 3) * 8;
+#pragma unroll
+      for (int b = 0; b < S::kBlocks; ++b) {
+        typedef __attribute__((address_space(3))) s16x4_t* lds_ptr_t;
+        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(tr0 + b * 32));
+        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(tr0 + 16 * kVStride + b * 32));
+        const bf16x8_t a = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8_t, ph), o[b], 0, 0, 0);
+        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8_t, pm), o[b], 0, 0, 0);
+        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pl, o[b], 0, 0, 0);
+      }
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
-  if (APPLY && ring_n > 0) flush_ring();
-  };  // stream_rows
-  if (TRACK && apply) stream_rows(std::integral_constant<bool, TRACK>{});
-  else stream_rows(std::false_type{});
 
   float l_tot = l_part;
   l_tot += __shfl_xor(l_tot, 16);
@@ -360,11 +393,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_partial_mxfp4(DecodePar
 // The recorded calls' weights from the K rows alone (see score_flush_mfma, also for the tickets).
 template <int D>
 __global__ __launch_bounds__(64 * kWaves) void score_flush_mxfp4(DecodeParams p) {
-  using S = Shape<D>;
-  extern __shared__ __attribute__((aligned(16))) float lds_ring[];
   const Item it = p.items[blockIdx.x];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int n16 = lane & 15, jg = lane >> 4;
   const int G = p.G;
   const int pending = p.lag_cnt[(int64_t)it.c * G];
   if (pending == 0) return;
@@ -387,112 +416,32 @@ __global__ __launch_bounds__(64 * kWaves) void score_flush_mxfp4(DecodeParams p)
     clear_record();
     return;
   }
-  Record<D> rec;
-  load_record<D>(p, it.c, G, pending, n16, jg, rec);
-  const int last = cnt - 1;
-  const unsigned char* Kb = reinterpret_cast<const unsigned char*>(p.k) + it.row0 * S::kBytes;
-  const uint8_t* Sb = p.kv_scale + it.row0 * (D / 16);
-  float* const sc_base = p.score + it.row0;
-  float* const ring = lds_ring + wave * p.ring_slots * kSlab;
-  const float cs = p.scale_log2e;
-  Slab<D> kr;
-  float sc_cur = 0.f;
-  int ring_n = 0, ring_t0 = 0;
-  auto flush_ring = [&]() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    for (int sidx = lane >> 5; sidx < ring_n; sidx += 2) {
-      const int r = ring_t0 + sidx * (kWaves * kSlab) + (lane & 31);
-      if (r < cnt) sc_base[r] = ring[sidx * kSlab + (lane & 31)];
-    }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    ring_n = 0;
-  };
-  int t0 = wave * kSlab;
-  if (t0 < cnt) {
-    load_slab<D>(kr, Kb, Sb, t0, n16, jg, last);
-    if (lane < kSlab) sc_cur = sc_base[min(t0 + lane, last)];
-  }
-  for (; t0 < cnt; t0 += kWaves * kSlab) {
-    const int tn = t0 + kWaves * kSlab;
-    floatx4_t sp[kSets][2];
-#pragma unroll
-    for (int T = 0; T < 2; ++T) {
-#pragma unroll
-      for (int e = 0; e < kSets; ++e) sp[e][T] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-      const float scale = mx_scale(kr.s[T]);
-#pragma unroll
-      for (int c = 0; c < S::kChunks; ++c) {
-        const bf16x8_t a = as_bf16x8(mx_values(kr.c[T].w[c], scale));
-#pragma unroll
-        for (int e = 0; e < kSets; ++e) sp[e][T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(rec.q[e][c], a, sp[e][T], 0, 0, 0);
-      }
-    }
-    const float sc_old = sc_cur;
-    load_slab<D>(kr, Kb, Sb, tn, n16, jg, last);
-    if (lane < kSlab) sc_cur = sc_base[min(tn + lane, last)];
-    const float wr = record_weights<D>(sp, rec, cs, it.start + t0, lane);
-    if (ring_n == 0) ring_t0 = t0;
-    if (lane < kSlab) ring[ring_n * kSlab + lane] = sc_old + wr;
-    if (++ring_n == p.ring_slots) flush_ring();
-  }
-  if (ring_n > 0) flush_ring();
+  constexpr int kSlots = 64;
+  __shared__ __attribute__((aligned(16))) float ring[kWaves * kSlots * kSlab];
+  add_recorded<D>(p, it, cnt, pending, ring + (threadIdx.x >> 6) * (kSlots * kSlab), kSlots);
   clear_record();
-}
-
-constexpr int kLdsTotal = 160 * 1024;
-template <int D> constexpr int dyn_alone() { return kLdsTotal - Shape<D>::kStatic - 512; }           // beside no other workgroup
-template <int D> constexpr int dyn_shared() { return (kLdsTotal - 2 * Shape<D>::kStatic - 1024) / 2; }
-constexpr int kFlushDyn = 48 * 1024;
-static_assert(dyn_shared<128>() >= kWaves * kSlab * 4, "room for one slab of scores per wavefront");
-
-int ring_slots(int bytes, int max_count) {
-  const int need = ((max_count + kSlab - 1) / kSlab + kWaves - 1) / kWaves;
-  return std::max(1, std::min(bytes / (kWaves * kSlab * 4), need));
-}
-
-template <int D>
-hipError_t launch_d(DecodeParams p, int n_items, int max_count, bool one_wave, hipStream_t s) {
-  const dim3 grid(n_items), block(64 * kWaves);
-  p.ring_slots = 0;
-  if (!p.lag) {
-    decode_partial_mxfp4<D, false><<<grid, block, 0, s>>>(p);
-    return hipGetLastError();
-  }
-  p.ring_slots = ring_slots(one_wave ? dyn_alone<D>() : dyn_shared<D>(), max_count);
-  decode_partial_mxfp4<D, true><<<grid, block, (size_t)p.ring_slots * kWaves * kSlab * 4, s>>>(p);
-  return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t prepare_decode_mxfp4() {
-  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(decode_partial_mxfp4<128, true>),
-                                     hipFuncAttributeMaxDynamicSharedMemorySize, dyn_alone<128>());
-  if (e != hipSuccess) return e;
-  e = hipFuncSetAttribute(reinterpret_cast<const void*>(decode_partial_mxfp4<64, true>),
-                          hipFuncAttributeMaxDynamicSharedMemorySize, dyn_alone<64>());
-  if (e != hipSuccess) return e;
-  e = hipFuncSetAttribute(reinterpret_cast<const void*>(score_flush_mxfp4<128>), hipFuncAttributeMaxDynamicSharedMemorySize, kFlushDyn);
-  if (e != hipSuccess) return e;
-  return hipFuncSetAttribute(reinterpret_cast<const void*>(score_flush_mxfp4<64>), hipFuncAttributeMaxDynamicSharedMemorySize, kFlushDyn);
-}
-
-hipError_t launch_decode_mxfp4(const DecodeParams& p, int D, int n_items, int max_count, bool one_wave, hipStream_t s) {
+hipError_t launch_decode_mxfp4(const DecodeParams& p, int D, int n_items, hipStream_t s) {
   if (n_items <= 0) return hipSuccess;
   if (p.G > 16) return hipErrorInvalidValue;
-  return D == 128 ? launch_d<128>(p, n_items, max_count, one_wave, s) : launch_d<64>(p, n_items, max_count, one_wave, s);
+  const dim3 grid(n_items), block(64 * kWaves);
+  if (D == 128) {
+    if (p.lag) decode_partial_mxfp4<128, true><<<grid, block, 0, s>>>(p);
+    else decode_partial_mxfp4<128, false><<<grid, block, 0, s>>>(p);
+  } else {
+    if (p.lag) decode_partial_mxfp4<64, true><<<grid, block, 0, s>>>(p);
+    else decode_partial_mxfp4<64, false><<<grid, block, 0, s>>>(p);
+  }
+  return hipGetLastError();
 }
 
-hipError_t launch_score_flush_mxfp4(const DecodeParams& p_in, int D, int n_items, int max_count, hipStream_t s) {
+hipError_t launch_score_flush_mxfp4(const DecodeParams& p, int D, int n_items, hipStream_t s) {
   if (n_items <= 0) return hipSuccess;
-  DecodeParams p = p_in;
-  p.ring_slots = ring_slots(kFlushDyn, max_count);
-  const size_t dyn = (size_t)p.ring_slots * kWaves * kSlab * 4;
-  if (D == 128) score_flush_mxfp4<128><<<dim3(n_items), dim3(64 * kWaves), dyn, s>>>(p);
-  else score_flush_mxfp4<64><<<dim3(n_items), dim3(64 * kWaves), dyn, s>>>(p);
+  if (D == 128) score_flush_mxfp4<128><<<dim3(n_items), dim3(64 * kWaves), 0, s>>>(p);
+  else score_flush_mxfp4<64><<<dim3(n_items), dim3(64 * kWaves), 0, s>>>(p);
   return hipGetLastError();
 }
 
