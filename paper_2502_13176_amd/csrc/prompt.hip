@@ -26,8 +26,6 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 4;
-constexpr int kTokPerWave = 32;
-constexpr int kTokPerWg = kWaves * kTokPerWave;
 constexpr int kKeyTile = 64;        // rows per LDS stage, two slabs of 32
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLowest = -3.402823466e38f;
@@ -36,8 +34,10 @@ constexpr float kMaxSlack = 8.f;    // a logit may exceed its token's reference 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ bf16x8_t as_bf16x8(u32x4_t x) { return __builtin_bit_cast(bf16x8_t, x); }
 
-template <int D>
-__global__ __launch_bounds__(64 * kWaves, 2) void prompt_attn_kernel(PromptParams p) {
+// N: groups of 32 tokens per wavefront.
+template <int D, int N>
+__global__ __launch_bounds__(64 * kWaves, N == 1 ? 2 : 1) void prompt_attn_kernel(PromptParams p) {
+  constexpr int kTokPerWave = 32 * N, kTokPerWg = kWaves * kTokPerWave;
   constexpr int kRow = D * 2;             // bytes of a row
   constexpr int kPieces = D / 8;          // 16-byte pieces of a row
   constexpr int kChunks = D / 16;         // head-dim steps of the first product
@@ -108,12 +108,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attn_kernel(PromptParam
   };
 
   // B operand of the first product: lane (token, h), chunk c holds Q[token][16c + 8h .. +8).
-  const int tok = qw0 + n32;
-  const int tok_row = min(tok, n_q - 1);  // tokens past the sequence repeat the last one and are never written
-  bf16x8_t qb[kChunks];
+  int tok[N];
+  bf16x8_t qb[N][kChunks];
 #pragma unroll
-  for (int c = 0; c < kChunks; ++c)
-    qb[c] = as_bf16x8(*reinterpret_cast<const u32x4_t*>(Qb + tok_row * p.q.tok + c * 32 + jh * 16));
+  for (int n = 0; n < N; ++n) {
+    tok[n] = qw0 + 32 * n + n32;
+    const int row = min(tok[n], n_q - 1);  // tokens past the sequence repeat the last one and are never written
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c)
+      qb[n][c] = as_bf16x8(*reinterpret_cast<const u32x4_t*>(Qb + row * p.q.tok + c * 32 + jh * 16));
+  }
 
   // Second product for a slab that some tokens do not see in part, value by value: a weight of zero times an infinite or NaN
   // value is left out.
@@ -141,14 +145,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attn_kernel(PromptParam
     }
   };
 
-  floatx16_t o[kBlocks];  // lane (token, h), register i of block b: O[token][32 b + 8 (i / 4) + 4 h + i % 4]
+  floatx16_t o[N][kBlocks];  // lane (token, h), register i of block b: O[token][32 b + 8 (i / 4) + 4 h + i % 4]
   // Reference maximum of the exponent, log2 units.  It starts at the lowest finite value, so that a masked logit weighs
   // 2^-inf = 0 and not 2^(-inf + inf), also where nothing has been visible yet.
-  float m_ref;
-  float l_part;           // this lane's share of the running sum
+  float m_ref[N];
+  float l_part[N];           // this lane's share of the running sum
   const float cs = p.scale_log2e;
 
-  auto logits = [&](floatx16_t (&s)[2], int kt) {
+  auto logits = [&](floatx16_t (&s)[N][2], int kt) {
     const unsigned char* base = lds_k[kt & 1] + n32 * kRow;
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
@@ -157,7 +161,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attn_kernel(PromptParam
       for (int sl = 0; sl < 2; ++sl) {
         const u32x4_t a = *reinterpret_cast<const u32x4_t*>(base + sl * 32 * kRow + slot);
         const floatx16_t zero = {};
-        s[sl] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), qb[c], c == 0 ? zero : s[sl], 0, 0, 0);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+          s[n][sl] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), qb[n][c], c == 0 ? zero : s[n][sl], 0, 0, 0);
       }
     }
   };
@@ -171,31 +177,31 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attn_kernel(PromptParam
   };
   // Lazy running maximum: a token's reference only moves when a logit exceeds it by more than kMaxSlack (log2 units), so
   // weights stay below 2^kMaxSlack and the rescale of the accumulators is rare after the first tile.
-  auto follow_max = [&](float mx) {
-    if (__any(mx > m_ref + kMaxSlack)) {
+  auto follow_max = [&](int n, float mx) {
+    if (__any(mx > m_ref[n] + kMaxSlack)) {
       mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float mn = fmaxf(m_ref, mx);
-      const float alpha = fast_exp2(m_ref - mn);
-      m_ref = mn;
-      l_part *= alpha;
+      const float mn = fmaxf(m_ref[n], mx);
+      const float alpha = fast_exp2(m_ref[n] - mn);
+      m_ref[n] = mn;
+      l_part[n] *= alpha;
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b) o[b] *= alpha;
+      for (int b = 0; b < kBlocks; ++b) o[n][b] *= alpha;
     }
   };
   // Weights of a slab of 32 keys as B operands, 16 keys each.
-  auto weights = [&](const floatx16_t& s, bf16x8_t (&pb)[2]) {
+  auto weights = [&](int n, const floatx16_t& s, bf16x8_t (&pb)[2]) {
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float w = fast_exp2(fmaf(s[8 * u + e], cs, -m_ref));
-        l_part += w;
+        const float w = fast_exp2(fmaf(s[8 * u + e], cs, -m_ref[n]));
+        l_part[n] += w;
         pb[u][e] = (__bf16)w;
       }
   };
   // Second product for a slab.  A transposed read hands lane m of a 16-lane group element m of the 16 d values the group points
   // at, for 4 consecutive keys: the group (h, d half) reads keys 4 h .. + 3 of each 8, two reads per 16 keys.
-  auto outputs = [&](int kt, int sl, const bf16x8_t (&pb)[2]) {
+  auto outputs = [&](int kt, int sl, const bf16x8_t (&pb)[N][2]) {
     const int n16 = lane & 15, half = (lane >> 4) & 1, k4 = n16 >> 2;
     const unsigned char* row = lds_v[kt & 1] + (sl * 32 + 4 * jh + k4) * kRow + half * 32 + (n16 & 3) * 8;
 #pragma unroll
@@ -207,45 +213,63 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attn_kernel(PromptParam
         const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)at);
         const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(at + 8 * kRow));
         const bf16x8_t a = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[u], o[b], 0, 0, 0);
+#pragma unroll
+        for (int n = 0; n < N; ++n) o[n][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[n][u], o[n][b], 0, 0, 0);
       }
   };
 
-  // Once; a second time, with the masked tiles value by value, where a result is not finite: an infinite or NaN value that some
-  // of a tile's tokens do not see would reach them through the product of a zero weight with it.
-  for (int careful = 0;; ++careful) {
+  auto clear = [&]() {
 #pragma unroll
-  for (int b = 0; b < kBlocks; ++b)
+    for (int n = 0; n < N; ++n) {
+      m_ref[n] = kLowest;
+      l_part[n] = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
-  m_ref = kLowest;
-  l_part = 0.f;
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[n][b][i] = 0.f;
+    }
+  };
+  auto mask = [&](floatx16_t (&s)[2], int n, int kt) {
+#pragma unroll
+    for (int sl = 0; sl < 2; ++sl)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (kt * kKeyTile + sl * 32 + 8 * (i / 4) + 4 * jh + i % 4 > before + tok[n]) s[sl][i] = kNegInf;
+  };
+
+  clear();
   if (n_key_tiles > 0) {
     stage_k(0);
     stage_v(0);
     if (n_key_tiles > 1) stage_k(1);
     publish();
-    floatx16_t s[2];
+    floatx16_t s[N][2];
+    float mx[N];
     logits(s, 0);
-    float mx = max_of(s);
+#pragma unroll
+    for (int n = 0; n < N; ++n) mx[n] = max_of(s[n]);
     __syncthreads();  // tile 0's K rows are overwritten by tile 2's in the first step
-    bf16x8_t pb[2][2];
+    bf16x8_t pb[2][N][2];
     // One pipeline step: tile kt from its logits in `s`, the next tile's logits into `sn`.
-    auto step = [&](const floatx16_t (&s)[2], floatx16_t (&sn)[2], int kt) {
+    auto step = [&](const floatx16_t (&s)[N][2], floatx16_t (&sn)[N][2], int kt) {
       if (kt + 2 < n_key_tiles) stage_k(kt + 2);
       stage_v(kt + 1);
-      follow_max(mx);
+#pragma unroll
+      for (int n = 0; n < N; ++n) follow_max(n, mx[n]);
       logits(sn, kt + 1);
-      weights(s[0], pb[0]);
-      outputs(kt, 0, pb[0]);
-      weights(s[1], pb[1]);
-      outputs(kt, 1, pb[1]);
-      mx = max_of(sn);
+#pragma unroll
+      for (int sl = 0; sl < 2; ++sl) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) weights(n, s[n][sl], pb[sl][n]);
+        outputs(kt, sl, pb[sl]);
+      }
+#pragma unroll
+      for (int n = 0; n < N; ++n) mx[n] = max_of(sn[n]);
       publish();
     };
     int kt = 0;
     for (; kt < n_full; kt += 2) {
-      floatx16_t sn[2];
+      floatx16_t sn[N][2];
       step(s, sn, kt);
       step(sn, s, kt + 1);
     }
@@ -256,16 +280,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attn_kernel(PromptParam
       if (kt + 2 < n_key_tiles) stage_k(kt + 2);
       if (kt0 <= before + qw0 + kTokPerWave - 1) {  // else wholly behind what this wavefront's tokens see
 #pragma unroll
-        for (int sl = 0; sl < 2; ++sl)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (kt0 + sl * 32 + 8 * (i / 4) + 4 * jh + i % 4 > before + tok) s[sl][i] = kNegInf;
-        follow_max(max_of(s));
+        for (int n = 0; n < N; ++n) {
+          mask(s[n], n, kt);
+          follow_max(n, max_of(s[n]));
+        }
 #pragma unroll
         for (int sl = 0; sl < 2; ++sl) {
-          weights(s[sl], pb[sl]);
-          if (careful) outputs_seen(o, kt, sl, pb[sl], before + tok);
-          else outputs(kt, sl, pb[sl]);
+#pragma unroll
+          for (int n = 0; n < N; ++n) weights(n, s[n][sl], pb[sl][n]);
+          outputs(kt, sl, pb[sl]);
         }
         if (kt + 1 < n_key_tiles) logits(s, kt + 1);
       }
@@ -274,42 +297,76 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attn_kernel(PromptParam
   }
   float sum = 0.f;  // not finite where one of them is not
 #pragma unroll
-  for (int b = 0; b < kBlocks; ++b)
+  for (int n = 0; n < N; ++n)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sum = fmaf(o[b][i], 0.f, sum);
-  if (careful || !__syncthreads_or(sum != 0.f)) break;
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum = fmaf(o[n][b][i], 0.f, sum);
+  if (__syncthreads_or(sum != 0.f)) {
+    // An infinite or NaN value that some of a tile's tokens do not see may have reached them, through the product of a zero
+    // weight with it: all again, step by step, with the tiles that are masked in part value by value.
+    clear();
+    for (int kt = 0; kt < n_key_tiles; ++kt) {
+      stage_k(kt);
+      stage_v(kt);
+      publish();
+      floatx16_t s[N][2];
+      logits(s, kt);
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        mask(s[n], n, kt);
+        follow_max(n, max_of(s[n]));
+      }
+#pragma unroll
+      for (int sl = 0; sl < 2; ++sl) {
+        bf16x8_t pb[N][2];
+#pragma unroll
+        for (int n = 0; n < N; ++n) weights(n, s[n][sl], pb[n]);
+        if ((kt + 1) * kKeyTile <= before + q0 + 1) {
+          outputs(kt, sl, pb);
+        } else {
+#pragma unroll
+          for (int n = 0; n < N; ++n) outputs_seen(o[n], kt, sl, pb[n], before + tok[n]);
+        }
+      }
+      __syncthreads();
+    }
   }
 
-  const float l_tot = l_part + __shfl_xor(l_part, 32);
-  const bool none = before + tok < 0;  // sees no key
-  const float inv = none ? 0.f : 1.f / l_tot;
-  if (tok >= n_q) return;
-  unsigned char* dst = reinterpret_cast<unsigned char*>(p.out.data) + out0 + tok * p.out.tok;
 #pragma unroll
-  for (int b = 0; b < kBlocks; ++b)
+  for (int n = 0; n < N; ++n) {
+    const float l_tot = l_part[n] + __shfl_xor(l_part[n], 32);
+    const bool none = before + tok[n] < 0;  // sees no key
+    const float inv = none ? 0.f : 1.f / l_tot;
+    if (tok[n] >= n_q) continue;
+    unsigned char* dst = reinterpret_cast<unsigned char*>(p.out.data) + out0 + tok[n] * p.out.tok;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
-      bf16x4_t r;
+    for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) r[i] = (__bf16)(o[b][4 * q + i] * inv);
-      *reinterpret_cast<bf16x4_t*>(dst + (b * 32 + q * 8 + jh * 4) * 2) = r;
-    }
-  if (p.lse.data && jh == 0)
-    *reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(p.lse.data) + lse0 + tok * p.lse.tok) =
-        none ? kNegInf : m_ref + __builtin_log2f(l_tot);
+      for (int q = 0; q < 4; ++q) {
+        typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+        bf16x4_t r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = (__bf16)(o[n][b][4 * q + i] * inv);
+        *reinterpret_cast<bf16x4_t*>(dst + (b * 32 + q * 8 + jh * 4) * 2) = r;
+      }
+    if (p.lse.data && jh == 0)
+      *reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(p.lse.data) + lse0 + tok[n] * p.lse.tok) =
+          none ? kNegInf : m_ref[n] + __builtin_log2f(l_tot);
+  }
 }
 
 }  // namespace
 
-int prompt_tile_tokens() { return kTokPerWg; }
+constexpr int kN = 1;
+int prompt_tile_tokens() { return 32 * kN * kWaves; }
 
 hipError_t launch_prompt_attn(const PromptParams& p, int D, int n_tiles, hipStream_t s) {
   const int64_t grid = (int64_t)n_tiles * p.Hq;
   if (grid <= 0) return hipSuccess;
   if (grid > INT32_MAX / (64 * kWaves)) return hipErrorInvalidValue;
-  if (D == 128) prompt_attn_kernel<128><<<dim3((unsigned)grid), dim3(64 * kWaves), 0, s>>>(p);
-  else prompt_attn_kernel<64><<<dim3((unsigned)grid), dim3(64 * kWaves), 0, s>>>(p);
+  if (D == 128) prompt_attn_kernel<128, kN><<<dim3((unsigned)grid), dim3(64 * kWaves), 0, s>>>(p);
+  else prompt_attn_kernel<64, kN><<<dim3((unsigned)grid), dim3(64 * kWaves), 0, s>>>(p);
   return hipGetLastError();
 }
 
