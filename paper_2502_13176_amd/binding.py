@@ -7,6 +7,7 @@ first call does, and fails loudly if the library has not been built.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import os
 from typing import List, Optional, Sequence
@@ -51,11 +52,6 @@ class Desc(C.Structure):
         ("off", C.c_void_p), ("cap", C.c_void_p), ("len", C.c_void_p), ("budget", C.c_void_p),
         ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("kv_scale", C.c_void_p),
     ]
-
-
-class Rows(C.Structure):
-    """baklava_rows: rows by sequence, token and head (strides in elements, seq_stride 0: packed)."""
-    _fields_ = [("data", C.c_void_p), ("seq_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
 class WorkItem(C.Structure):
@@ -119,13 +115,12 @@ def lib() -> C.CDLL:
     L.baklava_prefill_scores.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
                                          C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]
     L.baklava_kv_importance.argtypes = [f64p, C.c_int32, C.c_int32, C.c_int32, f64p]
-    rowsp = C.POINTER(Rows)
-    L.baklava_qk_norm_rope.argtypes = [rowsp, rowsp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
-                                       C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_int32, C.POINTER(C.c_uint8), f64p,
-                                       C.c_int32, C.c_int32, rowsp, rowsp, C.c_void_p]
-    L.baklava_prompt_attn.argtypes = [rowsp, rowsp, rowsp, C.c_int32, i32p, i32p, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
-                                      rowsp, rowsp, C.c_void_p]
-    L.baklava_append_prompt.argtypes = [C.c_void_p, C.c_int32, rowsp, rowsp, i32p, i32p, rowsp, C.c_void_p]
+    # (baklava_rows and the arrays of lengths travel as addresses: see _Rows and _ints)
+    vp = C.c_void_p
+    L.baklava_qk_norm_rope.argtypes = [vp, vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, vp, vp, C.c_float, vp,
+                                       C.c_int32, C.c_char_p, vp, C.c_int32, C.c_int32, vp, vp, vp]
+    L.baklava_prompt_attn.argtypes = [vp, vp, vp, C.c_int32, vp, vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp]
+    L.baklava_append_prompt.argtypes = [vp, C.c_int32, vp, vp, vp, vp, vp, vp]
     L.baklava_read_rows.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
     for name in EXPORTS:
         if name not in ("baklava_strerror", "baklava_workspace_bytes", "baklava_profile_workspace_bytes",
@@ -327,15 +322,15 @@ class Arena:
         (padded), of any strides with contiguous rows; scores [Hkv, tokens] or [batch, Hkv, T] fp32, or None (zeros)."""
         if len(lens) != self.batch or (pos0 is not None and len(pos0) != self.batch):
             raise ValueError("one length (and position) per sequence expected")
+        n, n_at, total, most = _ints(lens)
         dt = self.torch.float32 if self.dtype == "f32" else self.torch.bfloat16
-        kr, vr = (_rows(t, name, lens, self.Hkv, self.D, dt) for t, name in ((k, "k"), (v, "v")))
-        sr = _lse_rows(scores, "scores", lens, self.Hkv) if scores is not None else None
-        n = _i32(lens)
-        p0 = _i32(pos0) if pos0 is not None else None
-        _check(lib().baklava_append_prompt(self.ctx, int(layer), C.byref(kr), C.byref(vr), _p(n, C.c_int32),
-                                           _p(p0, C.c_int32) if p0 is not None else None,
-                                           C.byref(sr) if sr is not None else None, _stream_ptr(stream)),
-               "baklava_append_prompt")
+        rows = _Rows(self.torch)
+        k_at = rows.add(k, "k", self.batch, total, most, self.Hkv, self.D, dt)
+        v_at = rows.add(v, "v", self.batch, total, most, self.Hkv, self.D, dt)
+        s_at = rows.add_values(scores, "scores", self.batch, total, most, self.Hkv) if scores is not None else None
+        p0, p0_at, _, _ = _ints(pos0) if pos0 is not None else (None, None, 0, 0)
+        st = lib().baklava_append_prompt(self.ctx, layer, k_at, v_at, n_at, p0_at, s_at, _stream_ptr(stream))
+        _check(st, "baklava_append_prompt")
 
     def read_rows(self, layer_begin: int, layer_count: int, n: int, stream=None):
         """baklava_read_rows: the last n rows of every cache of the range as values, (k, v) [caches, n, D]."""
@@ -485,51 +480,82 @@ def layer_similarity_static(x_in, x_out, sim, cos=None, stream=None) -> None:
 # prompts
 # ---------------------------------------------------------------------------
 
-def _on_device(t, name: str):
+def _current_device() -> int:
     import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} must be a tensor on the current GPU")
+    try:
+        return torch._C._cuda_getDevice()
+    except AttributeError:
+        return torch.cuda.current_device()
 
 
-def _rows(t, name: str, lens, heads: int, D: int, dtype) -> Rows:
-    """Rows of D elements: [tokens, heads, D] packed, or [batch, heads, T, D]."""
-    if t.dtype != dtype:
-        raise ValueError(f"{name}: {dtype} expected")
-    if t.dim() == 3:
-        ok = t.shape[0] >= sum(lens) and t.shape[1] == heads
-        st = (0, t.stride(0), t.stride(1))
-    elif t.dim() == 4:
-        ok = t.shape[0] == len(lens) and t.shape[1] == heads and t.shape[2] >= max(lens, default=0)
-        st = (t.stride(0), t.stride(2), t.stride(1))
-        if t.shape[0] > 1 and st[0] == 0:
-            raise ValueError(f"{name}: sequences must not share their memory")
-    else:
-        ok = False
-    if not ok or t.shape[-1] != D:
-        raise ValueError(f"{name} must be [tokens, {heads}, {D}] or [batch, {heads}, T, {D}] and hold all tokens")
-    if t.stride(-1) != 1:
-        raise ValueError(f"{name}: contiguous rows expected")
-    _on_device(t, name)
-    return Rows(t.data_ptr(), *st)
+def _ints(values):
+    """int32 array of host integers: (the array, which has to outlive the call, its address, sum, maximum)."""
+    a = array.array("i", values)
+    return a, a.buffer_info()[0], sum(a), max(a, default=0)
 
 
-def _lse_rows(t, name: str, lens, heads: int) -> Rows:
-    """One fp32 value per token and head: [heads, tokens] packed, or [batch, heads, T]."""
-    import torch
-    if t.dtype != torch.float32:
-        raise ValueError(f"{name}: float32 expected")
-    if t.dim() == 2:
-        ok = t.shape[0] == heads and t.shape[1] >= sum(lens)
-        st = (0, t.stride(1), t.stride(0))
-    else:
-        ok = t.dim() == 3 and t.shape[0] == len(lens) and t.shape[1] == heads and t.shape[2] >= max(lens, default=0)
-        st = (t.stride(0), t.stride(2), t.stride(1)) if ok else (0, 0, 0)
-        if ok and t.shape[0] > 1 and st[0] == 0:
-            raise ValueError(f"{name}: sequences must not share their memory")
-    if not ok:
-        raise ValueError(f"{name} must be [{heads}, tokens] or [batch, {heads}, T] and hold all tokens")
-    _on_device(t, name)
-    return Rows(t.data_ptr(), *st)
+class _Rows:
+    """Up to five baklava_rows in one array of 64-bit words; each is handed over by its address, which add() returns.
+
+    These wrappers run once per layer and step, where a small call takes some 5 us on the GPU: hence the care for what they
+    cost on the host."""
+
+    def __init__(self, torch):
+        self.torch = torch
+        self.words = (C.c_int64 * 20)()
+        self.base = C.addressof(self.words)
+        self.n = 0
+        self.device = _current_device() if torch.cuda.is_initialized() else -1  # (no tensor is on a GPU then)
+
+    def on_device(self, t, name: str) -> None:
+        if not t.is_cuda or t.get_device() != self.device:
+            raise ValueError(f"{name} must be on the current GPU")
+
+    def _put(self, t, name, seq, tok, head) -> int:
+        self.on_device(t, name)
+        i = 4 * self.n
+        self.n += 1
+        self.words[i:i + 4] = (t.data_ptr(), seq, tok, head)
+        return self.base + 8 * i
+
+    def add(self, t, name: str, n_seq: int, total: int, most: int, heads: int, D: int, dtype) -> int:
+        """Rows of D elements: [tokens, heads, D] packed, or [batch, heads, T, D]."""
+        if t.dtype != dtype:
+            raise ValueError(f"{name}: {dtype} expected")
+        shape, stride = t.shape, t.stride()
+        if len(shape) == 3:
+            ok = shape[0] >= total and shape[1] == heads and shape[2] == D
+            seq, tok, head = 0, stride[0], stride[1]
+        elif len(shape) == 4:
+            ok = shape[0] == n_seq and shape[1] == heads and shape[2] >= most and shape[3] == D
+            seq, head, tok = stride[:3]
+            if n_seq > 1 and seq == 0:
+                raise ValueError(f"{name}: sequences must not share their memory")
+        else:
+            ok = False
+        if not ok:
+            raise ValueError(f"{name} must be [tokens, {heads}, {D}] or [batch, {heads}, T, {D}] and hold all tokens")
+        if stride[-1] != 1:
+            raise ValueError(f"{name}: contiguous rows expected")
+        return self._put(t, name, seq, tok, head)
+
+    def add_values(self, t, name: str, n_seq: int, total: int, most: int, heads: int) -> int:
+        """One fp32 value per token and head: [heads, tokens] packed, or [batch, heads, T]."""
+        if t.dtype != self.torch.float32:
+            raise ValueError(f"{name}: float32 expected")
+        shape, stride = t.shape, t.stride()
+        if len(shape) == 2:
+            ok = shape[0] == heads and shape[1] >= total
+            seq, tok, head = 0, stride[1], stride[0]
+        else:
+            ok = len(shape) == 3 and shape[0] == n_seq and shape[1] == heads and shape[2] >= most
+            if ok:
+                seq, head, tok = stride
+                if n_seq > 1 and seq == 0:
+                    raise ValueError(f"{name}: sequences must not share their memory")
+        if not ok:
+            raise ValueError(f"{name} must be [{heads}, tokens] or [batch, {heads}, T] and hold all tokens")
+        return self._put(t, name, seq, tok, head)
 
 
 def prompt_attn(q, k, v, lens: Sequence[int], kv_lens: Optional[Sequence[int]] = None, out=None, lse=None,
@@ -539,25 +565,29 @@ def prompt_attn(q, k, v, lens: Sequence[int], kv_lens: Optional[Sequence[int]] =
     Returns out (like q; places past a sequence's length are not written), and with want_lse or lse given also lse (fp32
     [Hq, tokens] or [batch, Hq, T])."""
     import torch
-    if q.dim() not in (3, 4) or k.dim() not in (3, 4) or k.shape != v.shape:
+    q_shape, k_shape = q.shape, k.shape
+    if len(q_shape) not in (3, 4) or len(k_shape) not in (3, 4) or k_shape != v.shape:
         raise ValueError("q, k, v of three or four dimensions expected, k and v alike")
-    if len(lens) == 0 or (kv_lens is not None and len(kv_lens) != len(lens)):
+    n_seq = len(lens)
+    if n_seq == 0 or (kv_lens is not None and len(kv_lens) != n_seq):
         raise ValueError("one length per sequence expected")
-    if min(lens) < 0 or (kv_lens is not None and min(kv_lens) < 0):
+    n_q, q_at, total, most = _ints(lens)
+    n_k, k_at, k_total, k_most = _ints(kv_lens) if kv_lens is not None else (n_q, None, total, most)
+    if min(n_q) < 0 or min(n_k) < 0:
         raise ValueError("lengths must not be negative")
-    Hq, Hkv, D = q.shape[1], k.shape[1], q.shape[-1]
-    keys = lens if kv_lens is None else kv_lens
-    rows = [_rows(t, name, n, h, D, torch.bfloat16) for t, name, n, h in ((q, "q", lens, Hq), (k, "k", keys, Hkv), (v, "v", keys, Hkv))]
+    Hq, Hkv, D = q_shape[1], k_shape[1], q_shape[-1]
+    dt = torch.bfloat16
+    rows = _Rows(torch)
+    at = [rows.add(q, "q", n_seq, total, most, Hq, D, dt), rows.add(k, "k", n_seq, k_total, k_most, Hkv, D, dt),
+          rows.add(v, "v", n_seq, k_total, k_most, Hkv, D, dt)]
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = q.new_empty(q_shape)
     if lse is None and want_lse:
-        lse = torch.empty((Hq, q.shape[0]) if q.dim() == 3 else q.shape[:3], dtype=torch.float32, device=q.device)
-    rows.append(_rows(out, "out", lens, Hq, D, torch.bfloat16))
-    rows.append(_lse_rows(lse, "lse", lens, Hq) if lse is not None else None)
-    n_q, n_k = _i32(lens), _i32(kv_lens) if kv_lens is not None else None
-    _check(lib().baklava_prompt_attn(*(C.byref(r) for r in rows[:3]), len(lens), _p(n_q, C.c_int32),
-                                     _p(n_k, C.c_int32) if n_k is not None else None, Hq, Hkv, D, BF16, C.byref(rows[3]),
-                                     C.byref(rows[4]) if lse is not None else None, _stream_ptr(stream)), "baklava_prompt_attn")
+        lse = q.new_empty((Hq, q_shape[0]) if len(q_shape) == 3 else q_shape[:3], dtype=torch.float32)
+    at.append(rows.add(out, "out", n_seq, total, most, Hq, D, dt))
+    at.append(rows.add_values(lse, "lse", n_seq, total, most, Hq) if lse is not None else None)
+    _check(lib().baklava_prompt_attn(at[0], at[1], at[2], n_seq, q_at, k_at, Hq, Hkv, D, BF16, at[3], at[4],
+                                     _stream_ptr(stream)), "baklava_prompt_attn")
     _hold_until_stream_passes((out, lse), stream)
     return (out, lse) if lse is not None else out
 
@@ -571,62 +601,62 @@ def qk_norm_rope(q, k, pos, inv_freq: Sequence[float], q_weight=None, k_weight=N
     The axis of every pair is given by axis_of_pair, or by sections: pairs of axis 0, of axis 1, ...  Weights [D] or None (not
     normed).  q_out, k_out may be q and k.  Returns (q_out, k_out)."""
     import torch
-    given = [t for t in (q, k) if t is not None]
-    if not given or any(t.dim() not in (3, 4) or t.dim() != given[0].dim() for t in given):
+    t0 = q if q is not None else k
+    if t0 is None or (q is not None and k is not None and q.dim() != k.dim()):
         raise ValueError("q or k of three or four dimensions expected, both alike")
-    t0 = given[0]
-    if t0.dtype not in (torch.bfloat16, torch.float32):
+    shape, dtype = t0.shape, t0.dtype
+    if len(shape) == 3:
+        n_seq, T = 1, shape[0]
+    elif len(shape) == 4:
+        n_seq, T = shape[0], shape[2]
+    else:
+        raise ValueError("q or k of three or four dimensions expected, both alike")
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
         raise ValueError("bf16 or fp32 tensors expected")
-    D, padded = t0.shape[-1], t0.dim() == 4
-    n_seq, T = (t0.shape[0], t0.shape[2]) if padded else (1, t0.shape[0])
-    for t in given:
-        if ((t.shape[0], t.shape[2]) if padded else (1, t.shape[0])) != (n_seq, T):
-            raise ValueError("q and k must hold the same tokens")
-    if n_seq * T == 0:
+    D, tokens = shape[-1], n_seq * T
+    if k is not None and ((1, k.shape[0]) if len(shape) == 3 else (k.shape[0], k.shape[2])) != (n_seq, T):
+        raise ValueError("q and k must hold the same tokens")
+    if tokens == 0:
         return tuple(None if t is None else o if o is not None else torch.empty_like(t) for t, o in ((q, q_out), (k, k_out)))
-    freq = np.ascontiguousarray(inv_freq, dtype=np.float64)
-    axes = 1
-    if freq.size:
-        if pos.dtype != torch.int32 or not pos.is_contiguous() or pos.numel() == 0 or pos.numel() % (n_seq * T):
+    rows = _Rows(torch)
+    freq = array.array("d", inv_freq)
+    n_freq, axes, pos_at = len(freq), 1, None
+    if n_freq:
+        n_pos = pos.numel()
+        if pos.dtype is not torch.int32 or not pos.is_contiguous() or n_pos == 0 or n_pos % tokens:
             raise ValueError("pos must be a contiguous int32 tensor with one value per axis and token")
-        _on_device(pos, "pos")
-        axes = pos.numel() // (n_seq * T)
+        rows.on_device(pos, "pos")
+        axes, pos_at = n_pos // tokens, pos.data_ptr()
+    axis = None
     if sections is not None:
-        if axis_of_pair is not None or sum(sections) != freq.size or len(sections) > axes or min(sections, default=0) < 0:
+        if axis_of_pair is not None or sum(sections) != n_freq or len(sections) > axes or min(sections, default=0) < 0:
             raise ValueError("sections must add up to the number of pairs, at most one for each axis")
-        axis_of_pair = [a for a, n in enumerate(sections) for _ in range(n)]
-    ax = None
-    if axis_of_pair is not None:
-        if len(axis_of_pair) != freq.size or any(not 0 <= a < axes for a in axis_of_pair):
+        axis = b"".join([bytes((a,)) * n for a, n in enumerate(sections)]) if len(sections) > 1 else None
+    elif axis_of_pair is not None:
+        if len(axis_of_pair) != n_freq or any(not 0 <= a < axes for a in axis_of_pair):
             raise ValueError("axis_of_pair must name an axis for every pair")
-        ax = np.ascontiguousarray(axis_of_pair, dtype=np.uint8)
-    lens = [T] * n_seq
-    ptr, outs, heads = [], [], []
-    for t, name, w, o in ((q, "q", q_weight, q_out), (k, "k", k_weight, k_out)):
+        axis = bytes(axis_of_pair)
+    in_at, out_at, w_at, outs, heads = [None, None], [None, None], [None, None], [None, None], [0, 0]
+    for i, (t, name, w, o) in enumerate(((q, "q", q_weight, q_out), (k, "k", k_weight, k_out))):
         if t is None:
             if w is not None or o is not None:
                 raise ValueError(f"no {name} given")
-            ptr.append((None, None, None))
-            outs.append(None)
-            heads.append(0)
             continue
+        h = heads[i] = t.shape[1]
+        in_at[i] = rows.add(t, name, n_seq, tokens, T, h, D, dtype)
         if w is not None:
-            if w.dtype != t.dtype or w.shape != (D,) or not w.is_contiguous():
+            if w.dtype is not dtype or w.shape != (D,) or not w.is_contiguous():
                 raise ValueError(f"{name}_weight must be a contiguous [{D}] tensor of the rows' type")
-            _on_device(w, f"{name}_weight")
-        r = _rows(t, name, lens, t.shape[1], D, t0.dtype)
+            rows.on_device(w, f"{name}_weight")
+            w_at[i] = w.data_ptr()
         if o is None:
-            o = torch.empty(t.shape, dtype=t.dtype, device=t.device)
+            o = t.new_empty(t.shape)
         elif o.shape != t.shape:
             raise ValueError(f"{name}_out must have the shape of {name}")
-        ptr.append((C.byref(r), w.data_ptr() if w is not None else None, C.byref(_rows(o, f"{name}_out", lens, t.shape[1], D, t0.dtype))))
-        outs.append(o)
-        heads.append(t.shape[1])
-    _check(lib().baklava_qk_norm_rope(ptr[0][0], ptr[1][0], n_seq, T, heads[0], heads[1], D,
-                                      BF16 if t0.dtype == torch.bfloat16 else F32, ptr[0][1], ptr[1][1], float(eps),
-                                      pos.data_ptr() if freq.size else None, axes,
-                                      _p(ax, C.c_uint8) if ax is not None else None, _p(freq, C.c_double), 2 * freq.size,
-                                      int(bool(interleaved)), ptr[0][2], ptr[1][2], _stream_ptr(stream)),
-           "baklava_qk_norm_rope")
+        out_at[i], outs[i] = rows.add(o, f"{name}_out", n_seq, tokens, T, h, D, dtype), o
+    _check(lib().baklava_qk_norm_rope(in_at[0], in_at[1], n_seq, T, heads[0], heads[1], D,
+                                      BF16 if dtype is torch.bfloat16 else F32, w_at[0], w_at[1], eps, pos_at, axes, axis,
+                                      freq.buffer_info()[0], 2 * n_freq, 1 if interleaved else 0, out_at[0], out_at[1],
+                                      _stream_ptr(stream)), "baklava_qk_norm_rope")
     _hold_until_stream_passes(outs, stream)
     return outs[0], outs[1]

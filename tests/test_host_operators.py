@@ -9,24 +9,28 @@ from paper_2502_13176_amd import binding as B
 OKP = 0x10000                                             # never dereferenced: the calls fail on their arguments
 
 
+class Rows(C.Structure):                                  # baklava_rows
+    _fields_ = [("data", C.c_void_p), ("seq_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
 def rows(data=OKP, seq=0, tok=1024, head=128):
-    return B.Rows(data, seq, tok, head)
+    return Rows(data, seq, tok, head)
 
 
 def ref(r):
-    return C.byref(r) if r is not None else None
+    return C.addressof(r) if r is not None else None
 
 
 def i32(*x):
-    return np.asarray(x, dtype=np.int32).ctypes.data_as(C.POINTER(C.c_int32))
+    return (C.c_int32 * max(1, len(x)))(*x)
 
 
 def rope(q=rows(), k=rows(), n_seq=1, T=4, Hq=4, Hkv=2, D=128, dtype=B.BF16, wq=OKP, wk=OKP, eps=1e-6, pos=OKP, axes=1, axis=None,
          freq=(1.0,) * 64, rot=128, qo=rows(), ko=rows()):
-    f = np.asarray(freq, dtype=np.float64)
-    a = np.asarray(axis, dtype=np.uint8).ctypes.data_as(C.POINTER(C.c_uint8)) if axis is not None else None
+    f = (C.c_double * 64)(*freq) if freq is not None else None
+    a = bytes(axis) if axis is not None else None
     return B.lib().baklava_qk_norm_rope(ref(q), ref(k), n_seq, T, Hq, Hkv, D, dtype, wq, wk, eps, pos, axes, a,
-                                        f.ctypes.data_as(C.POINTER(C.c_double)) if freq is not None else None, rot, 0, ref(qo),
+                                        f, rot, 0, ref(qo),
                                         ref(ko), None)
 
 
@@ -50,7 +54,7 @@ def test_rope_refuses(kw):
     assert rope(**kw) == B.EINVAL
 
 
-def attn(q=rows(), k=rows(), v=rows(), q_len=(4, 0, 7), kv_len=None, Hq=4, Hkv=2, D=128, dtype=B.BF16, out=rows(), lse=B.Rows(OKP, 0, 1, 11)):
+def attn(q=rows(), k=rows(), v=rows(), q_len=(4, 0, 7), kv_len=None, Hq=4, Hkv=2, D=128, dtype=B.BF16, out=rows(), lse=Rows(OKP, 0, 1, 11)):
     n = len(q_len) if q_len is not None else 3
     return B.lib().baklava_prompt_attn(ref(q), ref(k), ref(v), n, i32(*q_len) if q_len is not None else None,
                                        i32(*kv_len) if kv_len is not None else None, Hq, Hkv, D, dtype, ref(out), ref(lse), None)
@@ -64,8 +68,8 @@ def test_prompt_attn_refuses_rows(arg, bad):
 
 @pytest.mark.parametrize("kw", [dict(q_len=None), dict(q_len=()), dict(q_len=(-1,)), dict(kv_len=(4, 0, -7)), dict(q_len=((1 << 29) + 1,)),
                                 dict(q_len=(1 << 29,) * 4), dict(kv_len=(1 << 29, 1 << 29, (1 << 29) + 1)), dict(Hq=0), dict(Hkv=0), dict(Hq=3), dict(D=96), dict(dtype=B.F32),
-                                dict(dtype=B.MXFP4), dict(lse=B.Rows(None, 0, 1, 11)), dict(lse=B.Rows(OKP + 2, 0, 1, 11)),
-                                dict(lse=B.Rows(OKP, 0, 0, 11)), dict(lse=B.Rows(OKP, 0, 1, 0)), dict(lse=B.Rows(OKP, 0, 1, -11)),
+                                dict(dtype=B.MXFP4), dict(lse=Rows(None, 0, 1, 11)), dict(lse=Rows(OKP + 2, 0, 1, 11)),
+                                dict(lse=Rows(OKP, 0, 0, 11)), dict(lse=Rows(OKP, 0, 1, 0)), dict(lse=Rows(OKP, 0, 1, -11)),
                                 dict(out=rows(tok=120)), dict(out=rows(head=0))])
 def test_prompt_attn_refuses(kw):
     assert attn(**kw) == B.EINVAL
