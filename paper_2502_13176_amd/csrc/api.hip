@@ -1094,10 +1094,10 @@ extern "C" int baklava_append_prompt(baklava_ctx* ctx, int32_t layer, const bakl
     for (int32_t h0 = 0; h0 < Hkv; h0 += heads) {
       const int32_t nh = std::min(heads, Hkv - h0);
       p.cache0 = (int32_t)(c0 + (int64_t)b0 * Hkv);
-      p.head0 = h0; p.seq0 = b0;
+      p.head0 = h0; p.n_heads = nh; p.seq0 = b0;
       for (int32_t i = 0; i < nb; ++i)
         for (int32_t h = 0; h < nh; ++h) p.start[i * nh + h] = ctx->len[c0 + (int64_t)(b0 + i) * Hkv + h0 + h];
-      if (!hip_ok(launch_append_prompt(p, query_row_bytes(&ctx->d) / 16, ctx->d.dtype == BAKLAVA_MXFP4, nh, nb, longest,
+      if (!hip_ok(launch_append_prompt(p, query_row_bytes(&ctx->d) / 16, ctx->d.dtype == BAKLAVA_MXFP4, nb, longest,
                                        (hipStream_t)stream)))
         return BAKLAVA_EHIP;
     }

@@ -207,7 +207,7 @@ struct PromptRowsParams {
   const int64_t* off;
   int32_t* len;
   int32_t cache0, Hkv;      // cache of sequence 0 of the launch, head 0
-  int32_t head0, seq0;
+  int32_t head0, n_heads, seq0, tile0;  // heads, first sequence and first tile of the launch
   struct Seq {
     int32_t n, first, pos0;
   } seq[kPromptSeqs];
@@ -298,7 +298,7 @@ hipError_t launch_qk_norm_rope(const RopeParams& p, int dtype, int D, bool inter
 hipError_t launch_prompt_attn(const PromptParams& p, int D, int n_tiles, hipStream_t s);
 int prompt_tile_tokens();  // query tokens per workgroup
 // pieces: 16-byte pieces of a row as the caller holds it; most: tokens of the longest sequence
-hipError_t launch_append_prompt(const PromptRowsParams& p, int pieces, bool mx, int n_heads, int n_seq, int most, hipStream_t s);
+hipError_t launch_append_prompt(const PromptRowsParams& p, int pieces, bool mx, int n_seq, int most, hipStream_t s);
 hipError_t launch_read_rows(const ReadRowsParams& p, int pieces, bool mx, int n_caches, hipStream_t s);
 hipError_t launch_set_lengths(const LengthsParams& p, hipStream_t s);
 hipError_t launch_fill_i32(int32_t* dst, int32_t value, int64_t n, hipStream_t s);

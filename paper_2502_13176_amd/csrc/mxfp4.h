@@ -66,7 +66,25 @@ __device__ __forceinline__ void mx_store(uint4 x, int piece, void* plane, uint8_
   if (piece % 4 == 0) kv_scale[row * (D / 16) + value * (D / 32) + piece / 4] = (uint8_t)byte;
 }
 
-// The same row back.
+// The scales of a row's key and value from those of its 32 elements each lane shares (the bytes of a quad are equal): words of
+// D / 32 bytes, in every lane of the row.
+template <int D>
+__device__ __forceinline__ uint2 mx_row_scales(uint32_t byte_k, uint32_t byte_v, int piece) {
+  const int shift = 8 * (piece / 4);
+  int k = (int)(byte_k << shift), v = (int)(byte_v << shift);
+  if (D == 128) {  // four quads of a row of 16 lanes
+    k |= __builtin_amdgcn_update_dpp(0, k, 0x124, 0xf, 0xf, true);  // row_ror:4
+    v |= __builtin_amdgcn_update_dpp(0, v, 0x124, 0xf, 0xf, true);
+    k |= __builtin_amdgcn_update_dpp(0, k, 0x128, 0xf, 0xf, true);  // row_ror:8
+    v |= __builtin_amdgcn_update_dpp(0, v, 0x128, 0xf, 0xf, true);
+  } else {  // two of eight
+    k |= __builtin_amdgcn_update_dpp(0, k, 0x141, 0xf, 0xf, true);  // row_half_mirror
+    v |= __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, true);
+  }
+  return make_uint2((uint32_t)k, (uint32_t)v);
+}
+
+// A row mx_store has written, back.
 template <int D>
 __device__ __forceinline__ uint4 mx_load(int piece, const void* plane, const uint8_t* kv_scale, int64_t row, int value) {
   return mx_values(reinterpret_cast<const uint32_t*>(plane)[row * (D / 8) + piece],

@@ -1,5 +1,9 @@
-// Prompts into the caches and cache rows back out (baklava_append_prompt, baklava_read_rows).  Both move rows and are bound by
-// HBM; a workgroup takes kTile rows of one cache, whole rows at a time.
+// Prompts into the caches and cache rows back out (baklava_append_prompt, baklava_read_rows).
+//
+// Both move rows, so HBM bounds them: a workgroup takes kTile rows of one cache, requests all of them, whole rows at a time, and
+// stores them (rounded to 4 bits on the way, see mxfp4.h).  Read and written together, behind a projection's output that the
+// last-level cache may hold in part: 8 x 32768 bf16 rows of 128 elements into 4 bits 23 us, 7.4 TB/s, of 16 bits 36 us, 7.5;
+// back out of 4 bits 25 us, 6.7 TB/s.  (A loop that requested rows four at a time, tiles in front of heads, took 35 us.)
 #include "common.h"
 #include "mxfp4.h"
 
@@ -9,36 +13,53 @@ namespace {
 
 constexpr int kThreads = 256, kTile = 64;
 
-// MX: 4-bit rows.  PIECES: 16-byte pieces of a row as the caller holds it.
+// MX: 4-bit rows.  PIECES: 16-byte pieces of a row as the caller holds it.  Workgroups go over the heads of a tile of tokens
+// first: a token's heads lie next to each other in what a projection writes.
 template <int PIECES, bool MX>
 __global__ __launch_bounds__(kThreads) void append_prompt_kernel(PromptRowsParams p) {
-  constexpr int kRows = kThreads / PIECES, D = PIECES * 8;  // (D: bf16 rows, where it matters)
-  const int i = blockIdx.z, h = p.head0 + blockIdx.y;
+  constexpr int kRows = kThreads / PIECES, kPer = kTile / kRows, D = PIECES * 8;  // (D: bf16 rows, where it matters)
+  const int i = blockIdx.y, h_rel = (uint32_t)blockIdx.x % (uint32_t)p.n_heads, h = p.head0 + h_rel;
   const PromptRowsParams::Seq q = p.seq[i];
-  const int r0 = blockIdx.x * kTile;
+  const int r0 = (p.tile0 + (uint32_t)blockIdx.x / (uint32_t)p.n_heads) * kTile;
   if (r0 >= q.n) return;
-  const int c = p.cache0 + i * p.Hkv + h, start = p.start[i * gridDim.y + blockIdx.y];
-  const int64_t row0 = p.off[c] + start;
-  const int tid = threadIdx.x, piece = tid % PIECES;
+  const int c = p.cache0 + i * p.Hkv + h, start = p.start[i * p.n_heads + h_rel];
+  const int tid = threadIdx.x, piece = tid % PIECES, row = r0 + tid / PIECES;
   const int e = min(r0 + kTile, q.n);
   const uint4* src_k = reinterpret_cast<const uint4*>(p.k.data) + p.k.begin(p.seq0 + i, q.first) + h * p.k.head + piece;
   const uint4* src_v = reinterpret_cast<const uint4*>(p.v.data) + p.v.begin(p.seq0 + i, q.first) + h * p.v.head + piece;
-#pragma unroll 4
-  for (int r = r0 + tid / PIECES; r < e; r += kRows) {
-    const uint4 k = src_k[r * p.k.tok], v = src_v[r * p.v.tok];
+  uint4 k[kPer], v[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {  // rows past the last one repeat it and are not written
+    const int64_t r = min(row + j * kRows, e - 1);
+    k[j] = src_k[r * p.k.tok];
+    v[j] = src_v[r * p.v.tok];
+  }
+  const int64_t row0 = p.off[c] + start;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int r = row + j * kRows;
     if (MX) {
-      mx_store<D>(k, piece, p.k_plane, p.kv_scale, row0 + r, 0);
-      mx_store<D>(v, piece, p.v_plane, p.kv_scale, row0 + r, 1);
-    } else {
-      reinterpret_cast<uint4*>(p.k_plane)[(row0 + r) * PIECES + piece] = k;
-      reinterpret_cast<uint4*>(p.v_plane)[(row0 + r) * PIECES + piece] = v;
+      const uint32_t bk = mx_scale_byte(mx_top(k[j])), bv = mx_scale_byte(mx_top(v[j]));
+      const uint32_t ck = mx_codes(k[j], bk), cv = mx_codes(v[j], bv);
+      const uint2 scales = mx_row_scales<D>(bk, bv, piece);
+      if (r < e) {
+        reinterpret_cast<uint32_t*>(p.k_plane)[(row0 + r) * (D / 8) + piece] = ck;
+        reinterpret_cast<uint32_t*>(p.v_plane)[(row0 + r) * (D / 8) + piece] = cv;
+        if (piece == 0) {
+          if (D == 128) reinterpret_cast<uint2*>(p.kv_scale)[row0 + r] = scales;
+          else reinterpret_cast<uint32_t*>(p.kv_scale)[row0 + r] = scales.x | scales.y << 16;
+        }
+      }
+    } else if (r < e) {
+      store_nt16(reinterpret_cast<uint4*>(p.k_plane) + (row0 + r) * PIECES + piece, k[j]);
+      store_nt16(reinterpret_cast<uint4*>(p.v_plane) + (row0 + r) * PIECES + piece, v[j]);
     }
   }
   if (tid < e - r0) {
     const int r = r0 + tid;
-    p.score[row0 + r] = 0.f;
-    if (p.scores.data)
-      p.score[row0 + r] = reinterpret_cast<const float*>(p.scores.data)[p.scores.begin(p.seq0 + i, q.first) + r * p.scores.tok + h * p.scores.head];
+    p.score[row0 + r] = p.scores.data ? reinterpret_cast<const float*>(p.scores.data)[p.scores.begin(p.seq0 + i, q.first) +
+                                                                                      r * p.scores.tok + h * p.scores.head]
+                                      : 0.f;
     p.pos[row0 + r] = q.pos0 + r;
   }
   if (r0 == 0 && tid == 0) p.len[c] = start + q.n;
@@ -46,27 +67,34 @@ __global__ __launch_bounds__(kThreads) void append_prompt_kernel(PromptRowsParam
 
 template <int PIECES, bool MX>
 __global__ __launch_bounds__(kThreads) void read_rows_kernel(ReadRowsParams p) {
-  constexpr int kRows = kThreads / PIECES, D = PIECES * 8;
+  constexpr int kRows = kThreads / PIECES, kPer = kTile / kRows, D = PIECES * 8;
   const int c = p.cache0 + blockIdx.y;
   const int r0 = blockIdx.x * kTile, e = min(r0 + kTile, p.n);
   const int skip = p.n - p.len[c];  // places in front of the cache's first row (or rows in front of the first one asked for)
-  const int64_t row0 = p.off[c] - skip;
-  const int tid = threadIdx.x, piece = tid % PIECES;
-#pragma unroll 4
-  for (int r = r0 + tid / PIECES; r < e; r += kRows) {
-    uint4 k = make_uint4(0, 0, 0, 0), v = k;
+  const int64_t row0 = p.off[c] - skip, out0 = (int64_t)blockIdx.y * p.n;
+  const int tid = threadIdx.x, piece = tid % PIECES, row = r0 + tid / PIECES;
+  uint4 k[kPer], v[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int r = min(row + j * kRows, e - 1);
+    k[j] = v[j] = make_uint4(0, 0, 0, 0);
     if (r >= skip) {
       if (MX) {
-        k = mx_load<D>(piece, p.k_plane, p.kv_scale, row0 + r, 0);
-        v = mx_load<D>(piece, p.v_plane, p.kv_scale, row0 + r, 1);
+        k[j] = mx_load<D>(piece, p.k_plane, p.kv_scale, row0 + r, 0);
+        v[j] = mx_load<D>(piece, p.v_plane, p.kv_scale, row0 + r, 1);
       } else {
-        k = reinterpret_cast<const uint4*>(p.k_plane)[(row0 + r) * PIECES + piece];
-        v = reinterpret_cast<const uint4*>(p.v_plane)[(row0 + r) * PIECES + piece];
+        k[j] = reinterpret_cast<const uint4*>(p.k_plane)[(row0 + r) * PIECES + piece];
+        v[j] = reinterpret_cast<const uint4*>(p.v_plane)[(row0 + r) * PIECES + piece];
       }
     }
-    const int64_t at = ((int64_t)blockIdx.y * p.n + r) * PIECES + piece;
-    reinterpret_cast<uint4*>(p.k_out)[at] = k;
-    reinterpret_cast<uint4*>(p.v_out)[at] = v;
+  }
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int r = row + j * kRows;
+    if (r < e) {
+      store_nt16(reinterpret_cast<uint4*>(p.k_out) + (out0 + r) * PIECES + piece, k[j]);
+      store_nt16(reinterpret_cast<uint4*>(p.v_out) + (out0 + r) * PIECES + piece, v[j]);
+    }
   }
 }
 
@@ -91,15 +119,19 @@ __global__ __launch_bounds__(64) void append_mx_kernel(AppendParams p) {
 
 }  // namespace
 
-hipError_t launch_append_prompt(const PromptRowsParams& p, int pieces, bool mx, int n_heads, int n_seq, int most, hipStream_t s) {
-  if (n_heads <= 0 || n_seq <= 0 || most <= 0) return hipSuccess;
-  const dim3 grid((most + kTile - 1) / kTile, n_heads, n_seq), block(kThreads);
-  if (mx && pieces == 16) append_prompt_kernel<16, true><<<grid, block, 0, s>>>(p);
-  else if (mx && pieces == 8) append_prompt_kernel<8, true><<<grid, block, 0, s>>>(p);
-  else if (pieces == 32) append_prompt_kernel<32, false><<<grid, block, 0, s>>>(p);
-  else if (pieces == 16) append_prompt_kernel<16, false><<<grid, block, 0, s>>>(p);
-  else if (pieces == 8) append_prompt_kernel<8, false><<<grid, block, 0, s>>>(p);
-  else return hipErrorInvalidValue;
+hipError_t launch_append_prompt(const PromptRowsParams& p_in, int pieces, bool mx, int n_seq, int most, hipStream_t s) {
+  if (p_in.n_heads <= 0 || n_seq <= 0 || most <= 0) return hipSuccess;
+  PromptRowsParams p = p_in;
+  const int tiles = (most + kTile - 1) / kTile, per_launch = (1 << 23) / p.n_heads;  // a grid dimension holds fewer than 2^32 threads
+  for (p.tile0 = 0; p.tile0 < tiles; p.tile0 += per_launch) {
+    const dim3 grid((tiles - p.tile0 < per_launch ? tiles - p.tile0 : per_launch) * p.n_heads, n_seq), block(kThreads);
+    if (mx && pieces == 16) append_prompt_kernel<16, true><<<grid, block, 0, s>>>(p);
+    else if (mx && pieces == 8) append_prompt_kernel<8, true><<<grid, block, 0, s>>>(p);
+    else if (pieces == 32) append_prompt_kernel<32, false><<<grid, block, 0, s>>>(p);
+    else if (pieces == 16) append_prompt_kernel<16, false><<<grid, block, 0, s>>>(p);
+    else if (pieces == 8) append_prompt_kernel<8, false><<<grid, block, 0, s>>>(p);
+    else return hipErrorInvalidValue;
+  }
   return hipGetLastError();
 }
 
