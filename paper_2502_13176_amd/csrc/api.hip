@@ -1004,12 +1004,11 @@ extern "C" int baklava_prompt_attn(const baklava_rows* q, const baklava_rows* k,
   const int32_t* const k_len = kv_len ? kv_len : q_len;
   int64_t n_q = 0, n_k = 0, tiles = 0;
   int32_t most_q = 0, most_k = 0;
-  const int tile = prompt_tile_tokens();
   for (int32_t b = 0; b < n_seq; ++b) {
     if (q_len[b] < 0 || k_len[b] < 0 || q_len[b] > kMostPromptTokens || k_len[b] > kMostPromptTokens) return BAKLAVA_EINVAL;
     n_q += q_len[b];
     n_k += k_len[b];
-    tiles += (q_len[b] + tile - 1) / tile;
+    tiles += (q_len[b] + 127) / 128;
     most_q = std::max(most_q, q_len[b]);
     most_k = std::max(most_k, k_len[b]);
   }
@@ -1029,6 +1028,10 @@ extern "C" int baklava_prompt_attn(const baklava_rows* q, const baklava_rows* k,
       k_first += k_len[b];
     }
     std::stable_sort(seq.begin(), seq.end(), [](const PromptParams::Seq& a, const PromptParams::Seq& b) { return a.k_len > b.k_len; });
+    int dev = 0, n_cus = 0;
+    if (!hip_ok(hipGetDevice(&dev)) || !hip_ok(hipDeviceGetAttribute(&n_cus, hipDeviceAttributeMultiprocessorCount, dev)))
+      return BAKLAVA_EHIP;
+    const int tile = prompt_tile_tokens(tiles * Hq, n_cus);
     PromptParams p{};
     p.q = device_rows(q, 2, 1); p.out = device_rows(out, 2, 1);
     p.k = n_k > 0 ? device_rows(k, 2, 1) : Rows{};
@@ -1044,7 +1047,7 @@ extern "C" int baklava_prompt_attn(const baklava_rows* q, const baklava_rows* k,
         end += (p.seq[i].q_len + tile - 1) / tile;
         p.seq[i].tile_end = end;
       }
-      if (!hip_ok(launch_prompt_attn(p, D, end, (hipStream_t)stream))) return BAKLAVA_EHIP;
+      if (!hip_ok(launch_prompt_attn(p, D, tile, end, n_cus, (hipStream_t)stream))) return BAKLAVA_EHIP;
     }
   } catch (const std::bad_alloc&) {
     return BAKLAVA_ENOMEM;

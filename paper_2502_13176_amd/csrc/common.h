@@ -187,6 +187,7 @@ constexpr int kPromptSeqs = 128;  // sequences per launch: their records travel 
 struct PromptParams {
   Rows q, k, v, out, lse;   // strides in bytes
   int32_t Hq, Hkv, n_seq;
+  int32_t reversed_from;    // workgroups from this one on take their tiles in the opposite order
   float scale_log2e;
   struct Seq {
     int32_t b, q_first, k_first;  // sequence, tokens and keys in front of it (packed rows)
@@ -295,8 +296,9 @@ hipError_t launch_score_pass(const ScoreParams& p, int n_items, int max_count, h
 hipError_t launch_append(const AppendParams& p, int n_caches, hipStream_t s);
 hipError_t launch_append_mx(const AppendParams& p, int D, int n_caches, hipStream_t s);  // 4-bit rows
 hipError_t launch_qk_norm_rope(const RopeParams& p, int dtype, int D, bool interleaved, hipStream_t s);
-hipError_t launch_prompt_attn(const PromptParams& p, int D, int n_tiles, hipStream_t s);
-int prompt_tile_tokens();  // query tokens per workgroup
+// query tokens per workgroup of a call that would have so many workgroups of 128
+int prompt_tile_tokens(int64_t n_tiles128, int n_cus);
+hipError_t launch_prompt_attn(const PromptParams& p, int D, int tile_tokens, int n_tiles, int n_cus, hipStream_t s);
 // pieces: 16-byte pieces of a row as the caller holds it; most: tokens of the longest sequence
 hipError_t launch_append_prompt(const PromptRowsParams& p, int pieces, bool mx, int n_seq, int most, hipStream_t s);
 hipError_t launch_read_rows(const ReadRowsParams& p, int pieces, bool mx, int n_caches, hipStream_t s);

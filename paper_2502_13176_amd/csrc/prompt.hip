@@ -34,10 +34,11 @@ constexpr float kMaxSlack = 8.f;    // a logit may exceed its token's reference 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ bf16x8_t as_bf16x8(u32x4_t x) { return __builtin_bit_cast(bf16x8_t, x); }
 
-// N: groups of 32 tokens per wavefront.
-template <int D, int N>
-__global__ __launch_bounds__(64 * kWaves, N == 1 ? 2 : 1) void prompt_attn_kernel(PromptParams p) {
-  constexpr int kTokPerWave = 32 * N, kTokPerWg = kWaves * kTokPerWave;
+// KS: wavefronts that share 32 tokens.  1: each takes both slabs of a tile of keys; 2: each takes one of them, and the two add up
+// what they have at the end.
+template <int D, int KS>
+__global__ __launch_bounds__(64 * kWaves, 2) void prompt_attn_kernel(PromptParams p) {
+  constexpr int kTokPerWg = 32 * kWaves / KS, kSlabs = 2 / KS;
   constexpr int kRow = D * 2;             // bytes of a row
   constexpr int kPieces = D / 8;          // 16-byte pieces of a row
   constexpr int kChunks = D / 16;         // head-dim steps of the first product
@@ -53,7 +54,9 @@ __global__ __launch_bounds__(64 * kWaves, N == 1 ? 2 : 1) void prompt_attn_kerne
   // Query heads that share a KV head meet on the same XCDs (consecutive workgroups go round them) while the number of KV
   // heads allows it.
   const int G = p.Hq / p.Hkv;
-  const int kv_head = blockIdx.x % p.Hkv, rest = blockIdx.x / p.Hkv;
+  int idx = blockIdx.x;
+  if (idx >= p.reversed_from) idx = p.reversed_from + (int)gridDim.x - 1 - idx;
+  const int kv_head = idx % p.Hkv, rest = idx / p.Hkv;
   const int head = kv_head * G + rest % G, rank = rest / G;
   int at = 0;  // the sequence of this tile: as many end in front of it
   for (int i0 = 0; i0 < p.n_seq; i0 += 64)
@@ -70,7 +73,8 @@ __global__ __launch_bounds__(64 * kWaves, N == 1 ? 2 : 1) void prompt_attn_kerne
   const int64_t lse0 = p.lse.begin(sq.b, sq.q_first) + head * p.lse.head;
 
   const int q0 = tile * kTokPerWg;          // first token of the workgroup
-  const int qw0 = q0 + wave * kTokPerWave;  // first token of this wavefront
+  const int qw0 = q0 + wave / KS * 32;      // first token of this wavefront
+  const int sl0 = KS == 1 ? 0 : wave & 1;   // its first slab of a tile
   const int before = n_k - n_q;             // keys in front of the first token's own (less than 0: tokens that see none)
   const int last_key = before + min(q0 + kTokPerWg, n_q) - 1;
   const int n_key_tiles = last_key < 0 ? 0 : last_key / kKeyTile + 1;
@@ -108,16 +112,12 @@ __global__ __launch_bounds__(64 * kWaves, N == 1 ? 2 : 1) void prompt_attn_kerne
   };
 
   // B operand of the first product: lane (token, h), chunk c holds Q[token][16c + 8h .. +8).
-  int tok[N];
-  bf16x8_t qb[N][kChunks];
+  const int tok = qw0 + n32;
+  const int tok_row = min(tok, n_q - 1);  // tokens past the sequence repeat the last one and are never written
+  bf16x8_t qb[kChunks];
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    tok[n] = qw0 + 32 * n + n32;
-    const int row = min(tok[n], n_q - 1);  // tokens past the sequence repeat the last one and are never written
-#pragma unroll
-    for (int c = 0; c < kChunks; ++c)
-      qb[n][c] = as_bf16x8(*reinterpret_cast<const u32x4_t*>(Qb + row * p.q.tok + c * 32 + jh * 16));
-  }
+  for (int c = 0; c < kChunks; ++c)
+    qb[c] = as_bf16x8(*reinterpret_cast<const u32x4_t*>(Qb + tok_row * p.q.tok + c * 32 + jh * 16));
 
   // Second product for a slab that some tokens do not see in part, value by value: a weight of zero times an infinite or NaN
   // value is left out.
@@ -145,65 +145,63 @@ __global__ __launch_bounds__(64 * kWaves, N == 1 ? 2 : 1) void prompt_attn_kerne
     }
   };
 
-  floatx16_t o[N][kBlocks];  // lane (token, h), register i of block b: O[token][32 b + 8 (i / 4) + 4 h + i % 4]
+  floatx16_t o[kBlocks];  // lane (token, h), register i of block b: O[token][32 b + 8 (i / 4) + 4 h + i % 4]
   // Reference maximum of the exponent, log2 units.  It starts at the lowest finite value, so that a masked logit weighs
   // 2^-inf = 0 and not 2^(-inf + inf), also where nothing has been visible yet.
-  float m_ref[N];
-  float l_part[N];           // this lane's share of the running sum
+  float m_ref;
+  float l_part;           // this lane's share of the running sum
   const float cs = p.scale_log2e;
 
-  auto logits = [&](floatx16_t (&s)[N][2], int kt) {
-    const unsigned char* base = lds_k[kt & 1] + n32 * kRow;
+  auto logits = [&](floatx16_t (&s)[kSlabs], int kt) {
+    const unsigned char* base = lds_k[kt & 1] + (sl0 * 32 + n32) * kRow;
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
       const int piece = 2 * c + jh, slot = (D == 128 ? piece ^ (n32 & 15) : piece ^ (n32 >> 1 & 7)) * 16;
 #pragma unroll
-      for (int sl = 0; sl < 2; ++sl) {
+      for (int sl = 0; sl < kSlabs; ++sl) {
         const u32x4_t a = *reinterpret_cast<const u32x4_t*>(base + sl * 32 * kRow + slot);
         const floatx16_t zero = {};
-#pragma unroll
-        for (int n = 0; n < N; ++n)
-          s[n][sl] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), qb[n][c], c == 0 ? zero : s[n][sl], 0, 0, 0);
+        s[sl] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), qb[c], c == 0 ? zero : s[sl], 0, 0, 0);
       }
     }
   };
-  auto max_of = [&](const floatx16_t (&s)[2]) {
+  auto max_of = [&](const floatx16_t (&s)[kSlabs]) {
     float mx = s[0][0];
 #pragma unroll
-    for (int sl = 0; sl < 2; ++sl)
+    for (int sl = 0; sl < kSlabs; ++sl)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[sl][i]);
     return mx * cs;
   };
   // Lazy running maximum: a token's reference only moves when a logit exceeds it by more than kMaxSlack (log2 units), so
   // weights stay below 2^kMaxSlack and the rescale of the accumulators is rare after the first tile.
-  auto follow_max = [&](int n, float mx) {
-    if (__any(mx > m_ref[n] + kMaxSlack)) {
+  auto follow_max = [&](float mx) {
+    if (__any(mx > m_ref + kMaxSlack)) {
       mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float mn = fmaxf(m_ref[n], mx);
-      const float alpha = fast_exp2(m_ref[n] - mn);
-      m_ref[n] = mn;
-      l_part[n] *= alpha;
+      const float mn = fmaxf(m_ref, mx);
+      const float alpha = fast_exp2(m_ref - mn);
+      m_ref = mn;
+      l_part *= alpha;
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b) o[n][b] *= alpha;
+      for (int b = 0; b < kBlocks; ++b) o[b] *= alpha;
     }
   };
   // Weights of a slab of 32 keys as B operands, 16 keys each.
-  auto weights = [&](int n, const floatx16_t& s, bf16x8_t (&pb)[2]) {
+  auto weights = [&](const floatx16_t& s, bf16x8_t (&pb)[2]) {
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float w = fast_exp2(fmaf(s[8 * u + e], cs, -m_ref[n]));
-        l_part[n] += w;
+        const float w = fast_exp2(fmaf(s[8 * u + e], cs, -m_ref));
+        l_part += w;
         pb[u][e] = (__bf16)w;
       }
   };
   // Second product for a slab.  A transposed read hands lane m of a 16-lane group element m of the 16 d values the group points
   // at, for 4 consecutive keys: the group (h, d half) reads keys 4 h .. + 3 of each 8, two reads per 16 keys.
-  auto outputs = [&](int kt, int sl, const bf16x8_t (&pb)[N][2]) {
+  auto outputs = [&](int kt, int sl, const bf16x8_t (&pb)[2]) {
     const int n16 = lane & 15, half = (lane >> 4) & 1, k4 = n16 >> 2;
-    const unsigned char* row = lds_v[kt & 1] + (sl * 32 + 4 * jh + k4) * kRow + half * 32 + (n16 & 3) * 8;
+    const unsigned char* row = lds_v[kt & 1] + ((sl0 + sl) * 32 + 4 * jh + k4) * kRow + half * 32 + (n16 & 3) * 8;
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -213,28 +211,24 @@ __global__ __launch_bounds__(64 * kWaves, N == 1 ? 2 : 1) void prompt_attn_kerne
         const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)at);
         const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(at + 8 * kRow));
         const bf16x8_t a = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-        for (int n = 0; n < N; ++n) o[n][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[n][u], o[n][b], 0, 0, 0);
+        o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[u], o[b], 0, 0, 0);
       }
   };
 
   auto clear = [&]() {
+    m_ref = kLowest;
+    l_part = 0.f;
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      m_ref[n] = kLowest;
-      l_part[n] = 0.f;
+    for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[n][b][i] = 0.f;
-    }
+      for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
   };
-  auto mask = [&](floatx16_t (&s)[2], int n, int kt) {
+  auto mask = [&](floatx16_t (&s)[kSlabs], int kt) {
 #pragma unroll
-    for (int sl = 0; sl < 2; ++sl)
+    for (int sl = 0; sl < kSlabs; ++sl)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (kt * kKeyTile + sl * 32 + 8 * (i / 4) + 4 * jh + i % 4 > before + tok[n]) s[sl][i] = kNegInf;
+        if (kt * kKeyTile + (sl0 + sl) * 32 + 8 * (i / 4) + 4 * jh + i % 4 > before + tok) s[sl][i] = kNegInf;
   };
 
   clear();
@@ -243,51 +237,41 @@ __global__ __launch_bounds__(64 * kWaves, N == 1 ? 2 : 1) void prompt_attn_kerne
     stage_v(0);
     if (n_key_tiles > 1) stage_k(1);
     publish();
-    floatx16_t s[N][2];
-    float mx[N];
+    floatx16_t s[kSlabs];
     logits(s, 0);
-#pragma unroll
-    for (int n = 0; n < N; ++n) mx[n] = max_of(s[n]);
+    float mx = max_of(s);
     __syncthreads();  // tile 0's K rows are overwritten by tile 2's in the first step
-    bf16x8_t pb[2][N][2];
+    bf16x8_t pb[kSlabs][2];
     // One pipeline step: tile kt from its logits in `s`, the next tile's logits into `sn`.
-    auto step = [&](const floatx16_t (&s)[N][2], floatx16_t (&sn)[N][2], int kt) {
+    auto step = [&](const floatx16_t (&s)[kSlabs], floatx16_t (&sn)[kSlabs], int kt) {
       if (kt + 2 < n_key_tiles) stage_k(kt + 2);
       stage_v(kt + 1);
-#pragma unroll
-      for (int n = 0; n < N; ++n) follow_max(n, mx[n]);
+      follow_max(mx);
       logits(sn, kt + 1);
 #pragma unroll
-      for (int sl = 0; sl < 2; ++sl) {
-#pragma unroll
-        for (int n = 0; n < N; ++n) weights(n, s[n][sl], pb[sl][n]);
+      for (int sl = 0; sl < kSlabs; ++sl) {
+        weights(s[sl], pb[sl]);
         outputs(kt, sl, pb[sl]);
       }
-#pragma unroll
-      for (int n = 0; n < N; ++n) mx[n] = max_of(sn[n]);
+      mx = max_of(sn);
       publish();
     };
     int kt = 0;
     for (; kt < n_full; kt += 2) {
-      floatx16_t sn[N][2];
+      floatx16_t sn[kSlabs];
       step(s, sn, kt);
       step(sn, s, kt + 1);
     }
     for (; kt < n_key_tiles; ++kt) {
-      const int kt0 = kt * kKeyTile;
       // (K of tile kt + 1 was staged by the step before, or in front of the loop; that of kt + 2 is not on its way yet)
       if (kt + 1 < n_key_tiles) stage_v(kt + 1);
       if (kt + 2 < n_key_tiles) stage_k(kt + 2);
-      if (kt0 <= before + qw0 + kTokPerWave - 1) {  // else wholly behind what this wavefront's tokens see
+      if (kt * kKeyTile + sl0 * 32 <= before + qw0 + 31) {  // else wholly behind what this wavefront's tokens see
+        mask(s, kt);
+        follow_max(max_of(s));
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-          mask(s[n], n, kt);
-          follow_max(n, max_of(s[n]));
-        }
-#pragma unroll
-        for (int sl = 0; sl < 2; ++sl) {
-#pragma unroll
-          for (int n = 0; n < N; ++n) weights(n, s[n][sl], pb[sl][n]);
+        for (int sl = 0; sl < kSlabs; ++sl) {
+          weights(s[sl], pb[sl]);
           outputs(kt, sl, pb[sl]);
         }
         if (kt + 1 < n_key_tiles) logits(s, kt + 1);
@@ -297,11 +281,9 @@ __global__ __launch_bounds__(64 * kWaves, N == 1 ? 2 : 1) void prompt_attn_kerne
   }
   float sum = 0.f;  // not finite where one of them is not
 #pragma unroll
-  for (int n = 0; n < N; ++n)
+  for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sum = fmaf(o[n][b][i], 0.f, sum);
+    for (int i = 0; i < 16; ++i) sum = fmaf(o[b][i], 0.f, sum);
   if (__syncthreads_or(sum != 0.f)) {
     // An infinite or NaN value that some of a tile's tokens do not see may have reached them, through the product of a zero
     // weight with it: all again, step by step, with the tiles that are masked in part value by value.
@@ -310,63 +292,99 @@ __global__ __launch_bounds__(64 * kWaves, N == 1 ? 2 : 1) void prompt_attn_kerne
       stage_k(kt);
       stage_v(kt);
       publish();
-      floatx16_t s[N][2];
+      floatx16_t s[kSlabs];
       logits(s, kt);
+      mask(s, kt);
+      follow_max(max_of(s));
 #pragma unroll
-      for (int n = 0; n < N; ++n) {
-        mask(s[n], n, kt);
-        follow_max(n, max_of(s[n]));
-      }
-#pragma unroll
-      for (int sl = 0; sl < 2; ++sl) {
-        bf16x8_t pb[N][2];
-#pragma unroll
-        for (int n = 0; n < N; ++n) weights(n, s[n][sl], pb[n]);
-        if ((kt + 1) * kKeyTile <= before + q0 + 1) {
-          outputs(kt, sl, pb);
-        } else {
-#pragma unroll
-          for (int n = 0; n < N; ++n) outputs_seen(o[n], kt, sl, pb[n], before + tok[n]);
-        }
+      for (int sl = 0; sl < kSlabs; ++sl) {
+        bf16x8_t pb[2];
+        weights(s[sl], pb);
+        if ((kt + 1) * kKeyTile <= before + q0 + 1) outputs(kt, sl, pb);
+        else outputs_seen(o, kt, sl0 + sl, pb, before + tok);
       }
       __syncthreads();
     }
   }
 
+  float l_tot = l_part + __shfl_xor(l_part, 32);
+  if (KS == 2) {  // the second wavefront of a pair hands over what it has (the staged tiles have been read)
+    float* const o_sum = reinterpret_cast<float*>(&lds_k[0][0]) + (wave >> 1) * (kBlocks * 16 * 64);  // [register][lane]
+    float2* const ml = reinterpret_cast<float2*>(&lds_v[0][0] + (wave | 1) * (32 * kRow));  // (where no rows will lie: the second one returns)
+    static_assert(sizeof(lds_k) >= kWaves / 2 * kBlocks * 16 * 64 * 4, "outputs of half the wavefronts");
+    if (wave & 1) {
+      ml[lane] = make_float2(m_ref, l_tot);
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const float l_tot = l_part[n] + __shfl_xor(l_part[n], 32);
-    const bool none = before + tok[n] < 0;  // sees no key
-    const float inv = none ? 0.f : 1.f / l_tot;
-    if (tok[n] >= n_q) continue;
-    unsigned char* dst = reinterpret_cast<unsigned char*>(p.out.data) + out0 + tok[n] * p.out.tok;
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o_sum[(b * 16 + i) * 64 + lane] = o[b][i];
+    }
+    __syncthreads();
+    if (wave & 1) return;
+    const float2 other = ml[lane];
+    const float m = fmaxf(m_ref, other.x), mine = fast_exp2(m_ref - m), theirs = fast_exp2(other.x - m);
+    m_ref = m;
+    l_tot = l_tot * mine + other.y * theirs;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
-        bf16x4_t r;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = (__bf16)(o[n][b][4 * q + i] * inv);
-        *reinterpret_cast<bf16x4_t*>(dst + (b * 32 + q * 8 + jh * 4) * 2) = r;
-      }
-    if (p.lse.data && jh == 0)
-      *reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(p.lse.data) + lse0 + tok[n] * p.lse.tok) =
-          none ? kNegInf : m_ref[n] + __builtin_log2f(l_tot);
+      for (int i = 0; i < 16; ++i) o[b][i] = o[b][i] * mine + o_sum[(b * 16 + i) * 64 + lane] * theirs;
   }
+  const bool none = before + tok < 0;  // sees no key
+  const float inv = none ? 0.f : 1.f / l_tot;
+  if (p.lse.data && jh == 0 && tok < n_q)
+    *reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(p.lse.data) + lse0 + tok * p.lse.tok) =
+        none ? kNegInf : m_ref + __builtin_log2f(l_tot);
+  // Rows of bf16 through LDS (this wavefront's part of where V was), so that whole rows are stored.
+  unsigned char* const rows = &lds_v[0][0] + wave * (32 * kRow);
+  static_assert(sizeof(lds_v) >= kWaves * 32 * kRow, "a wavefront's rows");
+#pragma unroll
+  for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+      bf16x4_t r;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = (__bf16)(o[b][4 * q + i] * inv);
+      const int piece = 4 * b + q;
+      *reinterpret_cast<bf16x4_t*>(rows + n32 * kRow + (D == 128 ? piece ^ (n32 & 15) : piece ^ (n32 >> 1 & 7)) * 16 + jh * 8) = r;
+    }
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+  for (int i = 0; i < 32 / kCopyRows; ++i) {
+    const int r = i * kCopyRows + lane / kPieces, piece = lane % kPieces;
+    const u32x4_t x = *reinterpret_cast<const u32x4_t*>(rows + r * kRow + (D == 128 ? piece ^ (r & 15) : piece ^ (r >> 1 & 7)) * 16);
+    if (qw0 + r < n_q)
+      *reinterpret_cast<u32x4_t*>(reinterpret_cast<unsigned char*>(p.out.data) + out0 + (qw0 + r) * p.out.tok + piece * 16) = x;
+  }
+}
+
+template <int D>
+void launch(const PromptParams& p, int tile_tokens, unsigned grid, hipStream_t s) {
+  if (tile_tokens == 32 * kWaves) prompt_attn_kernel<D, 1><<<dim3(grid), dim3(64 * kWaves), 0, s>>>(p);
+  else prompt_attn_kernel<D, 2><<<dim3(grid), dim3(64 * kWaves), 0, s>>>(p);
 }
 
 }  // namespace
 
-constexpr int kN = 1;
-int prompt_tile_tokens() { return 32 * kN * kWaves; }
+// A call that would leave compute units idle, or give each no more than one workgroup of 128 tokens, whose chain of tiles it then
+// waits for, takes workgroups of 64 tokens that share their keys.  us, 128 / 64 tokens, 32 heads of 128: one prompt of 512
+// tokens 15.9 / 12.4, of 1024 (one workgroup for each) 24.4 / 20.7, 4 of 500 (two) 23.7 / 28.9, one of 2048 47.4 / 52.1; 8 heads,
+// one of 4096 75.6 / 57.6, of 8192 156 / 161.
+int prompt_tile_tokens(int64_t n_tiles128, int n_cus) { return n_tiles128 <= n_cus ? 16 * kWaves : 32 * kWaves; }
 
-hipError_t launch_prompt_attn(const PromptParams& p, int D, int n_tiles, hipStream_t s) {
-  const int64_t grid = (int64_t)n_tiles * p.Hq;
+hipError_t launch_prompt_attn(const PromptParams& p_in, int D, int tile_tokens, int n_tiles, int n_cus, hipStream_t s) {
+  const int64_t grid = (int64_t)n_tiles * p_in.Hq;
   if (grid <= 0) return hipSuccess;
   if (grid > INT32_MAX / (64 * kWaves)) return hipErrorInvalidValue;
-  if (D == 128) prompt_attn_kernel<128, kN><<<dim3((unsigned)grid), dim3(64 * kWaves), 0, s>>>(p);
-  else prompt_attn_kernel<64, kN><<<dim3((unsigned)grid), dim3(64 * kWaves), 0, s>>>(p);
+  // Longest first, which evens out many rounds of workgroups.  Where all run at once, two to a compute unit, those that join
+  // the first ones there come in the opposite order: the shortest beside the longest.
+  PromptParams p = p_in;
+  p.reversed_from = grid <= 2 * n_cus ? n_cus : INT32_MAX;
+  if (D == 128) launch<128>(p, tile_tokens, (unsigned)grid, s);
+  else launch<64>(p, tile_tokens, (unsigned)grid, s);
   return hipGetLastError();
 }
 
