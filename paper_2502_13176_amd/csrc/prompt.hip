@@ -24,6 +24,7 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float floatx16_t __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x8_t __attribute__((ext_vector_type(8)));
 
 constexpr int kWaves = 4;
 constexpr int kKeyTile = 64;        // rows per LDS stage, two slabs of 32
@@ -119,9 +120,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attn_kernel(PromptParam
   for (int c = 0; c < kChunks; ++c)
     qb[c] = as_bf16x8(*reinterpret_cast<const u32x4_t*>(Qb + tok_row * p.q.tok + c * 32 + jh * 16));
 
-  // Second product for a slab that some tokens do not see in part, value by value: a weight of zero times an infinite or NaN
-  // value is left out.
-  auto outputs_seen = [&](floatx16_t (&o)[kBlocks], int kt, int sl, const bf16x8_t (&pb)[2], int most) {
+  // What a slab that some tokens do not see in part leaves out of the second product, its infinite and NaN values, for the
+  // tokens that see them.
+  auto add_seen = [&](floatx16_t (&o)[kBlocks], int kt, int sl, const bf16x8_t (&pb)[2], int most) {
     for (int j = 0; j < 32; ++j) {
       float w = 0.f;
 #pragma unroll
@@ -137,10 +138,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attn_kernel(PromptParam
         for (int q = 0; q < 4; ++q) {
           const int piece = 4 * b + q;
           const uint2 raw = *reinterpret_cast<const uint2*>(src + (D == 128 ? piece ^ 4 * (row & 3) : piece ^ 4 * (row >> 1 & 1)) * 16 + jh * 8);
-          o[b][4 * q] = fmaf(w, __uint_as_float(raw.x << 16), o[b][4 * q]);
-          o[b][4 * q + 1] = fmaf(w, __uint_as_float(raw.x & 0xffff0000u), o[b][4 * q + 1]);
-          o[b][4 * q + 2] = fmaf(w, __uint_as_float(raw.y << 16), o[b][4 * q + 2]);
-          o[b][4 * q + 3] = fmaf(w, __uint_as_float(raw.y & 0xffff0000u), o[b][4 * q + 3]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float x = __uint_as_float(((e & 2 ? raw.y : raw.x) << (e & 1 ? 0 : 16)) & 0xffff0000u);
+            if ((__float_as_uint(x) & 0x7f800000u) == 0x7f800000u) o[b][4 * q + e] = fmaf(w, x, o[b][4 * q + e]);
+          }
         }
     }
   };
@@ -198,8 +200,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attn_kernel(PromptParam
       }
   };
   // Second product for a slab.  A transposed read hands lane m of a 16-lane group element m of the 16 d values the group points
-  // at, for 4 consecutive keys: the group (h, d half) reads keys 4 h .. + 3 of each 8, two reads per 16 keys.
-  auto outputs = [&](int kt, int sl, const bf16x8_t (&pb)[2]) {
+  // at, for 4 consecutive keys: the group (h, d half) reads keys 4 h .. + 3 of each 8, two reads per 16 keys.  finite: infinite
+  // and NaN values count as zero.
+  auto outputs = [&](int kt, int sl, const bf16x8_t (&pb)[2], bool finite = false) {
     const int n16 = lane & 15, half = (lane >> 4) & 1, k4 = n16 >> 2;
     const unsigned char* row = lds_v[kt & 1] + ((sl0 + sl) * 32 + 4 * jh + k4) * kRow + half * 32 + (n16 & 3) * 8;
 #pragma unroll
@@ -210,7 +213,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attn_kernel(PromptParam
         const unsigned char* at = row + u * 16 * kRow + (D == 128 ? b ^ k4 : b ^ (k4 >> 1)) * 64;
         const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)at);
         const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(at + 8 * kRow));
-        const bf16x8_t a = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        s16x8_t v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        if (finite) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if ((v[e] & 0x7f80) == 0x7f80) v[e] = 0;
+        }
+        const bf16x8_t a = __builtin_bit_cast(bf16x8_t, v);
         o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[u], o[b], 0, 0, 0);
       }
   };
@@ -286,7 +295,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attn_kernel(PromptParam
     for (int i = 0; i < 16; ++i) sum = fmaf(o[b][i], 0.f, sum);
   if (__syncthreads_or(sum != 0.f)) {
     // An infinite or NaN value that some of a tile's tokens do not see may have reached them, through the product of a zero
-    // weight with it: all again, step by step, with the tiles that are masked in part value by value.
+    // weight with it: all again, step by step, and the tiles that are masked in part without such values, which follow one by
+    // one.  The other tokens get the same bits as in front of such a value.
     clear();
     for (int kt = 0; kt < n_key_tiles; ++kt) {
       stage_k(kt);
@@ -300,8 +310,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_attn_kernel(PromptParam
       for (int sl = 0; sl < kSlabs; ++sl) {
         bf16x8_t pb[2];
         weights(s[sl], pb);
-        if ((kt + 1) * kKeyTile <= before + q0 + 1) outputs(kt, sl, pb);
-        else outputs_seen(o, kt, sl0 + sl, pb, before + tok);
+        const bool in_part = (kt + 1) * kKeyTile > before + q0 + 1;
+        outputs(kt, sl, pb, in_part);
+        if (in_part) add_seen(o, kt, sl0 + sl, pb, before + tok);
       }
       __syncthreads();
     }

@@ -114,8 +114,44 @@ def test_steep_logits(scale):
     run([150, 90], scale=scale)
 
 
-def test_a_long_prompt_at_some_tokens():
-    run([6000, 2049], Hq=2, Hkv=1, heads=[1], tokens=[0, 1, 63, 64, 127, 128, 2047, 2048, 4095, 5990, 5999])
+# Above, a call has at most one workgroup of 128 tokens for each of 256 compute units; these have one to two, and more.
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("lens,kv", [([257, 1, 130], None), ([300, 129, 64, 1, 500, 33], None), ([200, 640], [263, 641]), ([130, 300, 260], [60, 299, 1000]),
+                                     ([1100], None)])
+def test_more_workgroups_than_compute_units(lens, kv, D):
+    run(lens, kv, Hq=60, Hkv=4, D=D, heads=[0, 14, 15, 59], layout="heads", seed=len(lens))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_more_workgroups_with_steep_logits_and_values_that_are_not_finite(D):
+    lens = [300, 200]
+    run(lens, Hq=64, Hkv=2, D=D, scale=40.0, heads=[5, 60])
+    q, k, v = inputs(lens, lens, 64, 2, D, "packed", 8)
+    want, want_lse = B.prompt_attn(q, k, v, lens, want_lse=True)
+    v2 = v.clone()
+    v2[250] = float("inf")
+    v2[499] = float("nan")
+    out, lse = B.prompt_attn(q, k, v2, lens, want_lse=True)
+    clean = [t for t in range(500) if not 250 <= t < 300 and t != 499]
+    assert torch.equal(out[clean], want[clean]) and torch.equal(lse, want_lse)
+    assert torch.isinf(out[250:300]).all() and torch.isnan(out[499]).all()
+
+
+def test_rows_behind_the_last_sequence_and_shared_heads():
+    """Tensors that hold more tokens than the lengths name, and keys of one head handed over as several."""
+    lens = [50, 100]
+    q, k, v = inputs([50, 100, 30], [50, 100, 30], 4, 1, 64, "packed", 12)
+    k4, v4 = (t.expand(-1, 4, -1) for t in (k, v))
+    out, lse = torch.full_like(q, 3.0), torch.full((4, 180), 3.0, device="cuda")
+    B.prompt_attn(q, k4, v4, lens, out=out, lse=lse)
+    assert (out[150:] == 3).all() and (lse[:, 150:] == 3).all()
+    want, want_lse = B.prompt_attn(q[:150], k[:150], v[:150], lens, want_lse=True)
+    assert torch.equal(out[:150], want) and torch.equal(lse[:, :150], want_lse)
+
+
+@pytest.mark.parametrize("Hq", [2, 24])
+def test_a_long_prompt_at_some_tokens(Hq):
+    run([6000, 2049], Hq=Hq, Hkv=1, heads=[1], tokens=[0, 1, 63, 64, 127, 128, 2047, 2048, 4095, 5990, 5999])
 
 
 def test_equal_rows_give_their_mean():
