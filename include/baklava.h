@@ -51,7 +51,8 @@ enum {
  * Rows are rounded when they enter a cache: the scale is 2^e with e = floor(log2(a)) - 2, a the largest magnitude of the
  * 32, or one more where a exceeds 1.75 * 2^floor(log2(a)); e stays within -125 .. 125; an element becomes the nearest code,
  * ties to the one with mantissa bit 0, magnitudes above 6 the code of 6.  32 elements of which one is infinite or NaN take
- * the scale byte 255: all of them are NaN from then on.  Relative error of N(0, 1) values: 0.112 (2-norm).
+ * the scale byte 255: all of them are NaN from then on.  Relative error of N(0, 1) values: 0.112 (2-norm).  A caller that
+ * writes codes itself keeps to the scale bytes 2 .. 252 and 255: every value is then a bf16 number that is no subnormal.
  */
 enum { BAKLAVA_BF16 = 0, BAKLAVA_F32 = 1, BAKLAVA_MXFP4 = 2 };
 enum { BAKLAVA_POLICY_SCORE = 0, BAKLAVA_POLICY_STREAMING = 1 };
@@ -492,7 +493,8 @@ int baklava_qk_norm_rope(const baklava_rows* q, const baklava_rows* k, int32_t n
  * lse NULL or fp32 "rows of one element" (strides in floats, any >= 0; 4-byte aligned): row (b, t, h) receives the log2 of
  * the sum over the visible keys of 2^(q.k log2(e)/sqrt(D)), as baklava_prefill_scores takes it.  Padded places of out and lse (past a
  * sequence's length) are not written.
- * q_len HOST int32 [n_seq]; kv_len HOST int32 [n_seq] or NULL (= q_len).  D in {64, 128}; dtype BAKLAVA_BF16.  fp32
+ * q_len HOST int32 [n_seq]; kv_len HOST int32 [n_seq] or NULL (= q_len); 0 .. 2^29 each, fewer than 2^31 together, and at
+ * most 2^21 pieces of 128 query tokens of a sequence and head.  D in {64, 128}; dtype BAKLAVA_BF16.  fp32
  * accumulation; the softmax weights enter the second product as bf16.  Enqueues one kernel for every 128 sequences on
  * `stream`; deterministic.
  * Errors: EINVAL (null, misaligned, bad shape, stride or length), EHIP.

@@ -329,7 +329,7 @@ class Arena:
         v_at = rows.add(v, "v", self.batch, total, most, self.Hkv, self.D, dt)
         s_at = rows.add_values(scores, "scores", self.batch, total, most, self.Hkv) if scores is not None else None
         p0, p0_at, _, _ = _ints(pos0) if pos0 is not None else (None, None, 0, 0)
-        st = lib().baklava_append_prompt(self.ctx, layer, k_at, v_at, n_at, p0_at, s_at, _stream_ptr(stream))
+        st = lib().baklava_append_prompt(self.ctx, int(layer), k_at, v_at, n_at, p0_at, s_at, _stream_ptr(stream))
         _check(st, "baklava_append_prompt")
 
     def read_rows(self, layer_begin: int, layer_count: int, n: int, stream=None):
@@ -500,62 +500,60 @@ class _Rows:
     These wrappers run once per layer and step, where a small call takes some 5 us on the GPU: hence the care for what they
     cost on the host."""
 
+    __slots__ = ("words", "at", "n", "device", "f32")
+
     def __init__(self, torch):
-        self.torch = torch
         self.words = (C.c_int64 * 20)()
-        self.base = C.addressof(self.words)
+        self.at = C.addressof(self.words)
         self.n = 0
         self.device = _current_device() if torch.cuda.is_initialized() else -1  # (no tensor is on a GPU then)
+        self.f32 = torch.float32
 
     def on_device(self, t, name: str) -> None:
         if not t.is_cuda or t.get_device() != self.device:
             raise ValueError(f"{name} must be on the current GPU")
 
-    def _put(self, t, name, seq, tok, head) -> int:
-        self.on_device(t, name)
-        i = 4 * self.n
-        self.n += 1
-        self.words[i:i + 4] = (t.data_ptr(), seq, tok, head)
-        return self.base + 8 * i
+    def _put(self, t, seq, tok, head) -> int:
+        i, at = self.n, self.at
+        self.words[i:i + 4] = t.data_ptr(), seq, tok, head
+        self.n = i + 4
+        self.at = at + 32
+        return at
 
     def add(self, t, name: str, n_seq: int, total: int, most: int, heads: int, D: int, dtype) -> int:
         """Rows of D elements: [tokens, heads, D] packed, or [batch, heads, T, D]."""
-        if t.dtype != dtype:
-            raise ValueError(f"{name}: {dtype} expected")
-        shape, stride = t.shape, t.stride()
-        if len(shape) == 3:
-            ok = shape[0] >= total and shape[1] == heads and shape[2] == D
-            seq, tok, head = 0, stride[0], stride[1]
-        elif len(shape) == 4:
-            ok = shape[0] == n_seq and shape[1] == heads and shape[2] >= most and shape[3] == D
-            seq, head, tok = stride[:3]
+        shape = t.shape
+        if len(shape) == 3 and shape[0] >= total and shape[1] == heads and shape[2] == D:
+            tok, head, one = t.stride()
+            seq = 0
+        elif len(shape) == 4 and shape[0] == n_seq and shape[1] == heads and shape[2] >= most and shape[3] == D:
+            seq, head, tok, one = t.stride()
             if n_seq > 1 and seq == 0:
                 raise ValueError(f"{name}: sequences must not share their memory")
         else:
-            ok = False
-        if not ok:
             raise ValueError(f"{name} must be [tokens, {heads}, {D}] or [batch, {heads}, T, {D}] and hold all tokens")
-        if stride[-1] != 1:
-            raise ValueError(f"{name}: contiguous rows expected")
-        return self._put(t, name, seq, tok, head)
+        if one != 1 or t.dtype is not dtype:
+            raise ValueError(f"{name}: contiguous rows of {dtype} expected")
+        if not t.is_cuda or t.get_device() != self.device:
+            raise ValueError(f"{name} must be on the current GPU")
+        return self._put(t, seq, tok, head)
 
     def add_values(self, t, name: str, n_seq: int, total: int, most: int, heads: int) -> int:
         """One fp32 value per token and head: [heads, tokens] packed, or [batch, heads, T]."""
-        if t.dtype != self.torch.float32:
-            raise ValueError(f"{name}: float32 expected")
-        shape, stride = t.shape, t.stride()
-        if len(shape) == 2:
-            ok = shape[0] == heads and shape[1] >= total
-            seq, tok, head = 0, stride[1], stride[0]
+        shape = t.shape
+        if len(shape) == 2 and shape[0] == heads and shape[1] >= total:
+            head, tok = t.stride()
+            seq = 0
+        elif len(shape) == 3 and shape[0] == n_seq and shape[1] == heads and shape[2] >= most:
+            seq, head, tok = t.stride()
+            if n_seq > 1 and seq == 0:
+                raise ValueError(f"{name}: sequences must not share their memory")
         else:
-            ok = len(shape) == 3 and shape[0] == n_seq and shape[1] == heads and shape[2] >= most
-            if ok:
-                seq, head, tok = stride
-                if n_seq > 1 and seq == 0:
-                    raise ValueError(f"{name}: sequences must not share their memory")
-        if not ok:
             raise ValueError(f"{name} must be [{heads}, tokens] or [batch, {heads}, T] and hold all tokens")
-        return self._put(t, name, seq, tok, head)
+        if t.dtype is not self.f32:
+            raise ValueError(f"{name}: float32 expected")
+        self.on_device(t, name)
+        return self._put(t, seq, tok, head)
 
 
 def prompt_attn(q, k, v, lens: Sequence[int], kv_lens: Optional[Sequence[int]] = None, out=None, lse=None,
@@ -655,7 +653,7 @@ def qk_norm_rope(q, k, pos, inv_freq: Sequence[float], q_weight=None, k_weight=N
             raise ValueError(f"{name}_out must have the shape of {name}")
         out_at[i], outs[i] = rows.add(o, f"{name}_out", n_seq, tokens, T, h, D, dtype), o
     _check(lib().baklava_qk_norm_rope(in_at[0], in_at[1], n_seq, T, heads[0], heads[1], D,
-                                      BF16 if dtype is torch.bfloat16 else F32, w_at[0], w_at[1], eps, pos_at, axes, axis,
+                                      BF16 if dtype is torch.bfloat16 else F32, w_at[0], w_at[1], float(eps), pos_at, axes, axis,
                                       freq.buffer_info()[0], 2 * n_freq, 1 if interleaved else 0, out_at[0], out_at[1],
                                       _stream_ptr(stream)), "baklava_qk_norm_rope")
     _hold_until_stream_passes(outs, stream)

@@ -67,6 +67,19 @@ def test_token_and_head_counts(n, Hq, Hkv):
     run("bf16", n, Hq, Hkv, 64, seed=n)
 
 
+@pytest.mark.parametrize("Hq,Hkv", [(0, 3), (40, 1), (130, 2)])
+def test_many_heads_and_none(Hq, Hkv):
+    """More heads than a workgroup takes rows at a time; keys alone."""
+    x = torch.randn((6, Hq + Hkv, 128)).bfloat16().cuda()
+    pos = torch.arange(6, dtype=torch.int32).cuda()
+    f = 10000.0 ** (-np.arange(64) / 64)
+    q, k = B.qk_norm_rope(x[:, :Hq] if Hq else None, x[:, Hq:], pos, f)
+    every = B.qk_norm_rope(x, None, pos, f)[0]
+    assert torch.equal(k, every[:, Hq:]) and (q is None or torch.equal(q, every[:, :Hq]))
+    want, _ = OP.norm_rope(x.double().cpu().numpy(), None, 0.0, pos.cpu().numpy()[None], f, [0] * 64, False)
+    assert (np.abs(every.double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + FP32 * 8).all()
+
+
 @pytest.mark.parametrize("far", [131072, 1 << 24, (1 << 31) - 1])
 def test_far_positions(far):
     run("f32", 64, 2, 1, 128, far=far, base=500000.0)
