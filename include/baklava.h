@@ -193,7 +193,7 @@ size_t baklava_workspace_bytes(const baklava_desc* desc, const int32_t* cap_host
  * len_host may be NULL for all-empty caches, in which case the caller must have zeroed desc->len
  * or call baklava_reset.  Writes the work-item table into the workspace with a synchronous copy.
  * Supported shapes: D in {64, 128}; Hq a multiple of Hkv with Hq/Hkv <= 16 (<= 8 for F32 and for BF16 with D = 64);
- * sink, recent >= 0.
+ * sink, recent >= 0; capacities of MXFP4 caches at most 2^25 rows each.
  * The arena must be packed the way baklava_layout lays it out: off_host[c] = sum of the capacities
  * of the caches before c (workspace planes that run parallel to the arena use the same offsets).
  * Errors: EINVAL (also: offsets that are not the packed prefix sums), EINFEASIBLE (some budget <

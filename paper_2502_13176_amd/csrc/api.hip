@@ -74,6 +74,9 @@ bool keeps_records(const baklava_desc* d) { return d->dtype == BAKLAVA_MXFP4 || 
 // Bytes of a row of queries (and of new rows), and of a cached row.
 int32_t query_row_bytes(const baklava_desc* d) { return d->D * (d->dtype == BAKLAVA_F32 ? 4 : 2); }
 int32_t cache_row_bytes(const baklava_desc* d) { return d->dtype == BAKLAVA_MXFP4 ? d->D / 2 : query_row_bytes(d); }
+// Rows of a cache: the offsets of 4-bit rows inside a work item are held in 32 bits (with 64 the attention kernel has no register
+// left and takes 2% longer), and an option may make an item of a whole cache.
+int32_t most_rows(const baklava_desc* d) { return d->dtype == BAKLAVA_MXFP4 ? 1 << 25 : INT32_MAX; }
 
 WorkspacePlan plan_workspace(const baklava_desc* d, const int32_t* cap) {
   WorkspacePlan w{};
@@ -168,6 +171,12 @@ struct baklava_ctx {
 
 namespace {
 
+// 4-bit rows: one round of workgroups, which are of eight wavefronts; two to a compute unit where there is enough to read
+// (one alone keeps too few loads in flight), one where each more work item costs more than it gives.  us per call with one /
+// two / five, attention alone, four heads, D = 128: 8 caches of 32768 rows 14.6 / 14.8 / 18.6, 64 of 10000 22.0 / 22.3 / 26.4, of
+// 32768 60.6 / 52.4 / 61.2, 256 of 2000 16.5 / 18.6 / 24.2, of 8192 54.1 / 54.2 / 57.1.
+int mx_items_per_cu(int64_t rows, int64_t cus) { return rows <= 2560 * cus ? 1 : 2; }
+
 // Work items per compute unit that a launch over the whole model aims at: runs long enough to amortise the per-item
 // costs (a merge of the wavefronts, and of the split partials), yet enough of them to even out the load.  Two run side by
 // side on a compute unit, so two are best while every cache can still be cut into about four (as for one wave of a layer),
@@ -177,12 +186,6 @@ namespace {
 // (three) 66.7 / 65.3 and 82.1 / 80.3; D = 64, 64 18.1 / 15.3 and 29.6 / 24.1; fp32, D = 128, 64 53.3 / 47.0 and 68.9 / 55.8;
 // 128 caches of 65536 rows (four) 632 / 627 and 733 / 724, with two 628 and 736; 256 of 8192 rows with four instead of five
 // 160 / 163 (one head) and 165 / 165, with two 197.
-// 4-bit rows: one round of workgroups, which are of eight wavefronts; two to a compute unit where there is enough to read
-// (one alone keeps too few loads in flight), one where each more work item costs more than it gives.  us per call with one /
-// two / five, attention alone, four heads, D = 128: 8 caches of 32768 rows 14.6 / 14.8 / 18.6, 64 of 10000 22.0 / 22.3 / 26.4, of
-// 32768 60.6 / 52.4 / 61.2, 256 of 2000 16.5 / 18.6 / 24.2, of 8192 54.1 / 54.2 / 57.1.
-int mx_items_per_cu(int64_t rows, int64_t cus) { return rows <= 2560 * cus ? 1 : 2; }
-
 int whole_items_per_cu(int64_t n_caches, int64_t rows, int64_t cus) {
   if (4 * n_caches <= 2 * cus) return rows <= 2 * cus * 8192 ? 2 : 4;
   if (4 * n_caches <= 3 * cus) return 3;
@@ -517,7 +520,7 @@ extern "C" size_t baklava_workspace_bytes(const baklava_desc* desc, const int32_
   if (!shape_ok(desc) || !cap_host || !budget_host) return 0;
   const int64_t n_caches = (int64_t)desc->L * desc->batch * desc->Hkv;
   for (int64_t c = 0; c < n_caches; ++c)
-    if (cap_host[c] < 0) return 0;
+    if (cap_host[c] < 0 || cap_host[c] > most_rows(desc)) return 0;
   for (int64_t i = 0; i < (int64_t)desc->L * desc->Hkv; ++i)
     if (budget_host[i] < 0) return 0;
   return plan_workspace(desc, cap_host).total;
@@ -545,7 +548,7 @@ extern "C" int baklava_create(const baklava_desc* desc, const int64_t* off_host,
   // workspace planes that run parallel to the arena (kept lists) are indexed by the same offsets.
   int64_t packed = 0;
   for (int64_t c = 0; c < n_caches; ++c) {
-    if (cap_host[c] < 0 || off_host[c] != packed) return BAKLAVA_EINVAL;
+    if (cap_host[c] < 0 || cap_host[c] > most_rows(desc) || off_host[c] != packed) return BAKLAVA_EINVAL;
     packed += cap_host[c];
     if (len_host && (len_host[c] < 0 || len_host[c] > cap_host[c])) return BAKLAVA_ECAPACITY;
   }

@@ -115,6 +115,20 @@ def test_contexts_of_4_bit_rows_refuse():
     assert create(d) == B.EINVAL
 
 
+def test_caches_of_4_bit_rows_have_a_most_length():
+    i32p, i64p = C.POINTER(C.c_int32), C.POINTER(C.c_int64)
+    budget = np.asarray([64, 64], dtype=np.int32)
+    for more in (0, 1):
+        cap = np.asarray([(1 << 25) + more, 64], dtype=np.int32)
+        off = np.asarray([0, cap[0]], dtype=np.int64)
+        d, ctx = mx_desc(), C.c_void_p()
+        size = B.lib().baklava_workspace_bytes(C.byref(d), cap.ctypes.data_as(i32p), budget.ctypes.data_as(i32p))
+        assert (size == 0) == bool(more)
+        if more:
+            assert B.lib().baklava_create(C.byref(d), off.ctypes.data_as(i64p), cap.ctypes.data_as(i32p), None,
+                                          budget.ctypes.data_as(i32p), C.byref(ctx)) == B.EINVAL
+
+
 def test_workspace_of_4_bit_rows_holds_records_of_bf16_queries():
     i32p = C.POINTER(C.c_int32)
     cap = np.full(2, 500, dtype=np.int32)
