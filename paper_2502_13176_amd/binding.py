@@ -232,8 +232,6 @@ class Arena:
         self.budget_host = _i32(budget)
         self.off_host, self.cap_host, self.total_tokens = layout(budget, L, Hkv, batch, slack)
         self.n_caches = L * batch * Hkv
-        if dtype not in ("bf16", "f32", "mxfp4"):
-            raise ValueError("dtype must be bf16, f32 or mxfp4")
         mx = dtype == "mxfp4"  # rows of D / 2 bytes of codes, their scales in a plane of their own
         tdt = torch.uint8 if mx else torch.bfloat16 if dtype == "bf16" else torch.float32
         dev = self.device
@@ -323,7 +321,7 @@ class Arena:
         if len(lens) != self.batch or (pos0 is not None and len(pos0) != self.batch):
             raise ValueError("one length (and position) per sequence expected")
         n, n_at, total, most = _ints(lens)
-        dt = self.torch.float32 if self.dtype == "f32" else self.torch.bfloat16
+        dt = self.torch.bfloat16 if self.dtype in ("bf16", "mxfp4") else self.torch.float32
         rows = _Rows(self.torch)
         k_at = rows.add(k, "k", self.batch, total, most, self.Hkv, self.D, dt)
         v_at = rows.add(v, "v", self.batch, total, most, self.Hkv, self.D, dt)
@@ -336,7 +334,7 @@ class Arena:
         """baklava_read_rows: the last n rows of every cache of the range as values, (k, v) [caches, n, D]."""
         if n < 1 or layer_count < 1:
             raise ValueError("at least one row of one layer expected")
-        dt = self.torch.float32 if self.dtype == "f32" else self.torch.bfloat16
+        dt = self.torch.bfloat16 if self.dtype in ("bf16", "mxfp4") else self.torch.float32
         shape = (layer_count * self.batch * self.Hkv, n, self.D)
         k, v = (self.torch.empty(shape, dtype=dt, device=self.device) for _ in range(2))
         _check(lib().baklava_read_rows(self.ctx, int(layer_begin), int(layer_count), int(n), k.data_ptr(), v.data_ptr(),

@@ -326,5 +326,63 @@ def test_context_options_and_refusals():
     with pytest.raises(B.BaklavaError) as e:
         c.a.decode_attn(0, 1, qd, torch.empty((1, 1, 4, 64), device="cuda"))
     assert e.value.status == B.ESTATE
-    with pytest.raises(ValueError):
-        B.Arena(1, 4, 2, 64, 1, "int4", [20, 20], 1, 2, 4)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_prompt_between_tracked_steps(D):
+    """Calls on record when more rows come in: they owe those rows nothing."""
+    c = Cache([70, 300], 4, 1, D, batch=2, slack=60, track=True)
+    calls = 0
+    for turn in range(3):
+        for t in range(5):
+            (k, kd), (v, vd), (q, qd) = c.new(1), c.new(1), c.q(1)
+            out = torch.full((1, 2, 4, D), float("nan"), device="cuda")
+            c.a.append_decode_attn(0, 1, kd, vd, 900 + calls, qd, out)
+            torch.cuda.synchronize()
+            for x in range(2):
+                c.grow(x, f64(k[0, x, 0]), f64(v[0, x, 0]), 900 + calls)
+            c.attend(0, 1, q, f64(out), weigh=True)
+            calls += 1
+        n = [7, 0] if turn else [3, 11]
+        k, v = (bf16(c.rng.standard_normal((sum(n), 1, D))) for _ in range(2))
+        sc = torch.from_numpy(c.rng.random((1, sum(n))).astype(np.float32))
+        c.a.append_prompt(0, k.cuda(), v.cuda(), n, [2000, 3000], scores=sc.cuda())
+        at = 0
+        for x in range(2):
+            for i in range(n[x]):
+                c.grow(x, f64(k[at, 0]), f64(v[at, 0]), (2000, 3000)[x] + i)
+                c.score[x][-1] = float(sc[0, at])
+                at += 1
+    c.a.flush_scores(0, 1)
+    c.check_planes(calls)
+
+
+def test_caches_behind_many_rows():
+    """Rows whose byte offsets take more than 32 bits: the same caches with and without three long empty ones in front."""
+    D, lens = 128, [0, 0, 0, 300, 40, 1, 77, 600]
+    far, near = (B.Arena(2, 16, 4, D, 1, "mxfp4", [m] * 3 + [700] * 5, 8, 2, 4, B.POLICY_SCORE, True) for m in ((1 << 25) - 8, 700))
+    assert int(far.off_host[3]) * D // 2 > 1 << 32
+    g = torch.Generator().manual_seed(3)
+    rows = {p: [torch.randint(lo, hi, (n, w), generator=g).to(torch.uint8).cuda() for n in lens]
+            for p, w, lo, hi in (("k", D // 2, 0, 256), ("v", D // 2, 0, 256), ("kv_scale", D // 16, 124, 129))}
+    q, kn, vn = (torch.randn((2, 1, h, D), generator=g).bfloat16().cuda() for h in (16, 4, 4))
+    kp, vp = (torch.randn((5, 4, D), generator=g).bfloat16().cuda() for _ in range(2))
+    got = []
+    for a in (far, near):
+        for p, x in rows.items():
+            for c, n in enumerate(lens):
+                a.__dict__[p][int(a.off_host[c]):int(a.off_host[c]) + n] = x[c]
+        a.score.zero_(), a.pos.zero_()
+        a.set_lengths(lens)
+        out = torch.empty((2, 1, 16, D), device="cuda")
+        for layer in range(2):
+            a.append_prompt(layer, kp, vp, [5])
+            a.append_decode_attn(layer, 1, kn[layer], vn[layer], 9, q[layer], out[layer])
+        a.flush_scores(0, 2)
+        a.compact(0, 2)
+        k, v = a.read_rows(0, 2, 20)
+        n = [x + 6 for x in lens]
+        got.append((out, k, v, torch.cat([a.score[int(a.off_host[c]):int(a.off_host[c]) + n[c]] for c in range(8)])))
+        assert a.lengths().tolist() == n
+    for x, y in zip(*got[:2]):
+        assert torch.equal(x, y) if x.dtype is torch.bfloat16 else torch.allclose(x, y, rtol=2.0 ** -16, atol=2.0 ** -16)

@@ -137,6 +137,38 @@ def test_more_workgroups_with_steep_logits_and_values_that_are_not_finite(D):
     assert torch.isinf(out[250:300]).all() and torch.isnan(out[499]).all()
 
 
+def test_more_workgroups_of_many_padded_sequences():
+    rng = np.random.default_rng(5)
+    lens = [int(x) for x in rng.integers(0, 200, 150)]
+    run(lens, [max(0, n + int(rng.integers(-5, 90))) for n in lens], Hq=4, Hkv=2, D=64, layout="padded", heads=[1, 2])
+
+
+def test_tokens_far_apart():
+    """Offsets of more than 2^31 elements, of tokens that are 2^20 elements apart."""
+    n, w = 2100, 1 << 20
+    far = torch.empty((n, w), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator().manual_seed(4)
+    q, k, v = (torch.randn((n, h, 64), generator=g).bfloat16().cuda() for h in (4, 2, 2))
+    at = {}
+    for name, x, i in (("q", q, 0), ("k", k, 4), ("v", v, 6), ("out", torch.zeros_like(q), 8), ("q_out", torch.zeros_like(q), 12)):
+        at[name] = far[:, 64 * i:64 * (i + x.shape[1])].unflatten(1, (-1, 64))
+        at[name].copy_(x)
+    want, want_lse = B.prompt_attn(q, k, v, [n - 50, 50], want_lse=True)
+    _, lse = B.prompt_attn(at["q"], at["k"], at["v"], [n - 50, 50], out=at["out"], want_lse=True)
+    assert torch.equal(at["out"], want) and torch.equal(lse, want_lse)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    f = [0.5 ** i for i in range(32)]
+    B.qk_norm_rope(at["q"], None, pos, f, q_out=at["q_out"])
+    assert torch.equal(at["q_out"], B.qk_norm_rope(q, None, pos, f)[0])
+    for dtype in ("bf16", "mxfp4"):
+        rows = []
+        for x, y in ((k, v), (at["k"], at["v"])):
+            a = B.Arena(1, 4, 2, 64, 2, dtype, [n] * 2, 0, 0, 0)
+            a.append_prompt(0, x, y, [n - 50, 50])
+            rows.append(a.read_rows(0, 1, n))
+        assert torch.equal(rows[0][0], rows[1][0]) and torch.equal(rows[0][1], rows[1][1])
+
+
 def test_rows_behind_the_last_sequence_and_shared_heads():
     """Tensors that hold more tokens than the lengths name, and keys of one head handed over as several."""
     lens = [50, 100]
