@@ -13,7 +13,18 @@
 //
 // A workgroup of 4 wavefronts owns 128 consecutive tokens of one head, 32 per wavefront.  Keys and values go from memory to
 // LDS without a stop in registers, in tiles of 64 rows, double-buffered.  The tiles that all of its tokens see form a software
-// pipeline: the first product of tile n + 1 runs beside the exponentials of tile n.  The others follow, masked.
+// pipeline: the first product of tile n + 1 runs beside the exponentials of tile n.  The others follow, masked.  Small launches
+// take workgroups of 64 tokens, two wavefronts to 32 tokens, each with one half of every tile of keys; their sums are added at
+// the end (rule and figures at prompt_tile_tokens).  Outputs that are not finite are computed a second time, by a loop of its own
+// at the end: in the main loop the test alone cost registers that went to scratch memory (8 prompts of 4096, 28 heads, 1229 / 1005
+// us).
+//
+// One prompt of 16384, 32 heads of 128: 1.97 to 2.05 ms by the box, 1.07 to 1.12 PFLOP/s, where a product of two matrices of 16384^2
+// reaches 1.28 to 1.30.  The power of the products bounds it: the matrix cores are busy 63% of the time at some 1.6 GHz, and
+// orders of instructions or waves' priorities make no difference.  (64 tokens per wavefront, one wavefront per SIMD, whose
+// operands from LDS serve twice as many products: 728 TFLOP/s, nothing runs beside a wavefront's exponentials.)  Heads of 64:
+// 0.93 PFLOP/s, bound by the vector ALUs, whose exponentials stand beside half the products.  8 prompts of 128 to 8192 tokens,
+// 28 heads, 2.35 ms.
 #include "common.h"
 
 namespace baklava {

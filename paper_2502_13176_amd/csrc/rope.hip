@@ -8,8 +8,8 @@
 // frequency needs more bits than fp32 has: at 131072 the error would be 0.008), through LDS to the lanes that need it, while
 // the first rows are on their way.
 //
-// 32768 tokens of 40 heads of 128 bf16 elements take 119 us, 5.6 TB/s read and written (6.2 is what a copy reaches), 12000 of
-// 24 heads in fp32 48 us, 6.1 TB/s; 8 tokens 4.7 us on the device, which the host's 17 us hide.
+// 32768 tokens of 40 heads of 128 bf16 elements take 115 to 119 us, 5.6 to 5.8 TB/s read and written (6.2 is what a copy reaches),
+// 12000 of 24 heads in fp32 48 us, 6.1 TB/s; 8 tokens 4.7 us on the device, which the 16 us of a call from Python hide.
 #include "common.h"
 
 #include <algorithm>
