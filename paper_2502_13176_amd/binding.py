@@ -336,7 +336,7 @@ class Arena:
             raise ValueError("at least one row of one layer expected")
         dt = self.torch.bfloat16 if self.dtype in ("bf16", "mxfp4") else self.torch.float32
         shape = (layer_count * self.batch * self.Hkv, n, self.D)
-        k, v = (self.torch.empty(shape, dtype=dt, device=self.device) for _ in range(2))
+        k, v = (_empty_on(stream, self.torch.empty, shape, dtype=dt, device=self.device) for _ in range(2))
         _check(lib().baklava_read_rows(self.ctx, int(layer_begin), int(layer_count), int(n), k.data_ptr(), v.data_ptr(),
                                        _stream_ptr(stream)), "baklava_read_rows")
         _hold_until_stream_passes((k, v), stream)
@@ -368,15 +368,29 @@ def stream_probe(dst, src, nbytes: int, mode: int, stream=None) -> None:
                                       _stream_ptr(stream)), "baklava_stream_probe")
 
 
+def _empty_on(stream, make, *shape, **kw):
+    """make(*shape, **kw), an allocation for kernels of `stream` (None: torch's current one).  It has to come from that stream's
+    part of the caching allocator: a block of the current stream's part may have been dropped while kernels of the current
+    stream still use it, and nothing would order another stream's kernels behind those."""
+    if stream is None:
+        return make(*shape, **kw)
+    import torch
+    with torch.cuda.stream(stream):
+        return make(*shape, **kw)
+
+
 def _hold_until_stream_passes(tensors, stream) -> None:
-    """Tensors allocated here on torch's current stream but used by kernels enqueued on another one:
-    the caching allocator must not hand their memory out again before that stream has passed the call
-    (the workspace is dropped as soon as the wrapper returns)."""
+    """Tensors that kernels enqueued on another stream than torch's current one use, and that the caller may use on the current
+    one: the caching allocator must not hand their memory out again before both have passed their use.  (A workspace that comes
+    from the other stream's part and is used there alone needs none of this.)"""
     if stream is None:
         return
+    import torch
+    here = torch.cuda.current_stream()
     for t in tensors:
         if t is not None:
             t.record_stream(stream)
+            t.record_stream(here)
 
 
 def kv_importance(similarity, L: int, Hq: int, Hkv: int) -> np.ndarray:
@@ -406,16 +420,16 @@ def profile_similarity(q, k, v, want_cos: bool = True, want_lse: bool = False, s
         raise ValueError("bf16 tensors expected")
     if not (q.is_contiguous() and k.is_contiguous() and v.is_contiguous()):
         raise ValueError("contiguous tensors expected")
-    sim = torch.empty((batch, Hq), dtype=torch.float32, device=q.device)
-    cos = torch.empty((batch, Hq, T), dtype=torch.float32, device=q.device) if want_cos else None
-    lse = torch.empty((batch, Hq, T), dtype=torch.float32, device=q.device) if want_lse else None
+    sim = _empty_on(stream, torch.empty, (batch, Hq), dtype=torch.float32, device=q.device)
+    cos = _empty_on(stream, torch.empty, (batch, Hq, T), dtype=torch.float32, device=q.device) if want_cos else None
+    lse = _empty_on(stream, torch.empty, (batch, Hq, T), dtype=torch.float32, device=q.device) if want_lse else None
     nbytes = profile_workspace_bytes(batch, Hq, T)
-    ws = torch.empty((max(nbytes, 256),), dtype=torch.uint8, device=q.device)
+    ws = _empty_on(stream, torch.empty, (max(nbytes, 256),), dtype=torch.uint8, device=q.device)
     _check(lib().baklava_profile_similarity(q.data_ptr(), k.data_ptr(), v.data_ptr(), batch, Hq, Hkv, T, D, BF16,
                                             cos.data_ptr() if want_cos else None, sim.data_ptr(),
                                             lse.data_ptr() if want_lse else None, ws.data_ptr(),
                                             nbytes, _stream_ptr(stream)), "baklava_profile_similarity")
-    _hold_until_stream_passes((ws, sim, cos, lse), stream)
+    _hold_until_stream_passes((sim, cos, lse), stream)
     return (sim, cos, lse) if want_lse else (sim, cos)
 
 
@@ -450,14 +464,14 @@ def layer_similarity(x_in, x_out, want_cos: bool = True, stream=None):
         raise ValueError("two bf16 tensors of equal shape expected")
     if not (x_in.is_contiguous() and x_out.is_contiguous()):
         raise ValueError("contiguous tensors expected")
-    sim = torch.empty((n_seq,), dtype=torch.float32, device=x_in.device)
-    cos = torch.empty((n_seq, T), dtype=torch.float32, device=x_in.device) if want_cos else None
+    sim = _empty_on(stream, torch.empty, (n_seq,), dtype=torch.float32, device=x_in.device)
+    cos = _empty_on(stream, torch.empty, (n_seq, T), dtype=torch.float32, device=x_in.device) if want_cos else None
     nbytes = int(lib().baklava_layer_workspace_bytes(n_seq, T))
-    ws = torch.empty((max(nbytes, 256),), dtype=torch.uint8, device=x_in.device)
+    ws = _empty_on(stream, torch.empty, (max(nbytes, 256),), dtype=torch.uint8, device=x_in.device)
     _check(lib().baklava_layer_similarity(x_in.data_ptr(), x_out.data_ptr(), n_seq, T, hidden, BF16,
                                           cos.data_ptr() if want_cos else None, sim.data_ptr(), ws.data_ptr(), nbytes,
                                           _stream_ptr(stream)), "baklava_layer_similarity")
-    _hold_until_stream_passes((ws, sim, cos), stream)
+    _hold_until_stream_passes((sim, cos), stream)
     return sim, cos
 
 
@@ -577,9 +591,9 @@ def prompt_attn(q, k, v, lens: Sequence[int], kv_lens: Optional[Sequence[int]] =
     at = [rows.add(q, "q", n_seq, total, most, Hq, D, dt), rows.add(k, "k", n_seq, k_total, k_most, Hkv, D, dt),
           rows.add(v, "v", n_seq, k_total, k_most, Hkv, D, dt)]
     if out is None:
-        out = q.new_empty(q_shape)
+        out = _empty_on(stream, q.new_empty, q_shape)
     if lse is None and want_lse:
-        lse = q.new_empty((Hq, q_shape[0]) if len(q_shape) == 3 else q_shape[:3], dtype=torch.float32)
+        lse = _empty_on(stream, q.new_empty, (Hq, q_shape[0]) if len(q_shape) == 3 else q_shape[:3], dtype=torch.float32)
     at.append(rows.add(out, "out", n_seq, total, most, Hq, D, dt))
     at.append(rows.add_values(lse, "lse", n_seq, total, most, Hq) if lse is not None else None)
     _check(lib().baklava_prompt_attn(at[0], at[1], at[2], n_seq, q_at, k_at, Hq, Hkv, D, BF16, at[3], at[4],
@@ -646,7 +660,7 @@ def qk_norm_rope(q, k, pos, inv_freq: Sequence[float], q_weight=None, k_weight=N
             rows.on_device(w, f"{name}_weight")
             w_at[i] = w.data_ptr()
         if o is None:
-            o = t.new_empty(t.shape)
+            o = _empty_on(stream, t.new_empty, t.shape)
         elif o.shape != t.shape:
             raise ValueError(f"{name}_out must have the shape of {name}")
         out_at[i], outs[i] = rows.add(o, f"{name}_out", n_seq, tokens, T, h, D, dtype), o
