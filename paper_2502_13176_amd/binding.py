@@ -435,7 +435,20 @@ def profile_similarity(q, k, v, want_cos: bool = True, want_lse: bool = False, s
 
 def prefill_scores(q, k_plane, lse, score_plane, batch: int, Hq: int, Hkv: int, T: int, row_off=None, stream=None):
     """baklava_prefill_scores: q [batch, Hq, T, 128] bf16, lse [batch, Hq, T] fp32, k_plane a bf16 tensor of
-    rows of 128 elements, score_plane fp32 rows, row_off an int64 device tensor [batch * Hkv] or None (dense)."""
+    rows of 128 elements (an arena's K plane: of a "bf16" arena, 4-bit rows are none), score_plane fp32, one value per row of
+    k_plane, row_off an int64 device tensor [batch * Hkv] or None (dense).  Contiguous tensors."""
+    import torch
+    if q.dtype is not torch.bfloat16 or k_plane.dtype is not torch.bfloat16 or k_plane.dim() < 1 or k_plane.shape[-1] != 128:
+        raise ValueError("q and k_plane must hold bf16 rows of 128 elements")
+    if lse.dtype is not torch.float32 or score_plane.dtype is not torch.float32:
+        raise ValueError("lse and score_plane must be fp32")
+    if not (q.is_contiguous() and k_plane.is_contiguous() and lse.is_contiguous() and score_plane.is_contiguous()):
+        raise ValueError("contiguous tensors expected")
+    rows = batch * Hkv * T if row_off is None else T  # (at least: with row_off the rows of a sequence lie where it says)
+    if q.numel() < batch * Hq * T * 128 or lse.numel() < batch * Hq * T or k_plane.numel() < rows * 128 or score_plane.numel() < rows:
+        raise ValueError("tensors too small for batch, heads and T")
+    if row_off is not None and (row_off.dtype is not torch.int64 or not row_off.is_contiguous() or row_off.numel() < batch * Hkv):
+        raise ValueError("row_off must be a contiguous int64 tensor of one row per sequence and KV head")
     _check(lib().baklava_prefill_scores(q.data_ptr(), k_plane.data_ptr(), lse.data_ptr(),
                                         row_off.data_ptr() if row_off is not None else None, batch, Hq, Hkv, T, 128,
                                         BF16, score_plane.data_ptr(), _stream_ptr(stream)), "baklava_prefill_scores")

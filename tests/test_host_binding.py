@@ -1,0 +1,26 @@
+"""What the binding refuses before it calls the library, without a GPU."""
+import pytest
+import torch
+
+from paper_2502_13176_amd import binding as B
+
+
+def scores(**kw):
+    a = dict(q=torch.zeros((2, 4, 6, 128), dtype=torch.bfloat16), k_plane=torch.zeros((2, 2, 6, 128), dtype=torch.bfloat16),
+             lse=torch.zeros((2, 4, 6)), score_plane=torch.zeros((24,)), batch=2, Hq=4, Hkv=2, T=6)
+    B.prefill_scores(**{**a, **kw})
+
+
+@pytest.mark.parametrize("kw", [
+    dict(k_plane=torch.zeros((24, 64), dtype=torch.uint8)),                           # the K plane of a 4-bit arena
+    dict(k_plane=torch.zeros((24, 64), dtype=torch.uint8), row_off=torch.zeros((4,), dtype=torch.int64)),
+    dict(k_plane=torch.zeros((5, 128), dtype=torch.bfloat16), row_off=torch.zeros((4,), dtype=torch.int64)),
+    dict(k_plane=torch.zeros((48, 64), dtype=torch.bfloat16)), dict(k_plane=torch.zeros((24, 128))), dict(q=torch.zeros((2, 4, 6, 128))),
+    dict(k_plane=torch.zeros((23, 128), dtype=torch.bfloat16)), dict(q=torch.zeros((2, 4, 5, 128), dtype=torch.bfloat16)),
+    dict(q=torch.zeros((2, 6, 4, 128), dtype=torch.bfloat16).transpose(1, 2)), dict(lse=torch.zeros((2, 4, 6), dtype=torch.float64)),
+    dict(lse=torch.zeros((4, 6))), dict(lse=torch.zeros((2, 4, 12))[:, :, ::2]), dict(score_plane=torch.zeros((23,))),
+    dict(score_plane=torch.zeros((24,), dtype=torch.bfloat16)), dict(row_off=torch.zeros((3,), dtype=torch.int64)),
+    dict(row_off=torch.zeros((4,), dtype=torch.int32))])
+def test_prefill_scores_refuses(kw):
+    with pytest.raises(ValueError):
+        scores(**kw)
