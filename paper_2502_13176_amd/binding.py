@@ -232,7 +232,7 @@ class Arena:
         self.budget_host = _i32(budget)
         self.off_host, self.cap_host, self.total_tokens = layout(budget, L, Hkv, batch, slack)
         self.n_caches = L * batch * Hkv
-        mx = dtype == "mxfp4"  # rows of D / 2 bytes of codes, their scales in a plane of their own
+        mx = self.mx = dtype == "mxfp4"  # rows of D / 2 bytes of codes, their scales in a plane of their own
         tdt = torch.uint8 if mx else torch.bfloat16 if dtype == "bf16" else torch.float32
         dev = self.device
         self.k = torch.zeros((self.total_tokens, D // 2 if mx else D), dtype=tdt, device=dev)
@@ -290,18 +290,30 @@ class Arena:
         a = _i32(len_host)
         _check(lib().baklava_set_lengths(self.ctx, _p(a, C.c_int32), _stream_ptr(stream)), "baklava_set_lengths")
 
+    def _expect_bf16(self, *rows) -> None:
+        """Rows for caches in 4 bits: codes in their place would be read as rows four times as long."""
+        for t in rows:
+            if t.dtype is not self.torch.bfloat16:
+                raise ValueError("queries and new rows of an mxfp4 arena are bf16")
+
     def append(self, layer_begin: int, layer_count: int, k_new, v_new, token_pos: int, stream=None) -> None:
+        if self.mx:
+            self._expect_bf16(k_new, v_new)
         _check(lib().baklava_append(self.ctx, layer_begin, layer_count, k_new.data_ptr(), v_new.data_ptr(),
                                     int(token_pos), _stream_ptr(stream)), "baklava_append")
 
     def append_decode_attn(self, layer_begin: int, layer_count: int, k_new, v_new, token_pos: int, q, out,
                            stream=None) -> None:
+        if self.mx:
+            self._expect_bf16(k_new, v_new, q)
         _check(lib().baklava_append_decode_attn(self.ctx, layer_begin, layer_count, k_new.data_ptr(),
                                                 v_new.data_ptr(), int(token_pos), q.data_ptr(), out.data_ptr(),
                                                 _stream_ptr(stream)), "baklava_append_decode_attn")
 
     def append_decode_attn_replay(self, layer_begin: int, layer_count: int, k_new, v_new, token_pos_dev, q, out,
                                   stream=None) -> None:
+        if self.mx:
+            self._expect_bf16(k_new, v_new, q)
         _check(lib().baklava_append_decode_attn_replay(self.ctx, layer_begin, layer_count, k_new.data_ptr(),
                                                        v_new.data_ptr(), token_pos_dev.data_ptr(), q.data_ptr(),
                                                        out.data_ptr(), _stream_ptr(stream)),
@@ -343,6 +355,8 @@ class Arena:
         return k, v
 
     def decode_attn(self, layer_begin: int, layer_count: int, q, out, stream=None) -> None:
+        if self.mx:
+            self._expect_bf16(q)
         _check(lib().baklava_decode_attn(self.ctx, layer_begin, layer_count, q.data_ptr(), out.data_ptr(),
                                          _stream_ptr(stream)), "baklava_decode_attn")
 

@@ -24,3 +24,22 @@ def scores(**kw):
 def test_prefill_scores_refuses(kw):
     with pytest.raises(ValueError):
         scores(**kw)
+
+
+def test_caches_in_4_bits_take_no_codes():
+    a = B.Arena.__new__(B.Arena)                          # (a context takes a GPU; the refusal comes before it is used)
+    a.torch, a.dtype, a.mx, a.ctx = torch, "mxfp4", True, None
+    row, codes, wide, out = (torch.zeros((1, 1, 2, n), dtype=t) for n, t in ((128, torch.bfloat16), (64, torch.uint8), (128, torch.float32),
+                                                                             (128, torch.float32)))
+    pos = torch.zeros((1,), dtype=torch.int32)
+    for bad in (codes, wide):
+        for k, v, q in ((bad, row, row), (row, bad, row), (row, row, bad)):
+            with pytest.raises(ValueError):
+                a.append_decode_attn(0, 1, k, v, 0, q, out)
+            with pytest.raises(ValueError):
+                a.append_decode_attn_replay(0, 1, k, v, pos, q, out)
+        for k, v in ((bad, row), (row, bad)):
+            with pytest.raises(ValueError):
+                a.append(0, 1, k, v, 0)
+        with pytest.raises(ValueError):
+            a.decode_attn(0, 1, bad, out)
