@@ -139,7 +139,7 @@ int baklava_plan_schedule(const int64_t* off_host, const int32_t* cap_host, int3
  * Device.
  *
  * Calls that only enqueue kernels on the caller's stream (safe inside a stream capture):
- * baklava_reset, baklava_append, baklava_append_prompt (its first rows are then those of the capture),
+ * baklava_reset, baklava_append, baklava_append_prompt (its rows are then those of the capture),
  * baklava_read_rows, baklava_qk_norm_rope, baklava_prompt_attn, baklava_decode_attn, baklava_append_decode_attn (its token
  * position and its capacity check are then those of the capture; baklava_append_decode_attn_replay
  * is the variant made for replay), baklava_flush_scores, baklava_compact, and the one-time passes
@@ -509,9 +509,11 @@ int baklava_prompt_attn(const baklava_rows* q, const baklava_rows* k, const bakl
  * pos0[b] + 1, ...; scores are taken from `scores`, or 0.
  * k, v rows of Hkv heads in the context's dtype (bf16 for MXFP4); n_tok HOST int32 [batch], 0 .. 2^29 each; pos0 HOST int32
  * [batch] or NULL (0); scores NULL or fp32 rows of one element, as lse above (read).
- * The host mirror of the lengths says where the rows go (see baklava_sync_lengths) and is advanced; a replay of a captured
- * call writes the rows that the capture found, and sets the same lengths.
- * Enqueues one kernel for at most 128 sequences of 512 caches on `stream`.
+ * Rows go where the lengths on the device say, also after replayed steps that the host mirror does not know of; the mirror
+ * decides on ECAPACITY and is advanced.  A cache that the device finds without room for its rows stays as it is and raises
+ * the status word that baklava_sync_lengths reports.  A captured call takes the rows that the host mirror names at its
+ * capture (see baklava_sync_lengths): every replay writes those, and sets the same lengths.
+ * Enqueues one kernel for at most 128 sequences of 512 caches on `stream`, two where a sequence has more than 8192 tokens.
  * Errors: EINVAL, ECAPACITY (some cache has no room; nothing is enqueued), EHIP.
  */
 int baklava_append_prompt(baklava_ctx* ctx, int32_t layer, const baklava_rows* k, const baklava_rows* v,

@@ -1084,7 +1084,16 @@ extern "C" int baklava_append_prompt(baklava_ctx* ctx, int32_t layer, const bakl
   p.scores = device_rows(scores, 1, 1);
   p.k_plane = ctx->d.k; p.v_plane = ctx->d.v;
   p.kv_scale = reinterpret_cast<uint8_t*>(ctx->d.kv_scale);
-  p.score = ctx->d.score; p.pos = ctx->d.pos; p.off = ctx->d.off; p.len = ctx->d.len;
+  p.score = ctx->d.score; p.pos = ctx->d.pos; p.off = ctx->d.off; p.cap = ctx->d.cap; p.len = ctx->d.len;
+  p.status = reinterpret_cast<int32_t*>(ctx->ws + ctx->plan.status);
+  // A captured call keeps the rows that it finds now, so that every replay writes the same ones.
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing((hipStream_t)stream, &capture) != hipSuccess) {
+    (void)hipGetLastError();  // (the default stream while another one is captured)
+    capture = hipStreamCaptureStatusNone;
+  }
+  p.from_len = capture == hipStreamCaptureStatusNone ? 1 : 0;
+  p.ticket = reinterpret_cast<int32_t*>(ctx->ws + ctx->plan.flush_ticket);
   p.Hkv = Hkv;
   const int32_t heads = std::min(Hkv, kPromptCaches);
   const int32_t seqs = std::min(kPromptSeqs, kPromptCaches / heads);

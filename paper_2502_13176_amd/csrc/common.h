@@ -100,7 +100,8 @@ struct DecodeParams {
   int32_t* lag_n;                  // [n_caches, kLagCalls] rows that were live at pending call s
   int32_t* lag_cnt;                // [n_caches, G] pending calls (one counter per head, all equal:
                                    // each block of the combine kernel reads and writes its own)
-  int32_t* flush_ticket;           // [n_caches * kTicketStride] work items of a flush that are done (0 at rest), or
+  int32_t* flush_ticket;           // [n_caches * kTicketStride] work items of a flush that are done (0 at rest; a prompt's tiles draw
+                                   // them too), or
                                    // null: a launch behind the flush empties the records
   const int32_t* cap;
   float* score;
@@ -206,13 +207,17 @@ struct PromptRowsParams {
   float* score;
   int32_t* pos;
   const int64_t* off;
+  const int32_t* cap;
   int32_t* len;
+  int32_t from_len;         // 1: rows go behind len (else behind start), which advances when every tile has read it:
+  int32_t* ticket;          // [n_caches * kTicketStride] tiles that have (0 at rest), or null: a launch behind this one does it
+  int32_t* status;          // raised by a cache without room
   int32_t cache0, Hkv;      // cache of sequence 0 of the launch, head 0
   int32_t head0, n_heads, seq0, tile0;  // heads, first sequence and first tile of the launch
   struct Seq {
     int32_t n, first, pos0;
   } seq[kPromptSeqs];
-  int32_t start[kPromptCaches];  // [sequence][head of the launch] live rows
+  int32_t start[kPromptCaches];  // [sequence][head of the launch] live rows, where the lengths on the device are not asked
 };
 
 struct ReadRowsParams {

@@ -22,7 +22,7 @@ __global__ __launch_bounds__(kThreads) void append_prompt_kernel(PromptRowsParam
   const PromptRowsParams::Seq q = p.seq[i];
   const int r0 = (p.tile0 + (uint32_t)blockIdx.x / (uint32_t)p.n_heads) * kTile;
   if (r0 >= q.n) return;
-  const int c = p.cache0 + i * p.Hkv + h, start = p.start[i * p.n_heads + h_rel];
+  const int c = p.cache0 + i * p.Hkv + h;
   const int tid = threadIdx.x, piece = tid % PIECES, row = r0 + tid / PIECES;
   const int e = min(r0 + kTile, q.n);
   const uint4* src_k = reinterpret_cast<const uint4*>(p.k.data) + p.k.begin(p.seq0 + i, q.first) + h * p.k.head + piece;
@@ -33,6 +33,28 @@ __global__ __launch_bounds__(kThreads) void append_prompt_kernel(PromptRowsParam
     const int64_t r = min(row + j * kRows, e - 1);
     k[j] = src_k[r * p.k.tok];
     v[j] = src_v[r * p.v.tok];
+  }
+  // Rows go behind the live ones as the device counts them: replays of captured steps move that count without the host's
+  // knowledge.  The tile that is the last of its cache to have read it advances it.
+  int start;
+  if (p.from_len) {
+    __shared__ int live;
+    if (tid == 0) live = p.len[c];
+    __syncthreads();
+    start = live;
+    if (tid == 0 && p.ticket) {
+      const int tiles = (q.n + kTile - 1) / kTile;
+      int32_t* const ticket = p.ticket + (int64_t)c * kTicketStride;
+      if (tiles == 1 || __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == tiles - 1) {
+        if (tiles > 1) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (start <= p.cap[c] - q.n) p.len[c] = start + q.n;
+        else *p.status = 1;
+      }
+    }
+    if (start > p.cap[c] - q.n) return;  // all or nothing of a prompt
+  } else {
+    start = p.start[i * p.n_heads + h_rel];
+    if (r0 == 0 && tid == 0) p.len[c] = start + q.n;
   }
   const int64_t row0 = p.off[c] + start;
 #pragma unroll
@@ -62,7 +84,16 @@ __global__ __launch_bounds__(kThreads) void append_prompt_kernel(PromptRowsParam
                                       : 0.f;
     p.pos[row0 + r] = q.pos0 + r;
   }
-  if (r0 == 0 && tid == 0) p.len[c] = start + q.n;
+}
+
+// Lengths behind rows whose tiles drew no tickets.
+__global__ __launch_bounds__(kThreads) void advance_lengths_kernel(PromptRowsParams p, int n_caches) {
+  for (int i = threadIdx.x; i < n_caches; i += kThreads) {
+    const int n = p.seq[i / p.n_heads].n, c = p.cache0 + i / p.n_heads * p.Hkv + p.head0 + i % p.n_heads;
+    if (n == 0) continue;
+    if (p.len[c] <= p.cap[c] - n) p.len[c] += n;
+    else *p.status = 1;
+  }
 }
 
 template <int PIECES, bool MX>
@@ -123,6 +154,9 @@ hipError_t launch_append_prompt(const PromptRowsParams& p_in, int pieces, bool m
   if (p_in.n_heads <= 0 || n_seq <= 0 || most <= 0) return hipSuccess;
   PromptRowsParams p = p_in;
   const int tiles = (most + kTile - 1) / kTile, per_launch = (1 << 23) / p.n_heads;  // a grid dimension holds fewer than 2^32 threads
+  // Tickets of one cache follow each other, some 15 ns apart.  us with tickets / with a launch more: 8 caches of 512 rows (8
+  // tickets each) 7.5 / 10.7, 32 of 3001 (47) 13.2 / 14.8, 8 of 32768 (512) 25.6 / 25.5, one of 65536 (1024) 15.6 / 10.3.
+  if (tiles > kMostTickets) p.ticket = nullptr;
   for (p.tile0 = 0; p.tile0 < tiles; p.tile0 += per_launch) {
     const dim3 grid((tiles - p.tile0 < per_launch ? tiles - p.tile0 : per_launch) * p.n_heads, n_seq), block(kThreads);
     if (mx && pieces == 16) append_prompt_kernel<16, true><<<grid, block, 0, s>>>(p);
@@ -132,6 +166,7 @@ hipError_t launch_append_prompt(const PromptRowsParams& p_in, int pieces, bool m
     else if (pieces == 8) append_prompt_kernel<8, false><<<grid, block, 0, s>>>(p);
     else return hipErrorInvalidValue;
   }
+  if (p.from_len && !p.ticket) advance_lengths_kernel<<<dim3(1), dim3(kThreads), 0, s>>>(p, n_seq * p.n_heads);
   return hipGetLastError();
 }
 
