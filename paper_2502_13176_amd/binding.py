@@ -533,6 +533,14 @@ def _ints(values):
     return a, a.buffer_info()[0], sum(a), max(a, default=0)
 
 
+def _refuse_grad(torch, *tensors) -> None:
+    """The library has no backward passes: a result without a graph would end a gradient silently."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("no gradient is computed here: call under torch.no_grad() or with detached tensors")
+
+
 class _Rows:
     """Up to five baklava_rows in one array of 64-bit words; each is handed over by its address, which add() returns.
 
@@ -600,8 +608,9 @@ def prompt_attn(q, k, v, lens: Sequence[int], kv_lens: Optional[Sequence[int]] =
     """baklava_prompt_attn on torch device tensors (bf16): q [tokens, Hq, D], k and v [keys, Hkv, D] (the sequences in a row)
     or q [batch, Hq, T, D], k and v [batch, Hkv, T', D] (padded); lens query tokens and kv_lens keys of every sequence.
     Returns out (like q; places past a sequence's length are not written), and with want_lse or lse given also lse (fp32
-    [Hq, tokens] or [batch, Hq, T])."""
+    [Hq, tokens] or [batch, Hq, T]).  No gradient: tensors that require one are refused outside torch.no_grad()."""
     import torch
+    _refuse_grad(torch, q, k, v)
     q_shape, k_shape = q.shape, k.shape
     if len(q_shape) not in (3, 4) or len(k_shape) not in (3, 4) or k_shape != v.shape:
         raise ValueError("q, k, v of three or four dimensions expected, k and v alike")
@@ -636,8 +645,10 @@ def qk_norm_rope(q, k, pos, inv_freq: Sequence[float], q_weight=None, k_weight=N
     None), bf16 or fp32, of any strides with contiguous rows; pos int32 [tokens] or [axes, tokens] ([axes, batch, T] in any
     shape of as many values); inv_freq one frequency per pair of rotated elements (empty: no rotation, pos is not looked at).
     The axis of every pair is given by axis_of_pair, or by sections: pairs of axis 0, of axis 1, ...  Weights [D] or None (not
-    normed).  q_out, k_out may be q and k.  Returns (q_out, k_out)."""
+    normed).  q_out, k_out may be q and k.  Returns (q_out, k_out).  No gradient: tensors that require one are refused outside
+    torch.no_grad()."""
     import torch
+    _refuse_grad(torch, q, k, q_weight, k_weight)
     t0 = q if q is not None else k
     if t0 is None or (q is not None and k is not None and q.dim() != k.dim()):
         raise ValueError("q or k of three or four dimensions expected, both alike")

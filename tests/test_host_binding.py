@@ -43,3 +43,26 @@ def test_caches_in_4_bits_take_no_codes():
                 a.append(0, 1, k, v, 0)
         with pytest.raises(ValueError):
             a.decode_attn(0, 1, bad, out)
+
+
+@pytest.mark.parametrize("which", range(3))
+def test_prompt_attn_refuses_tensors_that_require_a_gradient(which):
+    t = [torch.zeros((3, 2, 64), dtype=torch.bfloat16) for _ in range(3)]
+    t[which].requires_grad_()
+    with pytest.raises(ValueError, match="gradient"):
+        B.prompt_attn(*t, [3])
+    with torch.no_grad(), pytest.raises(ValueError, match="GPU"):  # refused for where it is alone
+        B.prompt_attn(*t, [3])
+    with pytest.raises(ValueError, match="GPU"):
+        B.prompt_attn(*(x.detach() for x in t), [3])
+
+
+@pytest.mark.parametrize("which", range(4))
+def test_qk_norm_rope_refuses_tensors_that_require_a_gradient(which):
+    t = [torch.zeros(s) for s in ((3, 2, 64), (3, 1, 64), (64,), (64,))]
+    t[which].requires_grad_()
+    pos = torch.zeros((3,), dtype=torch.int32)
+    with pytest.raises(ValueError, match="gradient"):
+        B.qk_norm_rope(t[0], t[1], pos, [1.0] * 32, q_weight=t[2], k_weight=t[3])
+    with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
+        B.qk_norm_rope(t[0], t[1], pos, [1.0] * 32, q_weight=t[2], k_weight=t[3])
