@@ -20,10 +20,12 @@ namespace baklava {
 namespace {
 
 constexpr int kThreads = 256;
-// Bytes of a workgroup's rows, about, from 4096 tokens on (shorter launches take a token each, to fill the chip).  What is on
-// its way together must not lie far apart, and a workgroup must have some to hide its angles behind.  us, 12 / 20 / 32 KiB:
-// 32768 bf16 tokens of 40 heads of 128 136 / 119 / 119, 30000 of 24 heads of 64 33.0 / 33.5 / 37.3; fp32, whose rows take half
-// the arithmetic for a byte, 12000 of 24 heads of 128 48.4 / 48.2 / 54.2, 20000 of 16 heads of 64 30.3 / 37.9 / 46.0.
+// Bytes of a workgroup's rows, about, from 4096 tokens of all sequences on (smaller launches take a token each, to fill the chip);
+// a workgroup's tokens are of one sequence.  us, a token each / as here: 64 sequences of 2048 bf16 tokens of 14 heads of 64 230 /
+// 76, of 2 heads 289 / 28, 16 of 2048 tokens of 40 heads of 128 142 / 127, 1024 of 17 tokens of 14 heads of 64 34.8 / 16.6.  What
+// is on its way together must not lie far apart, and a workgroup must have some to hide its angles behind.  us, 12 / 20 / 32 KiB:
+// 32768 bf16 tokens of 40 heads of 128 136 / 119 / 119, 30000 of 24 heads of 64 33.0 / 33.5 / 37.3; fp32, whose rows take half the
+// arithmetic for a byte, 12000 of 24 heads of 128 48.4 / 48.2 / 54.2, 20000 of 16 heads of 64 30.3 / 37.9 / 46.0.
 constexpr int kWgBytes16 = 20 * 1024, kWgBytes32 = 12 * 1024;
 
 // Sum over four or eight neighbouring lanes, every one of them receiving it.
@@ -215,7 +217,7 @@ hipError_t launch_qk_norm_rope(const RopeParams& p_in, int dtype, int D, bool in
   if (p_in.n_seq <= 0 || p_in.T <= 0 || p_in.Hq + p_in.Hkv <= 0) return hipSuccess;
   RopeParams p = p_in;
   const int token_bytes = (p.Hq + p.Hkv) * D * (dtype == 0 ? 2 : 4);
-  p.tok = p.T < 4096 ? 1 : std::max(1, std::min(16, (dtype == 0 ? kWgBytes16 : kWgBytes32) / token_bytes));
+  p.tok = (int64_t)p.n_seq * p.T < 4096 ? 1 : std::max(1, std::min({16, p.T, (dtype == 0 ? kWgBytes16 : kWgBytes32) / token_bytes}));
   for (p.seq0 = 0; p.seq0 < p.n_seq; p.seq0 += 65535) {  // a grid's second dimension holds no more
     const dim3 grid((p.T + p.tok - 1) / p.tok, std::min(65535, p.n_seq - p.seq0));
     if (dtype == 0) {

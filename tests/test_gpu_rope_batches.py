@@ -1,0 +1,50 @@
+"""GPU: baklava_qk_norm_rope over batches of sequences, as right and as fast as over the same tokens packed."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2502_13176_amd import binding as B
+from test_gpu_rope import run
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,kw", [(1366, dict()), (2053, dict(interleaved=True)), (1500, dict(rot=22)), (1367, dict(in_place=True))])
+def test_several_tokens_of_a_workgroup_in_a_batch(dtype, n, kw):
+    """Three sequences of fewer than 4096 tokens that have more together."""
+    run(dtype, n, 2, 1, 64, axes=2, layout="batch", **kw)
+
+
+def test_sequences_shorter_than_a_workgroup_takes_tokens():
+    x = torch.randn((700, 2, 7, 64)).bfloat16().cuda()
+    pos = torch.randint(0, 9000, (700 * 7,), dtype=torch.int32).cuda()
+    f = 10000.0 ** (-np.arange(32) / 32)
+    got = B.qk_norm_rope(x, None, pos, f)[0]
+    for i in (0, 1, 350, 699):
+        assert torch.equal(got[i:i + 1], B.qk_norm_rope(x[i:i + 1], None, pos[7 * i:7 * i + 7], f)[0])
+
+
+def us(call):
+    call()
+    torch.cuda.synchronize()
+    best = float("inf")
+    for _ in range(5):
+        a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        a.record()
+        for _ in range(10):
+            call()
+        b.record()
+        torch.cuda.synchronize()
+        best = min(best, a.elapsed_time(b) * 100)
+    return best
+
+
+def test_a_batch_takes_no_token_alone():
+    """64 sequences of 2048 tokens, two heads: 10 times the packed call's time with a token for each workgroup, 1.0 with several."""
+    x = torch.randn((64, 2, 2048, 64)).bfloat16().cuda()
+    out, pos, f = torch.empty_like(x), torch.arange(64 * 2048, dtype=torch.int32).cuda(), 10000.0 ** (-np.arange(32) / 32)
+    rows, rows_out = (t.view(64 * 2048, 2, 64) for t in (x, out))
+    batch = us(lambda: B.qk_norm_rope(x, None, pos, f, q_out=out))
+    packed = us(lambda: B.qk_norm_rope(rows, None, pos, f, q_out=rows_out))
+    assert batch < 4 * packed, (batch, packed)
