@@ -475,7 +475,8 @@ typedef struct {
  * q_weight, k_weight DEVICE [D] in `dtype`, 16-byte aligned, or NULL: these rows are not normed.
  * pos DEVICE int32 [n_axes, n_seq * T]; axis_of_pair HOST uint8 [rot_dim/2], each < n_axes, or NULL (axis 0);
  * inv_freq HOST double [rot_dim/2], finite.  rot_dim even, 0 .. D; 0: no rotation, the three are not looked at.
- * D in {64, 128}; n_axes 1 .. 8; eps >= 0.  Enqueues one kernel on `stream`; deterministic.
+ * D in {64, 128}; n_axes 1 .. 8; eps >= 0.  Enqueues one kernel on `stream` (more beyond 65535 sequences or 2^24 - 1 tokens of
+ * one); deterministic.
  * Errors: EINVAL (null, misaligned, bad shape, stride, dtype, eps or frequency), EHIP.
  */
 int baklava_qk_norm_rope(const baklava_rows* q, const baklava_rows* k, int32_t n_seq, int32_t T, int32_t Hq, int32_t Hkv,

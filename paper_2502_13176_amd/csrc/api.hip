@@ -32,7 +32,7 @@ constexpr int kWholeItemsPerCu = 5;       // launches over many caches aim at th
 constexpr int kShortestRun = 64;          // where those would leave compute units idle (see build_schedule)
 constexpr int kMostFillItems = 256;       // most work items such short runs are cut for: one per compute unit (sizes the workspace)
 constexpr int32_t kMostPromptTokens = 1 << 29;      // of a sequence
-constexpr int32_t kMostRopeTokens = 1 << 26;        // of a sequence: a grid dimension holds fewer than 2^32 threads
+constexpr int32_t kMostRopeTokens = 1 << 26;        // of a sequence
 constexpr int64_t kMostTokenStride = 1 << 24;       // offsets inside a tile of rows stay below 2^32 bytes
 constexpr int kMaxChunk = 1 << 22; // row offsets inside a work item stay below 2^32 bytes
 inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }

@@ -179,7 +179,7 @@ struct RopeParams {
   int32_t n_seq, T, Hq, Hkv;
   int32_t rot;              // elements that are rotated
   int32_t tok;              // tokens per workgroup
-  int32_t seq0;             // first sequence of the launch
+  int32_t seq0, tok0;       // first sequence, and first token of each, of the launch
   double turns[64];         // frequency of every pair, in turns per position
   uint8_t axis[64];         // its axis
 };

@@ -20,6 +20,7 @@ namespace baklava {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kMostWgs = (1 << 24) - 1;  // a grid's first dimension holds fewer than 2^32 threads
 // Bytes of a workgroup's rows, about, from 4096 tokens of all sequences on (smaller launches take a token each, to fill the chip);
 // a workgroup's tokens are of one sequence.  us, a token each / as here: 64 sequences of 2048 bf16 tokens of 14 heads of 64 230 /
 // 76, of 2 heads 289 / 28, 16 of 2048 tokens of 40 heads of 128 142 / 127, 1024 of 17 tokens of 14 heads of 64 34.8 / 16.6.  What
@@ -93,7 +94,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(RopeParams p) {
   constexpr int kLanes = D / 16, kPairs = D / 2, kRows = kThreads / kLanes;  // rows at a time
   extern __shared__ __attribute__((aligned(16))) float2 turn[];              // [tok][kPairs] (cos, sin)
   const int tid = threadIdx.x;
-  const int b = p.seq0 + blockIdx.y, tok0 = blockIdx.x * p.tok, n_here = min(p.tok, p.T - tok0);
+  const int b = p.seq0 + blockIdx.y, tok0 = p.tok0 + blockIdx.x * p.tok, n_here = min(p.tok, p.T - tok0);
   const int64_t n_tok = (int64_t)p.n_seq * p.T;
   const int32_t* pos = p.pos + (int64_t)b * p.T + tok0;
   const int sub = tid % kLanes;
@@ -218,14 +219,18 @@ hipError_t launch_qk_norm_rope(const RopeParams& p_in, int dtype, int D, bool in
   RopeParams p = p_in;
   const int token_bytes = (p.Hq + p.Hkv) * D * (dtype == 0 ? 2 : 4);
   p.tok = (int64_t)p.n_seq * p.T < 4096 ? 1 : std::max(1, std::min({16, p.T, (dtype == 0 ? kWgBytes16 : kWgBytes32) / token_bytes}));
-  for (p.seq0 = 0; p.seq0 < p.n_seq; p.seq0 += 65535) {  // a grid's second dimension holds no more
-    const dim3 grid((p.T + p.tok - 1) / p.tok, std::min(65535, p.n_seq - p.seq0));
-    if (dtype == 0) {
-      if (D == 128) launch<uint16_t, 128>(p, interleaved, grid, s);
-      else launch<uint16_t, 64>(p, interleaved, grid, s);
-    } else {
-      if (D == 128) launch<float, 128>(p, interleaved, grid, s);
-      else launch<float, 64>(p, interleaved, grid, s);
+  const int most_tok = kMostWgs * p.tok;
+  for (int64_t seq0 = 0; seq0 < p.n_seq; seq0 += 65535) {  // a grid's second dimension holds no more
+    p.seq0 = (int32_t)seq0;
+    for (p.tok0 = 0; p.tok0 < p.T; p.tok0 += most_tok) {
+      const dim3 grid((std::min(most_tok, p.T - p.tok0) + p.tok - 1) / p.tok, std::min(65535, p.n_seq - p.seq0));
+      if (dtype == 0) {
+        if (D == 128) launch<uint16_t, 128>(p, interleaved, grid, s);
+        else launch<uint16_t, 64>(p, interleaved, grid, s);
+      } else {
+        if (D == 128) launch<float, 128>(p, interleaved, grid, s);
+        else launch<float, 64>(p, interleaved, grid, s);
+      }
     }
   }
   return hipGetLastError();

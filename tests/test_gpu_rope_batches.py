@@ -48,3 +48,30 @@ def test_a_batch_takes_no_token_alone():
     batch = us(lambda: B.qk_norm_rope(x, None, pos, f, q_out=out))
     packed = us(lambda: B.qk_norm_rope(rows, None, pos, f, q_out=rows_out))
     assert batch < 4 * packed, (batch, packed)
+
+
+def test_more_tokens_than_a_launch_has_workgroups():
+    """Rows so wide that every token takes a workgroup: 2^24 + 3 tokens of 25 fp32 heads, 107 GB written, from one row read again and again."""
+    torch.cuda.empty_cache()
+    n, H, D = (1 << 24) + 3, 25, 64
+    one = torch.randn((1, H, D)).cuda()
+    out = torch.full((n, H, D), float("nan"), device="cuda")
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    f, w = 10000.0 ** (-np.arange(32) / 32), torch.ones(D, device="cuda")
+    B.qk_norm_rope(one.expand(n, H, D), None, pos, f, q_weight=w, q_out=out)
+    at = torch.tensor([0, 1, 255, (1 << 23) + 1, (1 << 24) - 2, (1 << 24) - 1, 1 << 24, n - 1]).cuda()
+    want = B.qk_norm_rope(one.expand(len(at), H, D), None, pos[at].contiguous(), f, q_weight=w)[0]
+    assert torch.equal(out[at], want)
+    for i in range(0, n, 1 << 20):                        # every row is written
+        assert not torch.isnan(out[i:i + (1 << 20), :, 0]).any()
+    del out
+    torch.cuda.empty_cache()
+
+
+def test_more_sequences_than_a_launch_holds():
+    x = torch.randn((65535 + 9, 1, 2, 64)).bfloat16().cuda()
+    pos = torch.randint(0, 9000, (x.shape[0] * 2,), dtype=torch.int32).cuda()
+    f = 10000.0 ** (-np.arange(32) / 32)
+    got = B.qk_norm_rope(x, None, pos, f)[0]
+    rows = B.qk_norm_rope(x.view(-1, 1, 64), None, pos, f)[0]
+    assert torch.equal(got.view(-1, 1, 64), rows)
