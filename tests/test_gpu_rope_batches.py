@@ -75,3 +75,12 @@ def test_more_sequences_than_a_launch_holds():
     got = B.qk_norm_rope(x, None, pos, f)[0]
     rows = B.qk_norm_rope(x.view(-1, 1, 64), None, pos, f)[0]
     assert torch.equal(got.view(-1, 1, 64), rows)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,Hq,Hkv", [(128, 6, 2), (128, 1, 1), (64, 7, 1)])
+@pytest.mark.parametrize("kw", [dict(axes=3), dict(interleaved=True), dict(rot=24), dict(rot=22), dict(rot=24, interleaved=True), dict(layout="heads"),
+                                dict(in_place=True), dict(in_place=True, rot=22), dict(in_place=True, layout="heads", interleaved=True)])
+def test_several_tokens_of_a_workgroup(dtype, D, Hq, Hkv, kw):
+    """4103 tokens: the last workgroup has fewer than the others (of 3 to 16, by the size of a token's rows)."""
+    run(dtype, 4103, Hq, Hkv, D, far=100000, **kw)
