@@ -74,8 +74,9 @@ bool keeps_records(const baklava_desc* d) { return d->dtype == BAKLAVA_MXFP4 || 
 // Bytes of a row of queries (and of new rows), and of a cached row.
 int32_t query_row_bytes(const baklava_desc* d) { return d->D * (d->dtype == BAKLAVA_F32 ? 4 : 2); }
 int32_t cache_row_bytes(const baklava_desc* d) { return d->dtype == BAKLAVA_MXFP4 ? d->D / 2 : query_row_bytes(d); }
-// Rows of a cache: the offsets of 4-bit rows inside a work item are held in 32 bits (with 64 the attention kernel has no register
-// left and takes 2% longer), and an option may make an item of a whole cache.
+// Rows of a cache: those of 4 bits are limited so that a plane's codes of one cache end within 2^31 bytes.  (The kernels address
+// a work item's rows with 32-bit offsets from its first, with 64 the attention kernel has no register left and takes 2%
+// longer; a work item has 2^22 rows at most.)
 int32_t most_rows(const baklava_desc* d) { return d->dtype == BAKLAVA_MXFP4 ? 1 << 25 : INT32_MAX; }
 
 WorkspacePlan plan_workspace(const baklava_desc* d, const int32_t* cap) {
@@ -937,8 +938,8 @@ extern "C" int baklava_prefill_scores(const void* q, const void* k, const float*
 
 namespace {
 
-// Whether rows of `heads` heads can be addressed: `unit` elements are a 16-byte piece (or one element), `wide` bytes an
-// element.  Strides that no row index multiplies are not looked at.
+// Whether rows of `heads` heads can be addressed: `unit` elements are a 16-byte piece (or one element), `align` bytes the
+// alignment of the first.  Strides that no row index multiplies are not looked at.
 bool rows_ok(const baklava_rows* r, int32_t n_seq, int64_t most_tokens, int32_t heads, int unit, int align) {
   if (!r || !r->data || ((uintptr_t)r->data & (align - 1))) return false;
   if (r->seq_stride < 0 || r->token_stride < 0 || r->head_stride < 0) return false;
