@@ -638,6 +638,19 @@ def prompt_attn(q, k, v, lens: Sequence[int], kv_lens: Optional[Sequence[int]] =
     return (out, lse) if lse is not None else out
 
 
+def _axes(sections, axis_of_pair, n_freq: int, axes: int) -> Optional[bytes]:
+    """The axis of every pair, a byte each; None: axis 0 for all."""
+    if sections is not None:
+        if axis_of_pair is not None or sum(sections) != n_freq or len(sections) > axes or min(sections, default=0) < 0:
+            raise ValueError("sections must add up to the number of pairs, at most one for each axis")
+        return b"".join([bytes((a,)) * n for a, n in enumerate(sections)]) if len(sections) > 1 else None
+    if axis_of_pair is not None:
+        if len(axis_of_pair) != n_freq or any(not 0 <= a < axes for a in axis_of_pair):
+            raise ValueError("axis_of_pair must name an axis for every pair")
+        return bytes(list(axis_of_pair))  # (an array's own bytes are those of its words)
+    return None
+
+
 def qk_norm_rope(q, k, pos, inv_freq: Sequence[float], q_weight=None, k_weight=None, eps: float = 1e-6,
                  sections: Optional[Sequence[int]] = None, axis_of_pair: Optional[Sequence[int]] = None,
                  interleaved: bool = False, q_out=None, k_out=None, stream=None):
@@ -675,15 +688,7 @@ def qk_norm_rope(q, k, pos, inv_freq: Sequence[float], q_weight=None, k_weight=N
             raise ValueError("pos must be a contiguous int32 tensor with one value per axis and token")
         rows.on_device(pos, "pos")
         axes, pos_at = n_pos // tokens, pos.data_ptr()
-    axis = None
-    if sections is not None:
-        if axis_of_pair is not None or sum(sections) != n_freq or len(sections) > axes or min(sections, default=0) < 0:
-            raise ValueError("sections must add up to the number of pairs, at most one for each axis")
-        axis = b"".join([bytes((a,)) * n for a, n in enumerate(sections)]) if len(sections) > 1 else None
-    elif axis_of_pair is not None:
-        if len(axis_of_pair) != n_freq or any(not 0 <= a < axes for a in axis_of_pair):
-            raise ValueError("axis_of_pair must name an axis for every pair")
-        axis = bytes(axis_of_pair)
+    axis = _axes(sections, axis_of_pair, n_freq, axes)
     in_at, out_at, w_at, outs, heads = [None, None], [None, None], [None, None], [None, None], [0, 0]
     for i, (t, name, w, o) in enumerate(((q, "q", q_weight, q_out), (k, "k", k_weight, k_out))):
         if t is None:

@@ -1,4 +1,7 @@
 """What the binding refuses before it calls the library, without a GPU."""
+import array
+
+import numpy as np
 import pytest
 import torch
 
@@ -66,3 +69,14 @@ def test_qk_norm_rope_refuses_tensors_that_require_a_gradient(which):
         B.qk_norm_rope(t[0], t[1], pos, [1.0] * 32, q_weight=t[2], k_weight=t[3])
     with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
         B.qk_norm_rope(t[0], t[1], pos, [1.0] * 32, q_weight=t[2], k_weight=t[3])
+
+
+@pytest.mark.parametrize("make", [list, tuple, np.array, lambda a: np.array(a, dtype=np.uint8), lambda a: array.array("i", a), torch.tensor, bytes])
+def test_axes_of_pairs_in_any_sequence(make):
+    axis = [0, 2, 1, 1, 0]
+    assert B._axes(None, make(axis), 5, 3) == bytes(axis)
+    assert B._axes(make([2, 0, 3]), None, 5, 3) == bytes([0, 0, 2, 2, 2])
+    assert B._axes(make([5]), None, 5, 3) is None and B._axes(None, None, 5, 3) is None
+    for sections, pairs in (([2, 2], None), ([2, 1, 1, 1], None), ([1, 4], axis), (None, axis[:4]), (None, [0, 3, 0, 0, 0])):
+        with pytest.raises(ValueError):
+            B._axes(make(sections) if sections else None, make(pairs) if pairs else None, 5, 3)
