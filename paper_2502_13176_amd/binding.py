@@ -627,7 +627,7 @@ def prompt_attn(q, k, v, lens: Sequence[int], kv_lens: Optional[Sequence[int]] =
     at = [rows.add(q, "q", n_seq, total, most, Hq, D, dt), rows.add(k, "k", n_seq, k_total, k_most, Hkv, D, dt),
           rows.add(v, "v", n_seq, k_total, k_most, Hkv, D, dt)]
     if out is None:
-        out = _empty_on(stream, q.new_empty, q_shape)
+        out = q.new_empty(q_shape) if stream is None else _empty_on(stream, q.new_empty, q_shape)
     if lse is None and want_lse:
         lse = _empty_on(stream, q.new_empty, (Hq, q_shape[0]) if len(q_shape) == 3 else q_shape[:3], dtype=torch.float32)
     at.append(rows.add(out, "out", n_seq, total, most, Hq, D, dt))
@@ -703,7 +703,7 @@ def qk_norm_rope(q, k, pos, inv_freq: Sequence[float], q_weight=None, k_weight=N
             rows.on_device(w, f"{name}_weight")
             w_at[i] = w.data_ptr()
         if o is None:
-            o = _empty_on(stream, t.new_empty, t.shape)
+            o = t.new_empty(t.shape) if stream is None else _empty_on(stream, t.new_empty, t.shape)
         elif o.shape != t.shape:
             raise ValueError(f"{name}_out must have the shape of {name}")
         out_at[i], outs[i] = rows.add(o, f"{name}_out", n_seq, tokens, T, h, D, dtype), o
