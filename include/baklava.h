@@ -308,7 +308,7 @@ int baklava_append_decode_attn_replay(baklava_ctx* ctx, int32_t layer_begin, int
 
 /*
  * Reads the device's length table back into the host mirror and returns ECAPACITY if, since the
- * last such call, a fused append found a cache full (the status word is then cleared).
+ * last such call, a fused append found a cache full, or a prompt one without room (the status word is then cleared).
  * Synchronises `stream`; not to be captured.
  */
 int baklava_sync_lengths(baklava_ctx* ctx, void* stream);

@@ -24,8 +24,8 @@ constexpr int kLagRows = 32;   // packed query rows of a cache's record of pendi
 constexpr int kLagCalls = 8;   // most calls such a record holds
 constexpr int kTicketStride = 32;  // words from one cache's flush ticket to the next: a cache line each
 constexpr int kMostTickets = 128;  // most work items of a cache that draw them
-// Eviction move: destination rows per tile by 16-byte pieces per row (128 KiB of K and V), threads per workgroup, caches
-// per launch
+// Eviction move: destination rows per tile by 16-byte pieces per row (128 KiB of K and V; of 4-bit rows, four pieces or two, 64
+// or 32 KiB: a tile has a thread for every row's score), threads per workgroup, caches per launch
 constexpr int kMoveRowsMin = 128;
 constexpr int move_rows(int pieces) { return pieces > 16 ? kMoveRowsMin : pieces > 8 ? 2 * kMoveRowsMin : 4 * kMoveRowsMin; }
 // most rows of a cache that one workgroup moves (half a tile, or a whole one of 512-byte rows)

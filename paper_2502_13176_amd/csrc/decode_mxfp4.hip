@@ -17,8 +17,11 @@
 // average, tracked: 20 us of which 12 are the bytes at 7.06 TB/s; calls of different sizes lie on 7 to 10 us + bytes / 6.57 TB/s.
 // The merge of the split caches is a kernel of its own (some 3 us); inside this one, by the last workgroup of a cache to
 // arrive, it took as long.  Recorded calls cost a pass over K in one call out of `lag_batch`; the flush of eight calls of four
-// heads over 2.5 million rows takes 45 us (27 for the bytes), bound by issue: per 32 rows 32 conversions, 16 products and 16
-// exponentials a lane, so that two slabs requested ahead instead of one make no difference.
+// heads over 2.5 million rows takes 45 us (27 for the bytes).  Nothing in it is saturated (vector ALUs 58% of the cycles in which
+// a compute unit is busy, matrix pipe 23%): a slab is a chain of requests, products, exponentials, exchanges through LDS and a
+// write to the ring, and a wavefront waits for data half of its time and for its turn to issue 30%.  Two slabs requested ahead
+// instead of one make no difference.  The attention kernel is no different: vector ALUs 46% (four heads, one workgroup per compute
+// unit) to 58% (seven heads, two), matrix pipe 23 to 28%, LDS 35 to 42%, two fifths of that bank conflicts.
 #include "common.h"
 #include "decode_tail.h"
 #include "mxfp4.h"

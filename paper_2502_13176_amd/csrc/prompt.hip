@@ -19,12 +19,12 @@
 // at the end: in the main loop the test alone cost registers that went to scratch memory (8 prompts of 4096, 28 heads, 1229 / 1005
 // us).
 //
-// One prompt of 16384, 32 heads of 128: 1.97 to 2.05 ms by the box, 1.07 to 1.12 PFLOP/s, where a product of two matrices of 16384^2
-// reaches 1.28 to 1.30.  The power of the products bounds it: the matrix cores are busy 63% of the time at some 1.6 GHz, and
-// orders of instructions or waves' priorities make no difference.  (64 tokens per wavefront, one wavefront per SIMD, whose
-// operands from LDS serve twice as many products: 728 TFLOP/s, nothing runs beside a wavefront's exponentials.)  Heads of 64:
-// 0.93 PFLOP/s, bound by the vector ALUs, whose exponentials stand beside half the products.  8 prompts of 128 to 8192 tokens,
-// 28 heads, 2.35 ms.
+// One prompt of 16384, 32 heads of 128: 1.97 to 2.05 ms by the box, 1.07 to 1.12 PFLOP/s, where a product of two matrices of
+// 16384^2 reaches 1.28 to 1.30.  The power of the products bounds it: the matrix cores are busy 63% of the time at some 1.6 GHz,
+// and orders of instructions or waves' priorities make no difference.  (64 tokens per wavefront, one wavefront per SIMD, whose
+// operands from LDS serve twice as many products: 728 TFLOP/s, nothing runs beside a wavefront's exponentials.)  Heads of 64: 0.94
+// to 0.97 PFLOP/s (1.14 to 1.17 ms), bound by the vector ALUs, whose exponentials stand beside half the products.  8 prompts of 128
+// to 8192 tokens, 28 heads, 2.35 ms.
 #include "common.h"
 
 namespace baklava {
@@ -394,7 +394,8 @@ void launch(const PromptParams& p, int tile_tokens, unsigned grid, hipStream_t s
 // A call that would leave compute units idle, or give each no more than one workgroup of 128 tokens, whose chain of tiles it then
 // waits for, takes workgroups of 64 tokens that share their keys.  us, 128 / 64 tokens, 32 heads of 128: one prompt of 512
 // tokens 15.9 / 12.4, of 1024 (one workgroup for each) 24.4 / 20.7, 4 of 500 (two) 23.7 / 28.9, one of 2048 47.4 / 52.1; 8 heads,
-// one of 4096 75.6 / 57.6, of 8192 156 / 161.
+// one of 4096 75.6 / 57.6, of 8192 156 / 161.  Keys are not split over workgroups: few tokens behind many keys take as long as their
+// chain of key tiles, 1 to 128 tokens of 32 heads behind 32768 keys 345 to 370 us, where the keys and values are read in 19.
 int prompt_tile_tokens(int64_t n_tiles128, int n_cus) { return n_tiles128 <= n_cus ? 16 * kWaves : 32 * kWaves; }
 
 hipError_t launch_prompt_attn(const PromptParams& p_in, int D, int tile_tokens, int n_tiles, int n_cus, hipStream_t s) {

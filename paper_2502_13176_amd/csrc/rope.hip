@@ -201,7 +201,8 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(RopeParams p) {
   if (p.Hq > 0 && p.Hkv > 0) rows(side(p.k, p.k_out, p.k_weight, p.Hkv), false);
 }
 
-// Runs of 16 bytes where halves are made of them, of four 16-bit elements where their length is a multiple of four.
+// Runs of 16 bytes where halves are made of them, of four 16-bit elements where their length is a multiple of four, else element by
+// element: 12000 bf16 tokens of 24 heads of 128, halves of 64 / 12 / 11 pairs 25.3 / 33.2 / 129 us, fp32 43.7 / 56.1 / 193.
 template <typename T, int D>
 void launch(const RopeParams& p, bool inter, dim3 grid, hipStream_t s) {
   constexpr int kRun = 16 / sizeof(T);

@@ -2,8 +2,9 @@
 //
 // Both move rows, so HBM bounds them: a workgroup takes kTile rows of one cache, requests all of them, whole rows at a time, and
 // stores them (rounded to 4 bits on the way, see mxfp4.h).  Read and written together, behind a projection's output that the
-// last-level cache may hold in part: 8 x 32768 bf16 rows of 128 elements into 4 bits 23 us, 7.4 TB/s, of 16 bits 36 us, 7.5;
-// back out of 4 bits 25 us, 6.7 TB/s.  (A loop that requested rows four at a time, tiles in front of heads, took 35 us.)
+// last-level cache may hold in part, us a call: 8 x 32768 bf16 rows of 128 elements into 4 bits 25 (2 of them the launch for
+// the lengths), 6.8 TB/s, of 16 bits 39, 6.9; back out of 4 bits 25, 6.7 TB/s.  (A loop that requested rows four at a
+// time, tiles in front of heads, took 35 us.)
 #include "common.h"
 #include "mxfp4.h"
 
