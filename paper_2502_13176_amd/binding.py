@@ -237,6 +237,7 @@ class Arena:
         dev = self.device
         self.k = torch.zeros((self.total_tokens, D // 2 if mx else D), dtype=tdt, device=dev)
         self.v = torch.zeros_like(self.k)
+        self.gpu = self.k.get_device()
         self.kv_scale = torch.full((self.total_tokens, D // 16), 2, dtype=torch.uint8, device=dev) if mx else None
         self.score = torch.zeros((self.total_tokens,), dtype=torch.float32, device=dev)
         self.pos = torch.zeros((self.total_tokens,), dtype=torch.int32, device=dev)
@@ -335,6 +336,8 @@ class Arena:
         n, n_at, total, most = _ints(lens)
         dt = self.torch.bfloat16 if self.dtype in ("bf16", "mxfp4") else self.torch.float32
         rows = _Rows(self.torch)
+        if rows.device != self.gpu:
+            raise ValueError("the arena's GPU must be the current one")
         k_at = rows.add(k, "k", self.batch, total, most, self.Hkv, self.D, dt)
         v_at = rows.add(v, "v", self.batch, total, most, self.Hkv, self.D, dt)
         s_at = rows.add_values(scores, "scores", self.batch, total, most, self.Hkv) if scores is not None else None
@@ -346,6 +349,8 @@ class Arena:
         """baklava_read_rows: the last n rows of every cache of the range as values, (k, v) [caches, n, D]."""
         if n < 1 or layer_count < 1:
             raise ValueError("at least one row of one layer expected")
+        if stream is None and _current_device() != self.gpu:
+            raise ValueError("the arena's GPU must be the current one, or a stream of it be given")
         dt = self.torch.bfloat16 if self.dtype in ("bf16", "mxfp4") else self.torch.float32
         shape = (layer_count * self.batch * self.Hkv, n, self.D)
         k, v = (_empty_on(stream, self.torch.empty, shape, dtype=dt, device=self.device) for _ in range(2))

@@ -80,3 +80,16 @@ def test_axes_of_pairs_in_any_sequence(make):
     for sections, pairs in (([2, 2], None), ([2, 1, 1, 1], None), ([1, 4], axis), (None, axis[:4]), (None, [0, 3, 0, 0, 0])):
         with pytest.raises(ValueError):
             B._axes(make(sections) if sections else None, make(pairs) if pairs else None, 5, 3)
+
+
+def test_rows_of_an_arena_on_another_gpu(monkeypatch):
+    a = B.Arena.__new__(B.Arena)
+    a.torch, a.dtype, a.mx, a.ctx, a.gpu, a.device = torch, "bf16", False, None, 1, torch.device("cpu")
+    a.L, a.batch, a.Hkv, a.D = 1, 1, 2, 64
+    monkeypatch.setattr(B, "_current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
+    k = torch.zeros((3, 2, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="arena"):
+        a.append_prompt(0, k, k, [3])
+    with pytest.raises(ValueError, match="arena"):
+        a.read_rows(0, 1, 1)
