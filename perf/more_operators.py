@@ -34,11 +34,11 @@ def listed():
         # the largest: contexts of 131072, trees of 64 nodes, seven query heads to a cache
         dict(name="tree_long_n64", kind="tree", store="bf16", L=1, Hq=28, Hkv=4, D=128, batch=4, N=64, shape="tree", ragged=False, ctx=131072, keep=30, sigma=1.0),
         # one user, a greedy chain (latency)
-        dict(name="verify_greedy_b1", kind="verify", dtype="bf16", batch=1, N=5, V=32000, shape="chain", ragged=False, drafts=False, temp="greedy", path=3),
+        dict(name="verify_greedy_b1", kind="verify", dtype="bf16", batch=1, N=5, V=32000, shape="chain", ragged=False, drafts=False, temp="greedy", path=2),
         # a serving batch, chains drawn from a draft model, fp32 logits, odd vocabulary
-        dict(name="verify_drafts_b16", kind="verify", dtype="f32", batch=16, N=6, V=100003, shape="chain", ragged=False, drafts=True, temp="one", path=3),
+        dict(name="verify_drafts_b16", kind="verify", dtype="f32", batch=16, N=6, V=100003, shape="chain", ragged=False, drafts=True, temp="one", path=4),
         # a serving batch, trees, every sequence with a temperature of its own
-        dict(name="verify_tree_b8", kind="verify", dtype="bf16", batch=8, N=32, V=131072, shape="tree", ragged=True, drafts=False, temp="mixed", path=4),
+        dict(name="verify_tree_b8", kind="verify", dtype="bf16", batch=8, N=32, V=131072, shape="tree", ragged=True, drafts=False, temp="mixed", path=2),
         # one user's accepted rows into all caches of a model of which nothing ranks rows (latency)
         dict(name="accept_stream_b1", kind="accept", store="bf16", L=32, Hq=32, Hkv=8, D=128, batch=1, N=8, path=4, ctx=2048, keep=30, sigma=1.0, track=False),
         # accepted rows and their scores, four layers of a serving batch
@@ -47,7 +47,7 @@ def listed():
         dict(name="accept_q4_llama_b8", kind="accept", store="mxfp4", L=4, Hq=32, Hkv=8, D=128, batch=8, N=16, path=5, ctx=32768, keep=30, sigma=1.5, track=True),
         # a whole step: attention of four layers, verification, the accepted rows of all layers
         dict(name="step_llama_b4", kind="step", store="bf16", L=4, Hq=32, Hkv=8, D=128, batch=4, N=16, shape="tree", ctx=32768, keep=30, sigma=1.0, track=True,
-             V=32000, path=4),
+             V=32000, path=2),
     ]
 
 
@@ -64,7 +64,7 @@ def draw(rng):
         drafts = rng.random() < 0.4
         V = _log(rng, 1000, min(160000, (1 << 25) // (batch * N * (2 if drafts else 1))))
         return dict(kind=kind, dtype=rng.choice(["bf16", "f32"]), batch=batch, N=N, V=V, shape="chain" if drafts and rng.random() < 0.7 else shape,
-                    ragged=rng.random() < 0.5, drafts=drafts, temp=rng.choice(["greedy", "one", "mixed", "mixed"]), path=min(N, 3))
+                    ragged=rng.random() < 0.5, drafts=drafts, temp=rng.choice(["greedy", "one", "mixed", "mixed"]), path=min(N, 2))
     Hkv = rng.choice([1, 2, 4, 8])
     D = rng.choice([128, 128, 64])
     store = rng.choice(["bf16", "bf16", "mxfp4", "f32"])
@@ -79,7 +79,7 @@ def draw(rng):
         return dict(case, shape=shape, ragged=rng.random() < 0.5)
     if kind == "accept":
         return dict(case, path=rng.randint(1, min(N, 8)), track=rng.random() < 0.7)
-    return dict(case, shape=shape, track=rng.random() < 0.7, V=_log(rng, 1000, 50000), path=min(N, 3))
+    return dict(case, shape=shape, track=rng.random() < 0.7, V=_log(rng, 1000, 50000), path=min(N, 2))
 
 
 # ---------------------------------------------------------------------------
@@ -243,7 +243,8 @@ def _prepare_caches(case, gen):
 
 
 def _prepare_logits(case, gen, parent):
-    """Logits of a model whose likely next tokens are in part the drafted ones."""
+    """Logits of a model whose likely next tokens are in part the drafted ones (`path` nodes are accepted on average, node 0
+    among them)."""
     batch, N, V = case["batch"], case["N"], case["V"]
     dev = parent.device
     dtype = torch.float32 if case.get("dtype") == "f32" else torch.bfloat16
