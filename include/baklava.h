@@ -140,7 +140,8 @@ int baklava_plan_schedule(const int64_t* off_host, const int32_t* cap_host, int3
  *
  * Calls that only enqueue kernels on the caller's stream (safe inside a stream capture):
  * baklava_reset, baklava_append, baklava_append_prompt (its rows are then those of the capture),
- * baklava_read_rows, baklava_qk_norm_rope, baklava_prompt_attn, baklava_decode_attn, baklava_append_decode_attn (its token
+ * baklava_read_rows, baklava_qk_norm_rope, baklava_prompt_attn, baklava_tree_attn, baklava_verify_draft, baklava_append_accepted,
+ * baklava_decode_attn, baklava_append_decode_attn (its token
  * position and its capacity check are then those of the capture; baklava_append_decode_attn_replay
  * is the variant made for replay), baklava_flush_scores, baklava_compact, and the one-time passes
  * further down.  Set-up calls that synchronise or copy synchronously and therefore must stay
@@ -528,6 +529,80 @@ int baklava_append_prompt(baklava_ctx* ctx, int32_t layer, const baklava_rows* k
  */
 int baklava_read_rows(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count, int32_t n, void* k_out, void* v_out,
                       void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Steps over several drafted tokens: attention of a tree of them over the caches, verification, and the accepted ones
+ * into the caches.  Of these calls the host mirror of the lengths knows nothing (as of baklava_append_decode_attn_replay):
+ * baklava_sync_lengths comes before the next call that relies on it.
+ *
+ * A tree is parent DEVICE int32 [batch, N] and n_nodes DEVICE int32 [batch] or NULL (N everywhere; values are taken into
+ * 0 .. N): node i's parent is an earlier node, parent[b][i] < i; anything else is none, the node then hangs on the cache alone.
+ * N 1 .. 256.  Rows of nodes are rows of n_seq = layer_count * batch sequences of N tokens each, those of the first layer first
+ * (packed rows: the sequences in a row, N tokens each whatever n_nodes says).  Rows of nodes from n_nodes on are neither read
+ * nor written.
+ * ------------------------------------------------------------------------------------------ */
+
+/*
+ * Attention of the nodes of every sequence's tree over the caches of a layer range: node i sees all live rows of a cache and,
+ * of the drafted rows k, v, those of its ancestors and its own:
+ *   out[i][hq] = softmax(q[i][hq] . [K_c; k of those]^T / sqrt(D)) [V_c; v of those],  c = the cache of KV head hq / G.
+ * A node on a path from the root gets what baklava_append_decode_attn gives when the path's tokens are appended one by one;
+ * for MXFP4 caches the drafted rows are rounded to 4 bits first, as an append does.  Nothing is appended, scores stay.  Caches may
+ * be empty.
+ * q, out rows of Hq heads, k, v rows of Hkv heads, in the context's dtype (bf16 for MXFP4); lse NULL or fp32 "rows of one
+ * element" as in baklava_prompt_attn.  fp32 accumulation; softmax weights of bf16 rows enter the second product as bf16.
+ * workspace DEVICE, baklava_tree_workspace_bytes(ctx, layer_count, N) bytes, 256-byte aligned, free again once the stream has
+ * passed the call; its contents do not matter.
+ * Live lengths are read on the device.  Enqueues two kernels on `stream`; deterministic.
+ * Errors: EINVAL (null, misaligned, bad range, N, shape or stride), ECAPACITY (workspace too small), EHIP.
+ */
+size_t baklava_tree_workspace_bytes(const baklava_ctx* ctx, int32_t layer_count, int32_t N);
+int baklava_tree_attn(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count, const baklava_rows* k, const baklava_rows* v,
+                      int32_t N, const int32_t* parent, const int32_t* n_nodes, const baklava_rows* q,
+                      const baklava_rows* out, const baklava_rows* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Which drafted tokens stand, and the token behind them, from given random numbers, so that tokens are distributed as if the
+ * target had been sampled one by one.  Node 0 of a tree is a token that is decided already; row i of `logits` is what the
+ * target says about the token behind node i.  With T the sequence's temperature and x a row of V logits, its distribution is
+ * softmax(x / T), or, where T is not above 0, all on the first of the largest logits.  p_i is that of target row i; q_i that
+ * of draft row i, from which token[b][i] was drawn, or, without draft_logits and where T is not above 0, all on token[b][i].
+ *   cur = 0, r = p_0;  for i = 1 .. n_nodes - 1 with parent i = cur:   u[b][i] q_i(token i) < r(token i):  cur = i, r = p_i
+ *                                                         otherwise  r = max(r - q_i, 0) / its sum (stays if that is 0)
+ * path_out[b] are the values cur took (then -1), n_path_out[b] how many; next_token_out[b] is the first v whose
+ * r(0) + ... + r(v) exceeds u[b][0] times the sum of r.  A sequence without nodes: 0, and -1 as the next token; also -1 behind
+ * a row without a logit above -inf.  A NaN logit counts as -inf, +inf as the largest fp32 number.  A token outside 0 .. V-1 is
+ * never accepted and leaves r as it is.
+ * logits, draft_logits DEVICE [n_seq * N] rows of V elements of `dtype` (BAKLAVA_BF16 or BAKLAVA_F32), contiguous, aligned to an
+ * element; draft_logits NULL or with its own row stride (strides in elements, >= 0).  token, parent DEVICE int32 [n_seq, N];
+ * temperature DEVICE fp32 [n_seq] or NULL (1); u DEVICE fp32 [n_seq, N], 0 <= u < 1.  path_out DEVICE int32 [n_seq, N],
+ * n_path_out, next_token_out DEVICE int32 [n_seq].  V 1 .. 2^30, rows times parts of 8192 elements below 2^21.
+ * workspace DEVICE, baklava_verify_workspace_bytes(n_seq, N, V, draft_logits != NULL) bytes, 256-byte aligned, as above.
+ * All sums and exponentials in 64 bits.  A rejected node of a sequence with draft_logits that has a later sibling costs a pass of
+ * one workgroup over two rows.  Enqueues kernels on `stream`; deterministic.
+ * Errors: EINVAL (null, misaligned, bad shape, stride or dtype), ECAPACITY (workspace too small), EHIP.
+ */
+size_t baklava_verify_workspace_bytes(int32_t n_seq, int32_t N, int32_t V, int32_t with_draft_logits);
+int baklava_verify_draft(const void* logits, int64_t row_stride, const void* draft_logits, int64_t draft_row_stride,
+                         int32_t dtype, int32_t n_seq, int32_t N, int32_t V, const int32_t* token, const int32_t* parent,
+                         const int32_t* n_nodes, const float* temperature, const float* u, int32_t* path_out,
+                         int32_t* n_path_out, int32_t* next_token_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Appends the rows of an accepted path to the caches of a layer range: rows path[b][0 .. n_path[b]) of sequence b's nodes go
+ * behind the live rows of each of its caches, rounded to 4 bits for MXFP4, at positions pos0[b], pos0[b] + 1, ...
+ * path DEVICE int32 [batch, N] (entries behind the first that is not within 0 .. N-1 are not looked at), n_path, pos0 DEVICE int32
+ * [batch], as baklava_verify_draft leaves them.  k, v as for baklava_tree_attn.
+ * With score tracking in force, q and lse as baklava_tree_attn took and gave them (of the nodes on the path alone): the weights
+ * of the path's attention are added to the scores of all rows, as decode steps over the path's tokens would add them, new rows
+ * among them; otherwise q and lse are not looked at and new rows get 0.
+ * A cache without room for its path stays as it is and raises the status word that baklava_sync_lengths reports.
+ * Enqueues one kernel on `stream`, two with tracking.
+ * Errors: EINVAL (null, misaligned, bad range, N, shape or stride), EHIP.
+ */
+int baklava_append_accepted(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count, const baklava_rows* k,
+                            const baklava_rows* v, int32_t N, const int32_t* path, const int32_t* n_path, const int32_t* pos0,
+                            const baklava_rows* q, const baklava_rows* lse, void* stream);
 
 /*
  * Algorithm 1, step 2, with the normalisation of "Head Importance Heuristic" (host only): the

@@ -34,6 +34,7 @@ EXPORTS = [
     "baklava_alloc_two_level", "baklava_layer_similarity_static", "baklava_append_decode_attn_replay",
     "baklava_sync_lengths", "baklava_flush_scores",
     "baklava_qk_norm_rope", "baklava_prompt_attn", "baklava_append_prompt", "baklava_read_rows",
+    "baklava_tree_workspace_bytes", "baklava_tree_attn", "baklava_verify_workspace_bytes", "baklava_verify_draft", "baklava_append_accepted",
 ]
 
 
@@ -122,8 +123,15 @@ def lib() -> C.CDLL:
     L.baklava_prompt_attn.argtypes = [vp, vp, vp, C.c_int32, vp, vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp]
     L.baklava_append_prompt.argtypes = [vp, C.c_int32, vp, vp, vp, vp, vp, vp]
     L.baklava_read_rows.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
+    L.baklava_tree_workspace_bytes.restype = C.c_size_t
+    L.baklava_tree_workspace_bytes.argtypes = [vp, C.c_int32, C.c_int32]
+    L.baklava_tree_attn.argtypes = [vp, C.c_int32, C.c_int32, vp, vp, C.c_int32, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    L.baklava_verify_workspace_bytes.restype = C.c_size_t
+    L.baklava_verify_workspace_bytes.argtypes = [C.c_int32] * 4
+    L.baklava_verify_draft.argtypes = [vp, C.c_int64, vp, C.c_int64] + [C.c_int32] * 4 + [vp] * 9 + [C.c_size_t, vp]
+    L.baklava_append_accepted.argtypes = [vp, C.c_int32, C.c_int32, vp, vp, C.c_int32] + [vp] * 6
     for name in EXPORTS:
-        if name not in ("baklava_strerror", "baklava_workspace_bytes", "baklava_profile_workspace_bytes",
+        if name not in ("baklava_tree_workspace_bytes", "baklava_verify_workspace_bytes", "baklava_strerror", "baklava_workspace_bytes", "baklava_profile_workspace_bytes",
                         "baklava_layer_workspace_bytes"):
             getattr(L, name).restype = C.c_int
     _lib = L
@@ -358,6 +366,68 @@ class Arena:
                                        _stream_ptr(stream)), "baklava_read_rows")
         _hold_until_stream_passes((k, v), stream)
         return k, v
+
+    def _nodes(self, rows, parent, n_nodes) -> int:
+        """Nodes of a tree, from its tensor of parents."""
+        _expect_ints(rows, parent, "parent", (self.batch, None))
+        if n_nodes is not None:
+            _expect_ints(rows, n_nodes, "n_nodes", (self.batch,))
+        return parent.shape[1]
+
+    def tree_attn(self, layer_begin: int, layer_count: int, k, v, parent, q, n_nodes=None, out=None, lse=None,
+                  want_lse: bool = False, stream=None):
+        """baklava_tree_attn: parent int32 [batch, N], n_nodes int32 [batch] or None (N); q [tokens, Hq, D], k and v [tokens,
+        Hkv, D] (N tokens of every sequence in a row, the sequences of the first layer first) or [layers * batch, H, N, D], of any
+        strides with contiguous rows.  Returns out (like q; places of absent nodes are not written), and with want_lse or lse given
+        also lse (fp32 [Hq, tokens] or [layers * batch, Hq, N]).  No gradient: tensors that require one are refused outside
+        torch.no_grad()."""
+        torch = self.torch
+        _refuse_grad(torch, q, k, v)
+        rows = _Rows(torch)
+        if rows.device != self.gpu:
+            raise ValueError("the arena's GPU must be the current one")
+        N = self._nodes(rows, parent, n_nodes)
+        n_seq = layer_count * self.batch
+        dt = torch.float32 if self.dtype not in ("bf16", "mxfp4") else torch.bfloat16
+        k_at = rows.add(k, "k", n_seq, n_seq * N, N, self.Hkv, self.D, dt)
+        v_at = rows.add(v, "v", n_seq, n_seq * N, N, self.Hkv, self.D, dt)
+        q_at = rows.add(q, "q", n_seq, n_seq * N, N, self.Hq, self.D, dt)
+        nbytes = lib().baklava_tree_workspace_bytes(self.ctx, int(layer_count), N)
+        if out is None:
+            out = _empty_on(stream, q.new_empty, q.shape)
+        if lse is None and want_lse:
+            lse = _empty_on(stream, q.new_empty, (self.Hq, q.shape[0]) if q.dim() == 3 else q.shape[:3], dtype=torch.float32)
+        out_at = rows.add(out, "out", n_seq, n_seq * N, N, self.Hq, self.D, dt)
+        lse_at = rows.add_values(lse, "lse", n_seq, n_seq * N, N, self.Hq) if lse is not None else None
+        ws = _empty_on(stream, torch.empty, (max(nbytes, 256),), dtype=torch.uint8, device=q.device)
+        _check(lib().baklava_tree_attn(self.ctx, int(layer_begin), int(layer_count), k_at, v_at, N, parent.data_ptr(),
+                                       n_nodes.data_ptr() if n_nodes is not None else None, q_at, out_at, lse_at, ws.data_ptr(),
+                                       nbytes, _stream_ptr(stream)), "baklava_tree_attn")
+        _hold_until_stream_passes((out, lse), stream)
+        return (out, lse) if lse is not None else out
+
+    def append_accepted(self, layer_begin: int, layer_count: int, k, v, path, n_path, pos0, q=None, lse=None, stream=None) -> None:
+        """baklava_append_accepted: path int32 [batch, N], n_path and pos0 int32 [batch]; k, v (and q, lse, which an arena that
+        tracks scores needs) as tree_attn took and gave them.  sync_lengths comes before the next call that takes its position
+        by value."""
+        torch = self.torch
+        rows = _Rows(torch)
+        if rows.device != self.gpu:
+            raise ValueError("the arena's GPU must be the current one")
+        _expect_ints(rows, path, "path", (self.batch, None))
+        _expect_ints(rows, n_path, "n_path", (self.batch,))
+        _expect_ints(rows, pos0, "pos0", (self.batch,))
+        if (q is None) != (lse is None):
+            raise ValueError("q and lse go together")
+        N, n_seq = path.shape[1], layer_count * self.batch
+        dt = torch.float32 if self.dtype not in ("bf16", "mxfp4") else torch.bfloat16
+        k_at = rows.add(k, "k", n_seq, n_seq * N, N, self.Hkv, self.D, dt)
+        v_at = rows.add(v, "v", n_seq, n_seq * N, N, self.Hkv, self.D, dt)
+        q_at = rows.add(q, "q", n_seq, n_seq * N, N, self.Hq, self.D, dt) if q is not None else None
+        lse_at = rows.add_values(lse, "lse", n_seq, n_seq * N, N, self.Hq) if lse is not None else None
+        _check(lib().baklava_append_accepted(self.ctx, int(layer_begin), int(layer_count), k_at, v_at, N, path.data_ptr(),
+                                             n_path.data_ptr(), pos0.data_ptr(), q_at, lse_at, _stream_ptr(stream)),
+               "baklava_append_accepted")
 
     def decode_attn(self, layer_begin: int, layer_count: int, q, out, stream=None) -> None:
         if self.mx:
@@ -606,6 +676,59 @@ class _Rows:
             raise ValueError(f"{name}: float32 expected")
         self.on_device(t, name)
         return self._put(t, seq, tok, head)
+
+
+def _expect_ints(rows: _Rows, t, name: str, shape) -> None:
+    """int32 [shape] (None: any size of at least one) on the current GPU, contiguous."""
+    import torch
+    if t.dtype is not torch.int32 or not t.is_contiguous() or t.dim() != len(shape) or any(
+            n < 1 if want is None else n != want for n, want in zip(t.shape, shape)):
+        raise ValueError(f"{name} must be a contiguous int32 tensor [{', '.join('N' if x is None else str(x) for x in shape)}]")
+    rows.on_device(t, name)
+
+
+def verify_draft(logits, token, parent, u, draft_logits=None, temperature=None, n_nodes=None, stream=None):
+    """baklava_verify_draft: logits (and draft_logits) [batch, N, V] or [batch * N, V] bf16 or fp32, rows of any one stride with
+    contiguous elements; token and parent int32 [batch, N], u fp32 [batch, N], temperature fp32 [batch] or None (1), n_nodes int32
+    [batch] or None (N).  Returns (path [batch, N], n_path [batch], next_token [batch]), int32."""
+    import torch
+    rows = _Rows(torch)
+    _expect_ints(rows, parent, "parent", (None, None))
+    batch, N = parent.shape
+    _expect_ints(rows, token, "token", (batch, N))
+    if n_nodes is not None:
+        _expect_ints(rows, n_nodes, "n_nodes", (batch,))
+    for t, name, shape in ((u, "u", (batch, N)), (temperature, "temperature", (batch,))):
+        if t is not None:
+            if t.dtype is not torch.float32 or not t.is_contiguous() or t.shape != shape:
+                raise ValueError(f"{name} must be a contiguous fp32 tensor {list(shape)}")
+            rows.on_device(t, name)
+    dt, V = logits.dtype, logits.shape[-1]
+    if dt is not torch.bfloat16 and dt is not torch.float32:
+        raise ValueError("bf16 or fp32 logits expected")
+    at = []
+    for t, name in ((logits, "logits"), (draft_logits, "draft_logits")):
+        if t is None:
+            at.append((None, 0))
+            continue
+        shape = t.shape
+        if shape != (batch, N, V) and shape != (batch * N, V):
+            raise ValueError(f"{name} must be [{batch}, {N}, {V}] or [{batch * N}, {V}]")
+        if t.dtype is not dt or (V > 1 and t.stride(-1) != 1) or (len(shape) == 3 and N > 1 and batch > 1 and t.stride(0) != N * t.stride(1)):
+            raise ValueError(f"{name}: contiguous rows of {dt}, at one distance, expected")
+        rows.on_device(t, name)
+        at.append((t.data_ptr(), t.stride(0) if len(shape) == 2 or N == 1 else t.stride(1)))
+    nbytes = lib().baklava_verify_workspace_bytes(batch, N, V, int(draft_logits is not None))
+    path = _empty_on(stream, parent.new_empty, (batch, N))
+    n_path, token_out = (_empty_on(stream, parent.new_empty, (batch,)) for _ in range(2))
+    ws = _empty_on(stream, torch.empty, (max(nbytes, 256),), dtype=torch.uint8, device=logits.device)
+    _check(lib().baklava_verify_draft(at[0][0], at[0][1], at[1][0], at[1][1], BF16 if dt is torch.bfloat16 else F32, batch, N, V,
+                                      token.data_ptr(), parent.data_ptr(), n_nodes.data_ptr() if n_nodes is not None else None,
+                                      temperature.data_ptr() if temperature is not None else None, u.data_ptr(), path.data_ptr(),
+                                      n_path.data_ptr(), token_out.data_ptr(), ws.data_ptr(), nbytes, _stream_ptr(stream)),
+           "baklava_verify_draft")
+    _hold_until_stream_passes((path, n_path, token_out), stream)
+    return path, n_path, token_out
 
 
 def prompt_attn(q, k, v, lens: Sequence[int], kv_lens: Optional[Sequence[int]] = None, out=None, lse=None,

@@ -34,6 +34,7 @@ constexpr int kMostFillItems = 256;       // most work items such short runs are
 constexpr int32_t kMostPromptTokens = 1 << 29;      // of a sequence
 constexpr int32_t kMostRopeTokens = 1 << 26;        // of a sequence
 constexpr int64_t kMostTokenStride = 1 << 24;       // offsets inside a tile of rows stay below 2^32 bytes
+constexpr int32_t kMostVocabulary = 1 << 30;
 constexpr int kMaxChunk = 1 << 22; // row offsets inside a work item stay below 2^32 bytes
 inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
@@ -48,7 +49,7 @@ struct WorkspacePlan {
   // several layers where that of a single one would cut needlessly short runs (see schedule_for)
   size_t items[3], multi[3];
   size_t part_o, part_ml, final_ml, logits, lag_q, lag_ml, lag_n, lag_cnt, flush_ticket, status, kept, info, order_all, order_layer;
-  size_t move_ticket, move_flags, tiles, spread, tile_hist, sel_state, total;
+  size_t move_ticket, move_flags, tiles, spread, tile_hist, sel_state, accept, total;
   int64_t n_tiles, n_long;
   int64_t max_items;
 };
@@ -128,6 +129,7 @@ WorkspacePlan plan_workspace(const baklava_desc* d, const int32_t* cap) {
   w.spread = o;       o = align256(o + (size_t)(w.n_tiles + n_caches) * sizeof(SelTile));
   w.tile_hist = o;    o = align256(o + (size_t)w.n_tiles * 4 * 256 * 4);
   w.sel_state = o;    o = align256(o + (size_t)w.n_long * 4 * sizeof(SelState));
+  w.accept = o;       o = align256(o + (size_t)n_caches * sizeof(int2));
   w.total = o;
   return w;
 }
@@ -1137,6 +1139,173 @@ extern "C" int baklava_read_rows(baklava_ctx* ctx, int32_t layer_begin, int32_t 
   if (!hip_ok(launch_read_rows(p, query_row_bytes(&ctx->d) / 16, ctx->d.dtype == BAKLAVA_MXFP4, layer_count * ctx->cpl,
                                (hipStream_t)stream)))
     return BAKLAVA_EHIP;
+  return BAKLAVA_OK;
+}
+
+namespace {
+
+// Rows of n_seq sequences of N tokens each, packed or not, with their strides as num / den of the caller's.
+Rows tree_rows(const baklava_rows* r, int64_t N, int64_t num, int64_t den) {
+  Rows x = device_rows(r, num, den);
+  if (!x.seq) x.seq = x.tok * N;  // packed: sequences of N tokens in a row
+  return x;
+}
+
+struct TreeSpace {
+  size_t ml, o, total;  // (the table of the caches is in front)
+};
+TreeSpace tree_space(const baklava_ctx* ctx, int32_t layer_count, int32_t N) {
+  const int64_t rows = (int64_t)N * ctx->G, n_caches = (int64_t)layer_count * ctx->cpl;
+  const TreeLaunch t = tree_launch(ctx->d.dtype, ctx->d.D, (int)rows, ctx->n_cus);
+  const size_t slots = 2 * (size_t)t.target * rows;
+  TreeSpace w;
+  w.ml = align256((size_t)n_caches * sizeof(int2));
+  w.o = align256(w.ml + slots * sizeof(float2));
+  w.total = align256(w.o + slots * ctx->d.D * sizeof(float));
+  return w;
+}
+
+}  // namespace
+
+extern "C" size_t baklava_tree_workspace_bytes(const baklava_ctx* ctx, int32_t layer_count, int32_t N) {
+  if (!ctx || layer_count < 1 || layer_count > ctx->d.L || N < 1 || N > kMostNodes) return 0;
+  return tree_space(ctx, layer_count, N).total;
+}
+
+extern "C" int baklava_tree_attn(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count, const baklava_rows* k,
+                                 const baklava_rows* v, int32_t N, const int32_t* parent, const int32_t* n_nodes,
+                                 const baklava_rows* q, const baklava_rows* out, const baklava_rows* lse, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+  if (!ctx || !range_ok(ctx, layer_begin, layer_count) || N < 1 || N > kMostNodes) return BAKLAVA_EINVAL;
+  if (!parent || (((uintptr_t)parent | (uintptr_t)n_nodes) & 3) || !workspace || ((uintptr_t)workspace & 255)) return BAKLAVA_EINVAL;
+  const int64_t n_seq64 = (int64_t)layer_count * ctx->d.batch;
+  if (n_seq64 * N > INT32_MAX) return BAKLAVA_EINVAL;
+  const int32_t n_seq = (int32_t)n_seq64, Hq = ctx->d.Hq, Hkv = ctx->d.Hkv, D = ctx->d.D;
+  const int es = ctx->d.dtype == BAKLAVA_F32 ? 4 : 2, unit = 16 / es;
+  if (!rows_ok(q, n_seq, N, Hq, unit, 16) || !rows_ok(k, n_seq, N, Hkv, unit, 16) || !rows_ok(v, n_seq, N, Hkv, unit, 16)) return BAKLAVA_EINVAL;
+  if (!written_rows_ok(out, n_seq, N, Hq, unit, 16, D) || (lse && !written_rows_ok(lse, n_seq, N, Hq, 1, 4, 1))) return BAKLAVA_EINVAL;
+  const TreeSpace w = tree_space(ctx, layer_count, N);
+  if (workspace_bytes < w.total) return BAKLAVA_ECAPACITY;
+  TreeParams p{};
+  p.q = tree_rows(q, N, es, 1); p.k = tree_rows(k, N, es, 1); p.v = tree_rows(v, N, es, 1);
+  p.out = tree_rows(out, N, es, 1); p.lse = tree_rows(lse, N, 4, 1);
+  p.k_plane = ctx->d.k; p.v_plane = ctx->d.v;
+  p.kv_scale = reinterpret_cast<const uint8_t*>(ctx->d.kv_scale);
+  p.off = ctx->d.off; p.len = ctx->d.len;
+  p.parent = parent; p.n_nodes = n_nodes;
+  char* const ws = reinterpret_cast<char*>(workspace);
+  p.table = reinterpret_cast<int2*>(ws);
+  p.part_ml = reinterpret_cast<float2*>(ws + w.ml);
+  p.part_o = reinterpret_cast<float*>(ws + w.o);
+  p.N = N; p.G = ctx->G; p.Hkv = Hkv; p.batch = ctx->d.batch;
+  p.cache0 = layer_begin * ctx->cpl; p.n_caches = layer_count * ctx->cpl;
+  p.rows = N * ctx->G;
+  const TreeLaunch t = tree_launch(ctx->d.dtype, D, p.rows, ctx->n_cus);
+  p.row_tiles = t.row_tiles; p.target = t.target; p.least = 1;
+  p.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)D));
+  if (!hip_ok(launch_tree_attn(p, t, ctx->d.dtype, D, p.n_caches, (hipStream_t)stream))) return BAKLAVA_EHIP;
+  return BAKLAVA_OK;
+}
+
+extern "C" int baklava_append_accepted(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count, const baklava_rows* k,
+                                       const baklava_rows* v, int32_t N, const int32_t* path, const int32_t* n_path,
+                                       const int32_t* pos0, const baklava_rows* q, const baklava_rows* lse, void* stream) {
+  if (!ctx || !range_ok(ctx, layer_begin, layer_count) || N < 1 || N > kMostNodes || !path || !n_path || !pos0) return BAKLAVA_EINVAL;
+  if (((uintptr_t)path | (uintptr_t)n_path | (uintptr_t)pos0) & 3) return BAKLAVA_EINVAL;
+  const int64_t n_seq64 = (int64_t)layer_count * ctx->d.batch;
+  if (n_seq64 * N > INT32_MAX) return BAKLAVA_EINVAL;
+  const int32_t n_seq = (int32_t)n_seq64;
+  const int es = ctx->d.dtype == BAKLAVA_F32 ? 4 : 2, unit = 16 / es;
+  if (!rows_ok(k, n_seq, N, ctx->d.Hkv, unit, 16) || !rows_ok(v, n_seq, N, ctx->d.Hkv, unit, 16)) return BAKLAVA_EINVAL;
+  const bool track = ctx->track_on;
+  if (track && (!rows_ok(q, n_seq, N, ctx->d.Hq, unit, 16) || !rows_ok(lse, n_seq, N, ctx->d.Hq, 1, 4))) return BAKLAVA_EINVAL;
+  AcceptParams p{};
+  p.k = tree_rows(k, N, 1, unit); p.v = tree_rows(v, N, 1, unit);
+  if (track) {
+    p.q = tree_rows(q, N, es, 1);
+    p.lse = tree_rows(lse, N, 4, 1);
+    p.table = reinterpret_cast<int2*>(ctx->ws + ctx->plan.accept);
+  }
+  p.k_plane = ctx->d.k; p.v_plane = ctx->d.v;
+  p.kv_scale = reinterpret_cast<uint8_t*>(ctx->d.kv_scale);
+  p.score = ctx->d.score; p.pos = ctx->d.pos; p.off = ctx->d.off; p.cap = ctx->d.cap; p.len = ctx->d.len;
+  p.path = path; p.n_path = n_path; p.pos0 = pos0;
+  p.status = reinterpret_cast<int32_t*>(ctx->ws + ctx->plan.status);
+  p.N = N; p.G = ctx->G; p.Hkv = ctx->d.Hkv; p.batch = ctx->d.batch;
+  p.cache0 = layer_begin * ctx->cpl; p.n_caches = layer_count * ctx->cpl;
+  p.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)ctx->d.D));
+  if (!hip_ok(launch_append_accepted(p, ctx->d.dtype, ctx->d.D, ctx->n_cus, (hipStream_t)stream))) return BAKLAVA_EHIP;
+  return BAKLAVA_OK;
+}
+
+namespace {
+
+struct VerifySpace {
+  int64_t parts;
+  size_t all, draft_all, end, tried, left, mass, top, total;  // (the statistics are in front)
+};
+VerifySpace verify_space(int32_t n_seq, int32_t N, int32_t V, bool draft) {
+  const size_t nodes = (size_t)n_seq * N;
+  VerifySpace w;
+  w.parts = ((int64_t)V + kVerifyPart - 1) / kVerifyPart;
+  w.all = align256(nodes * w.parts * (draft ? 2 : 1) * sizeof(VerifyStat));
+  w.draft_all = align256(w.all + nodes * sizeof(VerifyStat));
+  w.end = align256(w.draft_all + (draft ? nodes : 0) * sizeof(VerifyStat));
+  w.tried = align256(w.end + (size_t)n_seq * sizeof(VerifyEnd));
+  w.left = align256(w.tried + nodes * sizeof(int32_t));
+  w.mass = align256(w.left + nodes * sizeof(double));
+  w.top = align256(w.mass + (size_t)n_seq * w.parts * 2 * sizeof(double));
+  w.total = align256(w.top + (size_t)n_seq * w.parts * sizeof(VerifyStat));
+  return w;
+}
+
+bool verify_shape_ok(int32_t n_seq, int32_t N, int32_t V, bool draft) {
+  if (n_seq < 1 || N < 1 || N > kMostNodes || V < 1 || V > kMostVocabulary) return false;
+  const int64_t parts = ((int64_t)V + kVerifyPart - 1) / kVerifyPart;
+  return (int64_t)n_seq * N <= INT32_MAX / 1024 && (int64_t)n_seq * N * (draft ? 2 : 1) * parts <= INT32_MAX / 1024;
+}
+
+}  // namespace
+
+extern "C" size_t baklava_verify_workspace_bytes(int32_t n_seq, int32_t N, int32_t V, int32_t with_draft_logits) {
+  if (!verify_shape_ok(n_seq, N, V, with_draft_logits != 0)) return 0;
+  return verify_space(n_seq, N, V, with_draft_logits != 0).total;
+}
+
+extern "C" int baklava_verify_draft(const void* logits, int64_t row_stride, const void* draft_logits, int64_t draft_row_stride,
+                                    int32_t dtype, int32_t n_seq, int32_t N, int32_t V, const int32_t* token,
+                                    const int32_t* parent, const int32_t* n_nodes, const float* temperature, const float* u,
+                                    int32_t* path, int32_t* n_path, int32_t* next_token, void* workspace,
+                                    size_t workspace_bytes, void* stream) {
+  if (!logits || !token || !parent || !u || !path || !n_path || !next_token || !workspace) return BAKLAVA_EINVAL;
+  if (dtype != BAKLAVA_BF16 && dtype != BAKLAVA_F32) return BAKLAVA_EINVAL;
+  if (!verify_shape_ok(n_seq, N, V, draft_logits != nullptr)) return BAKLAVA_EINVAL;
+  const uintptr_t es = dtype == BAKLAVA_F32 ? 4 : 2;
+  if (((uintptr_t)logits | (uintptr_t)draft_logits) & (es - 1)) return BAKLAVA_EINVAL;
+  if (((uintptr_t)token | (uintptr_t)parent | (uintptr_t)n_nodes | (uintptr_t)temperature | (uintptr_t)u | (uintptr_t)path |
+       (uintptr_t)n_path | (uintptr_t)next_token) & 3)
+    return BAKLAVA_EINVAL;
+  const int64_t most_stride = INT64_MAX / 8 / ((int64_t)n_seq * N);
+  if (row_stride < 0 || row_stride > most_stride || (draft_logits && (draft_row_stride < 0 || draft_row_stride > most_stride))) return BAKLAVA_EINVAL;
+  if ((uintptr_t)workspace & 255) return BAKLAVA_EINVAL;
+  const VerifySpace w = verify_space(n_seq, N, V, draft_logits != nullptr);
+  if (workspace_bytes < w.total) return BAKLAVA_ECAPACITY;
+  VerifyParams p{};
+  p.logits = logits; p.draft = draft_logits;
+  p.row = row_stride; p.draft_row = draft_row_stride;
+  p.token = token; p.parent = parent; p.n_nodes = n_nodes; p.temp = temperature; p.u = u;
+  p.path = path; p.n_path = n_path; p.next = next_token;
+  char* const ws = reinterpret_cast<char*>(workspace);
+  p.stat = reinterpret_cast<VerifyStat*>(ws);
+  p.all = reinterpret_cast<VerifyStat*>(ws + w.all);
+  p.draft_all = reinterpret_cast<VerifyStat*>(ws + w.draft_all);
+  p.end = reinterpret_cast<VerifyEnd*>(ws + w.end);
+  p.tried = reinterpret_cast<int32_t*>(ws + w.tried);
+  p.left = reinterpret_cast<double*>(ws + w.left);
+  p.mass = reinterpret_cast<double*>(ws + w.mass);
+  p.top = reinterpret_cast<VerifyStat*>(ws + w.top);
+  p.n_seq = n_seq; p.N = N; p.V = V; p.parts = (int32_t)w.parts;
+  if (!hip_ok(launch_verify_draft(p, dtype, (hipStream_t)stream))) return BAKLAVA_EHIP;
   return BAKLAVA_OK;
 }
 

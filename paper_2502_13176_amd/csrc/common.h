@@ -231,6 +231,88 @@ struct ReadRowsParams {
   int32_t cache0, n;
 };
 
+constexpr int kMostNodes = 256;  // nodes of a tree of drafted tokens
+struct TreeParams {
+  Rows q, k, v, out, lse;   // strides in bytes; sequences: batch of every layer of the launch, none packed
+  const void* k_plane;
+  const void* v_plane;
+  const uint8_t* kv_scale;
+  const int64_t* off;
+  const int32_t* len;
+  const int32_t* parent;    // [batch, N]
+  const int32_t* n_nodes;   // [batch] or null (N)
+  int2* table;              // [n_caches] of a cache: first partial slot, work items
+  float2* part_ml;          // [slots, rows] maximum (log2 units) and sum
+  float* part_o;            // [slots, rows, D]
+  int32_t N, G, Hkv, batch;
+  int32_t cache0, n_caches;
+  int32_t rows;             // N * G
+  int32_t row_tiles;        // workgroups of a work item
+  int32_t target;           // work items of the launch, about
+  int32_t least;            // tiles of a work item, at least where its cache has several
+  float scale_log2e;
+};
+// How a launch over query rows of this many is cut: wavefronts that share 32 of them, workgroups of a work item, work items.
+struct TreeLaunch {
+  int ks, row_tiles, target;
+};
+
+constexpr int kAcceptRows = kMostNodes * 16;  // query rows of a path
+struct AcceptParams {
+  Rows k, v;                // strides in 16-byte pieces; sequences as in TreeParams
+  Rows q, lse;              // in bytes (tracking only)
+  void* k_plane;
+  void* v_plane;
+  uint8_t* kv_scale;
+  float* score;
+  int32_t* pos;
+  const int64_t* off;
+  const int32_t* cap;
+  int32_t* len;
+  const int32_t* path;      // [batch, N]
+  const int32_t* n_path;    // [batch]
+  const int32_t* pos0;      // [batch]
+  int32_t* status;          // raised by a cache without room
+  int2* table;              // [n_caches] of a cache: live rows before, new rows; null: scores are not tracked
+  int32_t N, G, Hkv, batch;
+  int32_t cache0, n_caches;
+  int32_t target, least;
+  float scale_log2e;
+};
+
+// Verification of drafted tokens: workspace of a call, and its launches.
+struct VerifyStat {       // of a part of a row of logits, or of all of it
+  double sum;             // of exp((x - top) / temperature)
+  float top;
+  int32_t first;          // where the first of the largest is
+};
+struct VerifyEnd {        // where the walk of a sequence has ended
+  int32_t last;           // node
+  int32_t n_tried;        // its children that were tried and not accepted, and have an effect on what may follow
+};
+struct VerifyParams {
+  const void* logits;     // [n_seq * N] rows of V elements
+  const void* draft;      // the same, or null
+  int64_t row, draft_row; // elements between rows
+  const int32_t* token;   // [n_seq, N]
+  const int32_t* parent;
+  const int32_t* n_nodes; // [n_seq] or null
+  const float* temp;      // [n_seq] or null (1)
+  const float* u;         // [n_seq, N]
+  int32_t* path;          // [n_seq, N]
+  int32_t* n_path;        // [n_seq]
+  int32_t* next;          // [n_seq]
+  VerifyStat* stat;       // [target, then draft rows][n_seq * N][parts]
+  VerifyStat* all;        // [n_seq * N] merged over the parts: target rows
+  VerifyStat* draft_all;  // [n_seq * N] draft rows
+  VerifyEnd* end;         // [n_seq]
+  int32_t* tried;         // [n_seq, N] those children
+  double* left;           // [n_seq, N] what each left of the distribution
+  double* mass;           // [n_seq][parts][2] weights of a part of the last node's row: with all of them taken off, without the last
+  VerifyStat* top;        // [n_seq][parts] the largest logit of it
+  int32_t n_seq, N, V, parts;
+};
+
 constexpr int kLengthsPerLaunch = 512;
 struct LengthsParams {
   int32_t* len;
@@ -307,6 +389,11 @@ hipError_t launch_prompt_attn(const PromptParams& p, int D, int tile_tokens, int
 // pieces: 16-byte pieces of a row as the caller holds it; most: tokens of the longest sequence
 hipError_t launch_append_prompt(const PromptRowsParams& p, int pieces, bool mx, int n_seq, int most, hipStream_t s);
 hipError_t launch_read_rows(const ReadRowsParams& p, int pieces, bool mx, int n_caches, hipStream_t s);
+TreeLaunch tree_launch(int type, int D, int rows, int n_cus);
+hipError_t launch_tree_attn(const TreeParams& p, const TreeLaunch& t, int type, int D, int n_caches, hipStream_t s);
+hipError_t launch_append_accepted(const AcceptParams& p, int type, int D, int n_cus, hipStream_t s);
+constexpr int kVerifyPart = 8192;  // elements of a row that a workgroup takes
+hipError_t launch_verify_draft(const VerifyParams& p, int dtype, hipStream_t s);
 hipError_t launch_set_lengths(const LengthsParams& p, hipStream_t s);
 hipError_t launch_fill_i32(int32_t* dst, int32_t value, int64_t n, hipStream_t s);
 // n_wide: caches of the range with more than kNarrowRows rows of capacity; sorted: they come first in p.order

@@ -1,0 +1,92 @@
+// Work items of launches over the ragged caches that are cut by the lengths on the device: the tiles of all caches of a launch,
+// in items of equal length.  Each workgroup finds its own by a scan over the caches.
+#ifndef BAKLAVA_TREE_H
+#define BAKLAVA_TREE_H
+
+#include "common.h"
+
+namespace baklava {
+
+#ifdef __HIPCC__
+// A value that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 |
+                   (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
+
+// Tiles [first, last) of cache c_rel of the launch: number `part` of its n_parts items.  slot: the cache's first partial slot.
+struct Span {
+  int c_rel, first, last, part, n_parts, slot;
+};
+
+// Sum of x over the workgroup's threads up to and with the calling one, and over all of them.
+template <int THREADS>
+__device__ __forceinline__ int scan_threads(int x, int32_t* lds, int& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int i = 1; i < 64; i *= 2) {
+    const int y = __shfl_up(x, i);
+    x += lane >= i ? y : 0;
+  }
+  __syncthreads();  // (lds may still be read)
+  if (lane == 63) lds[wave] = x;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) {
+    const int y = lds[w];
+    before += w < wave ? y : 0;
+    total += y;
+  }
+  return x + before;
+}
+
+// The item number `item` of n_caches caches of tiles(c) tiles each; false: there is none.  Items have at most
+// run = max(least, all tiles / target, rounded up) tiles, so there are at most target + n_caches; the items of a cache are of equal
+// length but for one tile.  Partial slots go to the caches of several items alone, which have fewer than 2 target of them
+// (ceil(x) < 2 x for x > 1).  lds: THREADS / 64 + 3 words, free for other use behind the next barrier.
+template <int THREADS, class Tiles>
+__device__ __forceinline__ bool find_span(int n_caches, int target, int least, int item, const Tiles& tiles, int32_t* lds, Span& sp) {
+  constexpr int kAt = THREADS / 64;
+  const int tid = threadIdx.x;
+  int all = 0;
+  for (int c = tid; c < n_caches; c += THREADS) all += tiles(c);
+  int total;
+  scan_threads<THREADS>(all, lds, total);
+  const int run = max((total + target - 1) / target, least);
+  if (tid == 0) lds[kAt] = -1;
+  int items0 = 0, slots0 = 0;
+  for (int c0 = 0; c0 < n_caches; c0 += THREADS) {
+    const int c = c0 + tid;
+    const int t = c < n_caches ? tiles(c) : 0;
+    const int parts = (t + run - 1) / run;
+    int n_items, n_slots;
+    const int end = items0 + scan_threads<THREADS>(parts, lds, n_items);
+    const int slot_end = slots0 + scan_threads<THREADS>(parts > 1 ? parts : 0, lds, n_slots);
+    if (item < end && item >= end - parts) {
+      lds[kAt] = c;
+      lds[kAt + 1] = slot_end - (parts > 1 ? parts : 0);
+      lds[kAt + 2] = item - (end - parts);
+    }
+    items0 += n_items;
+    slots0 += n_slots;
+    if (item < items0) break;
+  }
+  __syncthreads();
+  const int c = __builtin_amdgcn_readfirstlane(lds[kAt]);
+  if (c < 0) return false;
+  sp.c_rel = c;
+  sp.slot = __builtin_amdgcn_readfirstlane(lds[kAt + 1]);
+  sp.part = __builtin_amdgcn_readfirstlane(lds[kAt + 2]);
+  const int t = __builtin_amdgcn_readfirstlane(tiles(c));
+  sp.n_parts = (t + run - 1) / run;
+  const int per = t / sp.n_parts, more = t % sp.n_parts;  // the first `more` items have one tile more
+  sp.first = sp.part * per + min(sp.part, more);
+  sp.last = sp.first + per + (sp.part < more ? 1 : 0);
+  return true;
+}
+#endif
+
+}  // namespace baklava
+#endif

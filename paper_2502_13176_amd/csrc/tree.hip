@@ -1,0 +1,570 @@
+// Attention of a tree of drafted tokens over ragged caches (baklava_tree_attn).
+//
+// A query row is a node of a sequence's tree and one of the G heads of a KV head (row r: node r / G, head r % G).  It sees every
+// live row of the cache, and of the drafted rows those of its ancestors and its own.  Both products run on the matrix cores, in
+// blocks of 32 query rows and slabs of 32 keys, with the keys on the M side:
+//
+//   S^T[key, row]  = K[key, :] . Q[row, :]          A = K from LDS, B = Q (registers)
+//   O^T[d, row]   += V^T[d, keys] . P^T[keys, row]   A = V from LDS, B = P^T
+//
+// The accumulator of S^T (lane (row, h), register i: key 8 (i / 4) + 4 h + i % 4) is a B operand of the second product once that
+// product's keys are numbered the way the lane holds them, so the softmax weights never leave their lane.  bf16 rows, and 4-bit
+// rows, whose values are bf16 numbers: v_mfma_f32_32x32x16_bf16, weights rounded to bf16 (as much as the rounding of the output
+// loses).  fp32 rows: v_mfma_f32_32x32x2_f32 throughout.
+//
+// One pass over the keys with the running maximum and sum of every row in fp32.  The keys of all caches of a launch are cut into
+// work items of equal length, as the lengths on the device are (so a replayed launch is balanced too); each workgroup finds its
+// item by a scan over the lengths.  Caches of several items are merged by a kernel of their own.
+#include "common.h"
+#include "mxfp4.h"
+#include "tree.h"
+
+namespace baklava {
+
+namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+typedef float floatx4_t __attribute__((ext_vector_type(4)));
+typedef float floatx16_t __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x8_t __attribute__((ext_vector_type(8)));
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr float kNegInf = -__builtin_huge_valf();
+constexpr float kLowest = -3.402823466e38f;
+constexpr float kMaxSlack = 8.f;  // a logit may exceed its row's reference maximum by this much (log2 units)
+
+__device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Keys per LDS stage, by the rows' type, head dimension and the wavefronts that share 32 query rows.
+constexpr int tree_tile(int ks) { return ks == 4 ? 128 : 64; }
+// Whether four wavefronts may share 32 query rows: two stages of 128 rows of K and V have to fit the LDS.
+constexpr bool tree_shares_four(int type, int D) { return !(type == 1 && D == 128); }
+// Workgroups that fit a compute unit.
+constexpr int tree_resident(int type, int D, int ks) {
+  return 4 * tree_tile(ks) * D * (type == 1 ? 4 : 2) > 72 * 1024 ? 1 : 2;
+}
+
+__device__ __forceinline__ int tree_nodes(const TreeParams& p, int b) {
+  return p.n_nodes ? min(max(p.n_nodes[b], 0), p.N) : p.N;
+}
+
+// What follows from the rows' type (BAKLAVA_BF16, F32, MXFP4), the head dimension and KS, the wavefronts that share 32 query rows.
+template <int TYPE, int D, int KS>
+struct Shape {
+  static constexpr bool kF32 = TYPE == 1, kMx = TYPE == 2;
+  static constexpr int kRows = 32 * kWaves / KS;             // query rows of a workgroup
+  static constexpr int kTile = tree_tile(KS);       // keys per LDS stage
+  static constexpr int kSlabs = kTile / 32 / KS;             // slabs of 32 keys that a wavefront takes of it
+  static constexpr int kRow = D * (kF32 ? 4 : 2);            // bytes of a row in LDS
+  static constexpr int kPieces = kRow / 16;
+  static constexpr int kChunks = kPieces / 2;                // pieces of a row that a lane takes in the first product
+  static constexpr int kBlocks = D / 32;
+  static constexpr int kStage = kTile * kRow;                // bytes of a plane's stage
+  // direct copies into LDS: rows per instruction, instructions per wavefront and plane
+  static constexpr int kCopyRows = 64 / kPieces, kCopies = kTile / kWaves / kCopyRows;
+  // 4-bit rows: 16-byte pieces (32 codes) of a row, and per thread of a tile of both planes
+  static constexpr int kMxPieces = D / 32, kMxPer = 2 * kTile * kMxPieces / kThreads;
+  // Where piece `x` of a row lies in LDS: permuted so that the operand reads spread over the banks.
+  static __device__ __forceinline__ int k_slot(int row, int x) {
+    return kF32 || D == 128 ? x ^ (row & 15) : x ^ (row >> 1 & 7);
+  }
+  static __device__ __forceinline__ int v_slot(int row, int x) {
+    if (kF32) return x ^ 8 * (row >> 2 & 1);
+    return D == 128 ? x ^ 4 * (row & 3) : x ^ 4 * (row >> 1 & 1);
+  }
+};
+
+template <int TYPE, int D, int KS>
+__global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
+  using S = Shape<TYPE, D, KS>;
+  constexpr int kSlabs = S::kSlabs, kBlocks = S::kBlocks, kRow = S::kRow, kTile = S::kTile;
+  __shared__ __attribute__((aligned(16))) unsigned char lds_k[2][S::kStage];
+  __shared__ __attribute__((aligned(16))) unsigned char lds_v[2][S::kStage];
+  __shared__ unsigned long long above[kMostNodes / 64][kMostNodes];  // [word][node]: the nodes that a node sees
+  __shared__ int32_t scan[kWaves + 3];
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n32 = lane & 31, jh = lane >> 5;
+  // The workgroups of an item's query rows follow each other on one XCD (consecutive workgroups go round them).
+  const int group = (uint32_t)blockIdx.x / (uint32_t)(8 * p.row_tiles), in_group = (uint32_t)blockIdx.x % (uint32_t)(8 * p.row_tiles);
+  const int item = group * 8 + (in_group & 7), row_tile = in_group >> 3;
+  // Tiles of live rows, then those of drafted rows.
+  auto tiles = [&](int c) {
+    const int n = tree_nodes(p, (uint32_t)c / (uint32_t)p.Hkv % (uint32_t)p.batch);
+    return n > 0 ? (p.len[p.cache0 + c] + kTile - 1) / kTile + (n + kTile - 1) / kTile : 0;
+  };
+  Span sp;
+  if (!find_span<kThreads>(p.n_caches, p.target, p.least, item, tiles, scan, sp)) return;
+  const int h = sp.c_rel % p.Hkv, s_rel = sp.c_rel / p.Hkv, b = s_rel % p.batch;
+  const int n_nodes = __builtin_amdgcn_readfirstlane(tree_nodes(p, b)), n_rows = n_nodes * p.G;
+  const int n_live = __builtin_amdgcn_readfirstlane(p.len[p.cache0 + sp.c_rel]), live_tiles = (n_live + kTile - 1) / kTile;
+  const int r0 = row_tile * S::kRows;  // first query row of the workgroup
+  if (row_tile == 0 && sp.part == 0 && tid == 0) p.table[sp.c_rel] = make_int2(sp.slot, sp.n_parts);
+  if (r0 >= n_rows) return;
+  const int64_t row0 = uniform(p.off[p.cache0 + sp.c_rel]);
+
+  // ---- query rows ------------------------------------------------------------------------------
+  const int rw0 = r0 + wave / KS * 32;      // first row of this wavefront
+  const int sl0 = wave % KS * kSlabs;       // its first slab of a tile
+  const bool idle = rw0 >= n_rows;          // (such a wavefront helps with the copies)
+  const int row = min(rw0 + n32, n_rows - 1);  // rows past the last repeat it and are not written
+  const int node = row / p.G, head = h * p.G + row % p.G;
+  const unsigned char* Qr = reinterpret_cast<const unsigned char*>(p.q.data) + s_rel * p.q.seq + node * p.q.tok + head * p.q.head;
+  u32x4_t qb[S::kChunks];  // chunk c: piece 2 c + h of the row
+#pragma unroll
+  for (int c = 0; c < S::kChunks; ++c) qb[c] = *reinterpret_cast<const u32x4_t*>(Qr + c * 32 + jh * 16);
+
+  floatx16_t o[kBlocks];  // lane (row, h), register i of block b: O[row][32 b + 8 (i / 4) + 4 h + i % 4]
+#pragma unroll
+  for (int x = 0; x < kBlocks; ++x)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[x][i] = 0.f;
+  // Reference maximum of the exponent, log2 units.  It starts at the lowest finite value, so that a masked logit weighs 2^-inf = 0.
+  float m_ref = kLowest, l_part = 0.f;
+  const float cs = p.scale_log2e;
+
+  // ---- one tile from LDS -----------------------------------------------------------------------
+  auto logits = [&](floatx16_t (&s)[kSlabs], int buf) {
+    const unsigned char* base = lds_k[buf] + (sl0 * 32 + n32) * kRow;
+#pragma unroll
+    for (int c = 0; c < S::kChunks; ++c) {
+      const int slot = S::k_slot(n32, 2 * c + jh) * 16;  // (32 rows further the permutation is the same)
+#pragma unroll
+      for (int sl = 0; sl < kSlabs; ++sl) {
+        const u32x4_t a = *reinterpret_cast<const u32x4_t*>(base + sl * 32 * kRow + slot);
+        const floatx16_t zero = {};
+        if constexpr (S::kF32) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            s[sl] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]), __uint_as_float(qb[c][e]), c == 0 && e == 0 ? zero : s[sl], 0, 0, 0);
+        } else {
+          s[sl] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, qb[c]), c == 0 ? zero : s[sl], 0, 0, 0);
+        }
+      }
+    }
+  };
+  // Lazy running maximum: a row's reference only moves when a logit exceeds it by more than kMaxSlack, so weights stay below
+  // 2^kMaxSlack and the rescale of the accumulators is rare after the first tile.
+  auto follow_max = [&](const floatx16_t (&s)[kSlabs]) {
+    float mx = s[0][0];
+#pragma unroll
+    for (int sl = 0; sl < kSlabs; ++sl)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[sl][i]);
+    mx *= cs;
+    if (__any(mx > m_ref + kMaxSlack)) {
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      const float mn = fmaxf(m_ref, mx);
+      const float alpha = fast_exp2(m_ref - mn);
+      m_ref = mn;
+      l_part *= alpha;
+#pragma unroll
+      for (int x = 0; x < kBlocks; ++x) o[x] *= alpha;
+    }
+  };
+  // Weights of a slab and what they add to the outputs.  finite: infinite and NaN values count as zero (see add_seen).
+  auto outputs = [&](const floatx16_t& s, int buf, int sl, bool finite) {
+    const unsigned char* base = lds_v[buf] + (sl0 + sl) * 32 * kRow;
+    if constexpr (S::kF32) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float w = fast_exp2(fmaf(s[i], cs, -m_ref));
+        l_part += w;
+        const int key = 8 * (i / 4) + 4 * jh + i % 4;
+#pragma unroll
+        for (int x = 0; x < kBlocks; ++x) {
+          float v = *reinterpret_cast<const float*>(base + key * kRow + S::v_slot(key, 8 * x) * 16 + n32 * 4);
+          if (finite && (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) v = 0.f;
+          o[x] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w, o[x], 0, 0, 0);
+        }
+      }
+    } else {
+      // A transposed read hands lane m of a 16-lane group element m of the 16 d values the group points at, for 4 consecutive
+      // keys: the group (h, d half) reads keys 4 h .. + 3 of each 8, two reads per 16 keys.
+      const int n16 = lane & 15, half = (lane >> 4) & 1, k4 = n16 >> 2;
+      const unsigned char* at0 = base + (4 * jh + k4) * kRow + half * 32 + (n16 & 3) * 8;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        bf16x8_t pb;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float w = fast_exp2(fmaf(s[8 * u + e], cs, -m_ref));
+          l_part += w;
+          pb[e] = (__bf16)w;
+        }
+#pragma unroll
+        for (int x = 0; x < kBlocks; ++x) {
+          typedef __attribute__((address_space(3))) s16x4_t* lds_ptr_t;
+          const unsigned char* at = at0 + u * 16 * kRow + (D == 128 ? x ^ k4 : x ^ (k4 >> 1)) * 64;
+          const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)at);
+          const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(at + 8 * kRow));
+          s16x8_t v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+          if (finite) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if ((v[e] & 0x7f80) == 0x7f80) v[e] = 0;
+          }
+          o[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), pb, o[x], 0, 0, 0);
+        }
+      }
+    }
+  };
+
+  // ---- live rows into LDS ----------------------------------------------------------------------
+  const unsigned char* Kp = reinterpret_cast<const unsigned char*>(p.k_plane);
+  const unsigned char* Vp = reinterpret_cast<const unsigned char*>(p.v_plane);
+  constexpr int kStored = S::kMx ? D / 2 : kRow;  // bytes of a row in the arena
+  u32x4_t mx_codes_of[S::kMx ? S::kMxPer : 1];
+  uint32_t mx_byte[S::kMx ? S::kMxPer : 1];
+  uint32_t k_off[S::kCopies], v_off[S::kCopies], c_row[S::kCopies];
+  if constexpr (!S::kMx) {
+#pragma unroll
+    for (int i = 0; i < S::kCopies; ++i) {
+      const int r = wave * (kTile / kWaves) + i * S::kCopyRows + lane / S::kPieces, slot = lane % S::kPieces;
+      c_row[i] = r;
+      k_off[i] = S::k_slot(r, slot) * 16;
+      v_off[i] = S::v_slot(r, slot) * 16;
+    }
+  }
+  // Requests tile kt.  bf16 and fp32 rows go straight to LDS, 1 KiB in lane order per instruction (the permutation of a row's
+  // pieces is in the addresses); 4-bit rows go through registers, and `arrive` puts their values into LDS.  Rows past the last
+  // live one repeat it; they are masked.
+  auto request = [&](int kt) {
+    const uint32_t most = n_live - 1 - kt * kTile;
+    const int64_t first = row0 + (int64_t)kt * kTile;
+    if constexpr (S::kMx) {
+#pragma unroll
+      for (int i = 0; i < S::kMxPer; ++i) {
+        const int x = i * kThreads + tid, value = x / (kTile * S::kMxPieces), y = x % (kTile * S::kMxPieces);
+        const int64_t r = first + min((uint32_t)(y / S::kMxPieces), most);
+        mx_codes_of[i] = *reinterpret_cast<const u32x4_t*>((value ? Vp : Kp) + r * kStored + y % S::kMxPieces * 16);
+        mx_byte[i] = p.kv_scale[r * (D / 16) + value * (D / 32) + y % S::kMxPieces];
+      }
+    } else {
+      const unsigned char* ks = Kp + first * kStored;
+      const unsigned char* vs = Vp + first * kStored;
+      const uint32_t at = wave * (kTile / kWaves) * kRow;
+      const uint32_t lk = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds_k[kt & 1] + at;
+      const uint32_t lv = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds_v[kt & 1] + at;
+#pragma unroll
+      for (int i = 0; i < S::kCopies; ++i) {
+        const uint32_t r = min(c_row[i], most) * (uint32_t)kStored;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                     :: "s"(lk + i * 1024), "v"(r + k_off[i]), "s"(ks) : "memory", "m0");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                     :: "s"(lv + i * 1024), "v"(r + v_off[i]), "s"(vs) : "memory", "m0");
+      }
+    }
+  };
+  auto put_mx = [&](int buf, int value, int r, int piece, u32x4_t codes, uint32_t byte) {
+    unsigned char* dst = (value ? lds_v[buf] : lds_k[buf]) + r * kRow;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      *reinterpret_cast<uint4*>(dst + (value ? S::v_slot(r, 4 * piece + e) : S::k_slot(r, 4 * piece + e)) * 16) = mx_values(codes[e], mx_scale(byte));
+  };
+  auto arrive = [&](int kt) {
+    if constexpr (S::kMx) {
+#pragma unroll
+      for (int i = 0; i < S::kMxPer; ++i) {
+        const int x = i * kThreads + tid, value = x / (kTile * S::kMxPieces), y = x % (kTile * S::kMxPieces);
+        put_mx(kt & 1, value, y / S::kMxPieces, y % S::kMxPieces, mx_codes_of[i], mx_byte[i]);
+      }
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    __syncthreads();
+  };
+
+  const int live_end = min(sp.last, live_tiles);
+  if (sp.first < live_end) {
+    request(sp.first);
+    arrive(sp.first);
+    for (int kt = sp.first; kt < live_end; ++kt) {
+      if (kt + 1 < live_end) request(kt + 1);
+      if (!idle) {
+        floatx16_t s[kSlabs];
+        logits(s, kt & 1);
+        if ((kt + 1) * kTile > n_live) {
+#pragma unroll
+          for (int sl = 0; sl < kSlabs; ++sl)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (kt * kTile + (sl0 + sl) * 32 + 8 * (i / 4) + 4 * jh + i % 4 >= n_live) s[sl][i] = kNegInf;
+        }
+        follow_max(s);
+#pragma unroll
+        for (int sl = 0; sl < kSlabs; ++sl) outputs(s[sl], kt & 1, sl, false);
+      }
+      if (kt + 1 < live_end) arrive(kt + 1);
+    }
+  }
+
+  // ---- drafted rows ----------------------------------------------------------------------------
+  if (sp.last > live_tiles) {
+    // Who sees whom: bits of a node's ancestors by doubling, all nodes at once.  A parent that is no earlier node is none.
+    static_assert(kMostNodes == kThreads, "a thread for every node");
+    const int words = (n_nodes + 63) / 64;
+    int32_t* const jump = reinterpret_cast<int32_t*>(lds_k[0]);
+    __syncthreads();  // (the last tile has been read)
+    int up = -1;
+    if (tid < n_nodes) up = p.parent[(int64_t)b * p.N + tid];
+    if (up < 0 || up >= tid) up = -1;
+    jump[tid] = up;
+    for (int w = 0; w < words; ++w) above[w][tid] = tid / 64 == w ? 1ull << (tid & 63) : 0ull;
+    __syncthreads();
+    for (int reach = 1; reach < n_nodes; reach *= 2) {
+      unsigned long long more[kMostNodes / 64];
+      const int to = jump[tid];
+      int next = -1;
+      if (to >= 0) {
+        next = jump[to];
+#pragma unroll
+        for (int w = 0; w < kMostNodes / 64; ++w) more[w] = w < words ? above[w][to] : 0;
+      }
+      __syncthreads();
+      if (to >= 0) {
+        jump[tid] = next;
+#pragma unroll
+        for (int w = 0; w < kMostNodes / 64; ++w)
+          if (w < words) above[w][tid] |= more[w];
+      }
+      __syncthreads();
+    }
+    const int first_dt = max(sp.first - live_tiles, 0), last_dt = sp.last - live_tiles;
+    const unsigned char* Kd = reinterpret_cast<const unsigned char*>(p.k.data) + s_rel * p.k.seq + h * p.k.head;
+    const unsigned char* Vd = reinterpret_cast<const unsigned char*>(p.v.data) + s_rel * p.v.seq + h * p.v.head;
+    for (int dt = first_dt; dt < last_dt; ++dt) {
+      // Rows past the last node repeat it; nobody sees them.
+      bool wild = false;  // an infinite or NaN value
+      auto is_wild = [](uint32_t w) {
+        return S::kF32 ? (w & 0x7f800000u) == 0x7f800000u : (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+      };
+      constexpr int kGroup = S::kMx ? 4 : 1;  // pieces of a row that a thread takes together: those of a scale
+      for (int x = tid; x < 2 * kTile * S::kPieces / kGroup; x += kThreads) {
+        const int value = x / (kTile * S::kPieces / kGroup), y = x % (kTile * S::kPieces / kGroup);
+        const int r = y / (S::kPieces / kGroup), piece = y % (S::kPieces / kGroup);
+        const int j = min(dt * kTile + r, n_nodes - 1);
+        const unsigned char* src = (value ? Vd + j * p.v.tok : Kd + j * p.k.tok) + piece * kGroup * 16;
+        u32x4_t w[kGroup];
+#pragma unroll
+        for (int e = 0; e < kGroup; ++e) w[e] = *reinterpret_cast<const u32x4_t*>(src + e * 16);
+        if (value) {
+#pragma unroll
+          for (int e = 0; e < kGroup; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) wild = wild || is_wild(w[e][i]);
+        }
+        if constexpr (S::kMx) {  // rounded to 4 bits, as they will be in a cache
+          uint32_t top = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = max(top, max(w[e][i] & 0x7fffu, w[e][i] >> 16 & 0x7fffu));
+          const uint32_t byte = mx_scale_byte(top);
+          u32x4_t codes;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) codes[e] = mx_codes(make_uint4(w[e][0], w[e][1], w[e][2], w[e][3]), byte);
+          put_mx(0, value, r, piece, codes, byte);
+        } else {
+          *reinterpret_cast<u32x4_t*>((value ? lds_v[0] : lds_k[0]) + r * kRow + (value ? S::v_slot(r, piece) : S::k_slot(r, piece)) * 16) = w[0];
+        }
+      }
+      wild = __syncthreads_or(wild);
+      if (!idle) {
+        floatx16_t s[kSlabs];
+        logits(s, 0);
+        uint32_t seen[kSlabs];
+#pragma unroll
+        for (int sl = 0; sl < kSlabs; ++sl) {
+          const int key0 = dt * kTile + (sl0 + sl) * 32;
+          seen[sl] = key0 < n_nodes ? (uint32_t)(above[key0 / 64][node] >> (key0 & 32)) : 0u;
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (!(seen[sl] >> (8 * (i / 4) + 4 * jh + i % 4) & 1)) s[sl][i] = kNegInf;
+        }
+        follow_max(s);
+#pragma unroll
+        for (int sl = 0; sl < kSlabs; ++sl) {
+          outputs(s[sl], 0, sl, wild);
+          // An infinite or NaN value counts for the rows that see it, one by one: the product of a zero weight with it would reach
+          // all the others.
+          if (wild) {
+            for (int j = 0; j < 32; ++j) {
+              float w = 0.f;
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                if (8 * (i / 4) + i % 4 == (j & ~4)) w = fast_exp2(fmaf(s[sl][i], cs, -m_ref));
+              w = __shfl(w, n32 + 8 * (j & 4));  // from the half that holds key j
+              if (!(seen[sl] >> j & 1)) continue;
+              const int r = (sl0 + sl) * 32 + j;
+#pragma unroll
+              for (int x = 0; x < kBlocks; ++x)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                  const int d = 32 * x + 8 * (i / 4) + 4 * jh + i % 4;
+                  const unsigned char* src = lds_v[0] + r * kRow + S::v_slot(r, d * (S::kF32 ? 4 : 2) / 16) * 16;
+                  const float v = S::kF32 ? *reinterpret_cast<const float*>(src + d % 4 * 4)
+                                          : __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(src + d % 8 * 2) << 16);
+                  if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[x][i] = fmaf(w, v, o[x][i]);
+                }
+            }
+          }
+        }
+      }
+      __syncthreads();
+    }
+  }
+
+  // ---- the end of a work item ------------------------------------------------------------------
+  float l_tot = l_part + __shfl_xor(l_part, 32);
+  if constexpr (KS > 1) {  // the other wavefronts of the same rows hand over what they have
+    constexpr int kPart = kBlocks * 16 * 64;  // floats, [register][lane]
+    static_assert(sizeof(lds_v) >= kWaves * 64 * sizeof(float2), "maxima and sums");
+    static_assert(sizeof(lds_k) >= (kWaves / KS) * kPart * 4, "outputs of one wavefront of each block");
+    float* const o_sum = reinterpret_cast<float*>(&lds_k[0][0]) + wave / KS * kPart;
+    float2* const ml = reinterpret_cast<float2*>(&lds_v[0][0]) + wave * 64;
+#pragma unroll
+    for (int other = 1; other < KS; ++other) {
+      __syncthreads();
+      if (wave % KS == other) {
+        ml[lane] = make_float2(m_ref, l_tot);
+#pragma unroll
+        for (int x = 0; x < kBlocks; ++x)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o_sum[(x * 16 + i) * 64 + lane] = o[x][i];
+      }
+      __syncthreads();
+      if (wave % KS == 0) {
+        const float2 got = ml[other * 64 + lane];
+        const float m = fmaxf(m_ref, got.x), mine = fast_exp2(m_ref - m), theirs = fast_exp2(got.x - m);
+        m_ref = m;
+        l_tot = l_tot * mine + got.y * theirs;
+#pragma unroll
+        for (int x = 0; x < kBlocks; ++x)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[x][i] = o[x][i] * mine + o_sum[(x * 16 + i) * 64 + lane] * theirs;
+      }
+    }
+    if (wave % KS) return;
+  }
+  if (rw0 + n32 >= n_rows) return;
+  if (sp.n_parts == 1) {
+    const float inv = 1.f / l_tot;
+    if (p.lse.data && jh == 0)
+      *reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(p.lse.data) + s_rel * p.lse.seq + node * p.lse.tok + head * p.lse.head) =
+          m_ref + __builtin_log2f(l_tot);
+    unsigned char* dst = reinterpret_cast<unsigned char*>(p.out.data) + s_rel * p.out.seq + node * p.out.tok + head * p.out.head;
+#pragma unroll
+    for (int x = 0; x < kBlocks; ++x)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int d = 32 * x + 8 * q + 4 * jh;
+        if constexpr (S::kF32) {
+          floatx4_t r;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) r[i] = o[x][4 * q + i] * inv;
+          *reinterpret_cast<floatx4_t*>(dst + d * 4) = r;
+        } else {
+          bf16x4_t r;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) r[i] = (__bf16)(o[x][4 * q + i] * inv);
+          *reinterpret_cast<bf16x4_t*>(dst + d * 2) = r;
+        }
+      }
+  } else {
+    const int64_t at = (int64_t)(sp.slot + sp.part) * p.rows + row;
+    if (jh == 0) p.part_ml[at] = make_float2(m_ref, l_tot);
+#pragma unroll
+    for (int x = 0; x < kBlocks; ++x)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        floatx4_t r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = o[x][4 * q + i];
+        *reinterpret_cast<floatx4_t*>(p.part_o + at * D + 32 * x + 8 * q + 4 * jh) = r;
+      }
+  }
+}
+
+// Partials of caches that have several work items: D / 4 lanes for a query row.
+template <int D, bool F32>
+__global__ __launch_bounds__(kThreads) void tree_merge_kernel(TreeParams p) {
+  constexpr int kLanes = D / 4, kPer = kThreads / kLanes;
+  const int c_rel = blockIdx.x, s_rel = c_rel / p.Hkv, h = c_rel % p.Hkv, b = s_rel % p.batch;
+  const int n_nodes = tree_nodes(p, b);
+  const int row = blockIdx.y * kPer + threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4;
+  if (row >= n_nodes * p.G) return;
+  const int2 t = p.table[c_rel];  // (written for every sequence that has nodes)
+  if (t.y <= 1) return;
+  const float2* ml = p.part_ml + (int64_t)t.x * p.rows + row;
+  const float* part = p.part_o + ((int64_t)t.x * p.rows + row) * D + d;
+  float m = kLowest;
+  for (int i = 0; i < t.y; ++i) m = fmaxf(m, ml[(int64_t)i * p.rows].x);
+  float l = 0.f;
+  floatx4_t o = {0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < t.y; ++i) {
+    const float2 x = ml[(int64_t)i * p.rows];
+    const float a = fast_exp2(x.x - m);
+    l += x.y * a;
+    o += *reinterpret_cast<const floatx4_t*>(part + (int64_t)i * p.rows * D) * a;
+  }
+  const int node = row / p.G, head = h * p.G + row % p.G;
+  if (p.lse.data && d == 0)
+    *reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(p.lse.data) + s_rel * p.lse.seq + node * p.lse.tok + head * p.lse.head) =
+        m + __builtin_log2f(l);
+  unsigned char* dst = reinterpret_cast<unsigned char*>(p.out.data) + s_rel * p.out.seq + node * p.out.tok + head * p.out.head;
+  const float inv = 1.f / l;
+  if (F32) {
+    *reinterpret_cast<floatx4_t*>(dst + d * 4) = o * inv;
+  } else {
+    bf16x4_t r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = (__bf16)(o[i] * inv);
+    *reinterpret_cast<bf16x4_t*>(dst + d * 2) = r;
+  }
+}
+
+template <int TYPE, int D>
+hipError_t launch(const TreeParams& p, int ks, unsigned grid, hipStream_t s) {
+  if (ks == 1) tree_attn_kernel<TYPE, D, 1><<<dim3(grid), dim3(kThreads), 0, s>>>(p);
+  else if (ks == 2 || !tree_shares_four(TYPE, D)) tree_attn_kernel<TYPE, D, 2><<<dim3(grid), dim3(kThreads), 0, s>>>(p);
+  else if constexpr (tree_shares_four(TYPE, D)) tree_attn_kernel<TYPE, D, 4><<<dim3(grid), dim3(kThreads), 0, s>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+TreeLaunch tree_launch(int type, int D, int rows, int n_cus) {
+  TreeLaunch t;
+  t.ks = rows <= 32 && tree_shares_four(type, D) ? 4 : rows <= 64 ? 2 : 1;
+  const int per = 32 * kWaves / t.ks;
+  t.row_tiles = (rows + per - 1) / per;
+  const int resident = tree_resident(type, D, t.ks);
+  t.target = resident * n_cus / t.row_tiles > 1 ? resident * n_cus / t.row_tiles : 1;
+  return t;
+}
+
+hipError_t launch_tree_attn(const TreeParams& p, const TreeLaunch& t, int type, int D, int n_caches, hipStream_t s) {
+  const int64_t grid = ((int64_t)t.target + n_caches + 7) / 8 * 8 * t.row_tiles;
+  const int per = kThreads / (D / 4), merge_rows = (p.rows + per - 1) / per;
+  if (grid > INT32_MAX / kThreads || merge_rows > 65535) return hipErrorInvalidValue;
+  hipError_t e = type == 1   ? D == 128 ? launch<1, 128>(p, t.ks, (unsigned)grid, s) : launch<1, 64>(p, t.ks, (unsigned)grid, s)
+                 : type == 2 ? D == 128 ? launch<2, 128>(p, t.ks, (unsigned)grid, s) : launch<2, 64>(p, t.ks, (unsigned)grid, s)
+                             : D == 128 ? launch<0, 128>(p, t.ks, (unsigned)grid, s) : launch<0, 64>(p, t.ks, (unsigned)grid, s);
+  if (e != hipSuccess) return e;
+  const dim3 mg((unsigned)n_caches, (unsigned)merge_rows);
+  if (type == 1) {
+    if (D == 128) tree_merge_kernel<128, true><<<mg, dim3(kThreads), 0, s>>>(p);
+    else tree_merge_kernel<64, true><<<mg, dim3(kThreads), 0, s>>>(p);
+  } else {
+    if (D == 128) tree_merge_kernel<128, false><<<mg, dim3(kThreads), 0, s>>>(p);
+    else tree_merge_kernel<64, false><<<mg, dim3(kThreads), 0, s>>>(p);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace baklava
