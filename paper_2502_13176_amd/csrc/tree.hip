@@ -34,6 +34,7 @@ typedef short s16x8_t __attribute__((ext_vector_type(8)));
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLowest = -3.402823466e38f;
+constexpr int kMostParts = 512;   // work items of a launch that are aimed at, and therefore of a cache, at most
 constexpr float kMaxSlack = 8.f;  // a logit may exceed its row's reference maximum by this much (log2 units)
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -490,28 +491,69 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
   }
 }
 
-// Partials of caches that have several work items: D / 4 lanes for a query row.
+// Partials of caches that have several work items.  D / 4 lanes take a query row's elements, kGroups of them its work items in
+// turn: with a workgroup to kMergeRows rows a small launch still has a few hundred wavefronts, each with four loads on the way.
+constexpr int kMergeRows = 2;
 template <int D, bool F32>
 __global__ __launch_bounds__(kThreads) void tree_merge_kernel(TreeParams p) {
-  constexpr int kLanes = D / 4, kPer = kThreads / kLanes;
+  constexpr int kLanes = D / 4, kPer = kThreads / kMergeRows, kGroups = kPer / kLanes;
+  __shared__ float weight[kMergeRows][kMostParts];
+  __shared__ float2 sums[kMergeRows][kPer / 64];
+  __shared__ floatx4_t part_sum[kMergeRows][kGroups][kLanes];
   const int c_rel = blockIdx.x, s_rel = c_rel / p.Hkv, h = c_rel % p.Hkv, b = s_rel % p.batch;
-  const int n_nodes = tree_nodes(p, b);
-  const int row = blockIdx.y * kPer + threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4;
-  if (row >= n_nodes * p.G) return;
+  const int n_rows = tree_nodes(p, b) * p.G;
+  const int r0 = blockIdx.y * kMergeRows;
+  if (r0 >= n_rows) return;
   const int2 t = p.table[c_rel];  // (written for every sequence that has nodes)
-  if (t.y <= 1) return;
+  const int n_parts = t.y;
+  if (n_parts <= 1) return;
+  const int tid = threadIdx.x, at = tid / kPer, in = tid % kPer;
+  const int row = min(r0 + at, n_rows - 1);  // (a row past the last repeats it)
   const float2* ml = p.part_ml + (int64_t)t.x * p.rows + row;
-  const float* part = p.part_o + ((int64_t)t.x * p.rows + row) * D + d;
+  // weights of the items: 2^(m_i - m)
   float m = kLowest;
-  for (int i = 0; i < t.y; ++i) m = fmaxf(m, ml[(int64_t)i * p.rows].x);
-  float l = 0.f;
-  floatx4_t o = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < t.y; ++i) {
-    const float2 x = ml[(int64_t)i * p.rows];
-    const float a = fast_exp2(x.x - m);
-    l += x.y * a;
-    o += *reinterpret_cast<const floatx4_t*>(part + (int64_t)i * p.rows * D) * a;
+  for (int i = in; i < n_parts; i += kPer) {
+    const float x = ml[(int64_t)i * p.rows].x;
+    weight[at][i] = x;
+    m = fmaxf(m, x);
   }
+#pragma unroll
+  for (int i = 32; i >= 1; i /= 2) m = fmaxf(m, __shfl_xor(m, i));
+  if (tid % 64 == 0) sums[at][in / 64].x = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kPer / 64; ++w) m = fmaxf(m, sums[at][w].x);
+  float l = 0.f;
+  for (int i = in; i < n_parts; i += kPer) {
+    const float a = fast_exp2(weight[at][i] - m);
+    weight[at][i] = a;
+    l += ml[(int64_t)i * p.rows].y * a;
+  }
+#pragma unroll
+  for (int i = 32; i >= 1; i /= 2) l += __shfl_xor(l, i);
+  if (tid % 64 == 0) sums[at][in / 64].y = l;
+  __syncthreads();
+  l = 0.f;
+#pragma unroll
+  for (int w = 0; w < kPer / 64; ++w) l += sums[at][w].y;
+  const int d = in % kLanes, group = in / kLanes;
+  const floatx4_t* part = reinterpret_cast<const floatx4_t*>(p.part_o + ((int64_t)t.x * p.rows + row) * D) + d;
+  const int64_t step = (int64_t)p.rows * (D / 4);
+  floatx4_t o = {0.f, 0.f, 0.f, 0.f};
+  int i = group;
+  for (; i + 3 * kGroups < n_parts; i += 4 * kGroups) {
+    floatx4_t x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = part[(i + e * kGroups) * step];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o += x[e] * weight[at][i + e * kGroups];
+  }
+  for (; i < n_parts; i += kGroups) o += part[i * step] * weight[at][i];
+  part_sum[at][group][d] = o;
+  __syncthreads();
+  if (group != 0 || r0 + at >= n_rows) return;
+#pragma unroll
+  for (int g = 1; g < kGroups; ++g) o += part_sum[at][g][d];
   const int node = row / p.G, head = h * p.G + row % p.G;
   if (p.lse.data && d == 0)
     *reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(p.lse.data) + s_rel * p.lse.seq + node * p.lse.tok + head * p.lse.head) =
@@ -519,12 +561,12 @@ __global__ __launch_bounds__(kThreads) void tree_merge_kernel(TreeParams p) {
   unsigned char* dst = reinterpret_cast<unsigned char*>(p.out.data) + s_rel * p.out.seq + node * p.out.tok + head * p.out.head;
   const float inv = 1.f / l;
   if (F32) {
-    *reinterpret_cast<floatx4_t*>(dst + d * 4) = o * inv;
+    reinterpret_cast<floatx4_t*>(dst)[d] = o * inv;
   } else {
     bf16x4_t r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = (__bf16)(o[i] * inv);
-    *reinterpret_cast<bf16x4_t*>(dst + d * 2) = r;
+    for (int e = 0; e < 4; ++e) r[e] = (__bf16)(o[e] * inv);
+    reinterpret_cast<bf16x4_t*>(dst)[d] = r;
   }
 }
 
@@ -544,13 +586,14 @@ TreeLaunch tree_launch(int type, int D, int rows, int n_cus) {
   const int per = 32 * kWaves / t.ks;
   t.row_tiles = (rows + per - 1) / per;
   const int resident = tree_resident(type, D, t.ks);
-  t.target = resident * n_cus / t.row_tiles > 1 ? resident * n_cus / t.row_tiles : 1;
+  const int all = resident * n_cus < kMostParts ? resident * n_cus : kMostParts;
+  t.target = all / t.row_tiles > 1 ? all / t.row_tiles : 1;
   return t;
 }
 
 hipError_t launch_tree_attn(const TreeParams& p, const TreeLaunch& t, int type, int D, int n_caches, hipStream_t s) {
   const int64_t grid = ((int64_t)t.target + n_caches + 7) / 8 * 8 * t.row_tiles;
-  const int per = kThreads / (D / 4), merge_rows = (p.rows + per - 1) / per;
+  const int merge_rows = (p.rows + kMergeRows - 1) / kMergeRows;
   if (grid > INT32_MAX / kThreads || merge_rows > 65535) return hipErrorInvalidValue;
   hipError_t e = type == 1   ? D == 128 ? launch<1, 128>(p, t.ks, (unsigned)grid, s) : launch<1, 64>(p, t.ks, (unsigned)grid, s)
                  : type == 2 ? D == 128 ? launch<2, 128>(p, t.ks, (unsigned)grid, s) : launch<2, 64>(p, t.ks, (unsigned)grid, s)
