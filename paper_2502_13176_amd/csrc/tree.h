@@ -42,24 +42,34 @@ __device__ __forceinline__ int scan_threads(int x, int32_t* lds, int& total) {
   return x + before;
 }
 
-// The item number `item` of n_caches caches of tiles(c) tiles each; false: there is none.  Items have at most
-// run = max(least, all tiles / target, rounded up) tiles, so there are at most target + n_caches; the items of a cache are of equal
-// length but for one tile.  Partial slots go to the caches of several items alone, which have fewer than 2 target of them
-// (ceil(x) < 2 x for x > 1).  lds: THREADS / 64 + 3 words, free for other use behind the next barrier.
+// The item number `item` of n_caches caches of tiles(c) tiles each; false: there is none.  Items have at most `run` tiles: at least
+// `least`, and all tiles / target, so that there are at most target + n_caches.  Where there are few caches run grows until there
+// are at most target: a launch of one round of workgroups would otherwise take a second one for a few of them.  The items of a cache
+// are of equal length but for one tile.  Partial slots go to the caches of several items alone, which have fewer than 2 target of
+// them (ceil(x) < 2 x for x > 1).  lds: THREADS / 64 + 3 words, free for other use behind the next barrier.
 template <int THREADS, class Tiles>
 __device__ __forceinline__ bool find_span(int n_caches, int target, int least, int item, const Tiles& tiles, int32_t* lds, Span& sp) {
   constexpr int kAt = THREADS / 64;
   const int tid = threadIdx.x;
-  int all = 0;
-  for (int c = tid; c < n_caches; c += THREADS) all += tiles(c);
+  const int mine = tid < n_caches ? tiles(tid) : 0;  // (of the first caches, often all of them)
+  int all = mine;
+  for (int c = tid + THREADS; c < n_caches; c += THREADS) all += tiles(c);
   int total;
   scan_threads<THREADS>(all, lds, total);
-  const int run = max((total + target - 1) / target, least);
+  int run = max((total + target - 1) / target, least);
+  if (2 * n_caches <= target && n_caches <= THREADS) {
+    for (int i = 0; i < 4; ++i) {
+      int count;
+      scan_threads<THREADS>((mine + run - 1) / run, lds, count);
+      if (count <= target) break;
+      run += max(1, (int)((int64_t)run * (count - target) / target));
+    }
+  }
   if (tid == 0) lds[kAt] = -1;
   int items0 = 0, slots0 = 0;
   for (int c0 = 0; c0 < n_caches; c0 += THREADS) {
     const int c = c0 + tid;
-    const int t = c < n_caches ? tiles(c) : 0;
+    const int t = c0 == 0 ? mine : c < n_caches ? tiles(c) : 0;
     const int parts = (t + run - 1) / run;
     int n_items, n_slots;
     const int end = items0 + scan_threads<THREADS>(parts, lds, n_items);

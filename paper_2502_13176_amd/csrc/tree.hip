@@ -66,8 +66,8 @@ struct Shape {
   static constexpr int kStage = kTile * kRow;                // bytes of a plane's stage
   // direct copies into LDS: rows per instruction, instructions per wavefront and plane
   static constexpr int kCopyRows = 64 / kPieces, kCopies = kTile / kWaves / kCopyRows;
-  // 4-bit rows: 16-byte pieces (32 codes) of a row, and per thread of a tile of both planes
-  static constexpr int kMxPieces = D / 32, kMxPer = 2 * kTile * kMxPieces / kThreads;
+  // 4-bit rows: 16-byte pieces (32 codes) of a row, and per thread of a plane's tile
+  static constexpr int kMxPieces = D / 32, kMxPer = (kTile * kMxPieces + kThreads - 1) / kThreads;
   // Where piece `x` of a row lies in LDS: permuted so that the operand reads spread over the banks.
   static __device__ __forceinline__ int k_slot(int row, int x) {
     return kF32 || D == 128 ? x ^ (row & 15) : x ^ (row >> 1 & 7);
@@ -150,13 +150,15 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
   };
   // Lazy running maximum: a row's reference only moves when a logit exceeds it by more than kMaxSlack, so weights stay below
   // 2^kMaxSlack and the rescale of the accumulators is rare after the first tile.
-  auto follow_max = [&](const floatx16_t (&s)[kSlabs]) {
+  auto max_of = [&](const floatx16_t (&s)[kSlabs]) {
     float mx = s[0][0];
 #pragma unroll
     for (int sl = 0; sl < kSlabs; ++sl)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[sl][i]);
-    mx *= cs;
+    return mx * cs;
+  };
+  auto follow_max = [&](float mx) {
     if (__any(mx > m_ref + kMaxSlack)) {
       mx = fmaxf(mx, __shfl_xor(mx, 32));
       const float mn = fmaxf(m_ref, mx);
@@ -219,8 +221,6 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
   const unsigned char* Kp = reinterpret_cast<const unsigned char*>(p.k_plane);
   const unsigned char* Vp = reinterpret_cast<const unsigned char*>(p.v_plane);
   constexpr int kStored = S::kMx ? D / 2 : kRow;  // bytes of a row in the arena
-  u32x4_t mx_codes_of[S::kMx ? S::kMxPer : 1];
-  uint32_t mx_byte[S::kMx ? S::kMxPer : 1];
   uint32_t k_off[S::kCopies], v_off[S::kCopies], c_row[S::kCopies];
   if constexpr (!S::kMx) {
 #pragma unroll
@@ -231,34 +231,32 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
       v_off[i] = S::v_slot(r, slot) * 16;
     }
   }
-  // Requests tile kt.  bf16 and fp32 rows go straight to LDS, 1 KiB in lane order per instruction (the permutation of a row's
-  // pieces is in the addresses); 4-bit rows go through registers, and `arrive` puts their values into LDS.  Rows past the last
-  // live one repeat it; they are masked.
-  auto request = [&](int kt) {
+  // bf16 and fp32 rows go straight to LDS, 1 KiB in lane order per instruction (the permutation of a row's pieces is in the
+  // addresses); 4-bit rows go through registers, and `put` puts their values into LDS.  Rows past the last live one repeat it;
+  // they are masked.
+  struct Codes {
+    u32x4_t c[S::kMx ? S::kMxPer : 1];
+    uint32_t byte[S::kMx ? S::kMxPer : 1];
+  } codes_k, codes_v;
+  auto request = [&](Codes& codes, int value, int kt) {
     const uint32_t most = n_live - 1 - kt * kTile;
     const int64_t first = row0 + (int64_t)kt * kTile;
+    const unsigned char* src = (value ? Vp : Kp) + first * kStored;
     if constexpr (S::kMx) {
+      const uint8_t* scale = p.kv_scale + first * (D / 16) + value * (D / 32);
 #pragma unroll
       for (int i = 0; i < S::kMxPer; ++i) {
-        const int x = i * kThreads + tid, value = x / (kTile * S::kMxPieces), y = x % (kTile * S::kMxPieces);
-        const int64_t r = first + min((uint32_t)(y / S::kMxPieces), most);
-        mx_codes_of[i] = *reinterpret_cast<const u32x4_t*>((value ? Vp : Kp) + r * kStored + y % S::kMxPieces * 16);
-        mx_byte[i] = p.kv_scale[r * (D / 16) + value * (D / 32) + y % S::kMxPieces];
+        const uint32_t x = i * kThreads + tid, r = min(x / S::kMxPieces, most), piece = x % S::kMxPieces;
+        codes.c[i] = *reinterpret_cast<const u32x4_t*>(src + (r * kStored + piece * 16));
+        codes.byte[i] = scale[r * (D / 16) + piece];
       }
     } else {
-      const unsigned char* ks = Kp + first * kStored;
-      const unsigned char* vs = Vp + first * kStored;
-      const uint32_t at = wave * (kTile / kWaves) * kRow;
-      const uint32_t lk = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds_k[kt & 1] + at;
-      const uint32_t lv = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds_v[kt & 1] + at;
+      const uint32_t dst = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)(value ? lds_v[kt & 1] : lds_k[kt & 1]) +
+                           wave * (kTile / kWaves) * kRow;
 #pragma unroll
-      for (int i = 0; i < S::kCopies; ++i) {
-        const uint32_t r = min(c_row[i], most) * (uint32_t)kStored;
+      for (int i = 0; i < S::kCopies; ++i)
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                     :: "s"(lk + i * 1024), "v"(r + k_off[i]), "s"(ks) : "memory", "m0");
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                     :: "s"(lv + i * 1024), "v"(r + v_off[i]), "s"(vs) : "memory", "m0");
-      }
+                     :: "s"(dst + i * 1024), "v"(min(c_row[i], most) * (uint32_t)kStored + (value ? v_off[i] : k_off[i])), "s"(src) : "memory", "m0");
     }
   };
   auto put_mx = [&](int buf, int value, int r, int piece, u32x4_t codes, uint32_t byte) {
@@ -267,28 +265,65 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
     for (int e = 0; e < 4; ++e)
       *reinterpret_cast<uint4*>(dst + (value ? S::v_slot(r, 4 * piece + e) : S::k_slot(r, 4 * piece + e)) * 16) = mx_values(codes[e], mx_scale(byte));
   };
-  auto arrive = [&](int kt) {
+  auto put = [&](const Codes& codes, int value, int kt) {
     if constexpr (S::kMx) {
 #pragma unroll
       for (int i = 0; i < S::kMxPer; ++i) {
-        const int x = i * kThreads + tid, value = x / (kTile * S::kMxPieces), y = x % (kTile * S::kMxPieces);
-        put_mx(kt & 1, value, y / S::kMxPieces, y % S::kMxPieces, mx_codes_of[i], mx_byte[i]);
+        const int x = i * kThreads + tid;
+        if (x < kTile * S::kMxPieces) put_mx(kt & 1, value, x / S::kMxPieces, x % S::kMxPieces, codes.c[i], codes.byte[i]);
       }
-    } else {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
+  };
+  auto arrive = [&]() {
+    if constexpr (!S::kMx) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   };
 
+  // ---- live rows: a software pipeline, the first product of tile kt + 1 beside the exponentials of tile kt -------------------
   const int live_end = min(sp.last, live_tiles);
   if (sp.first < live_end) {
-    request(sp.first);
-    arrive(sp.first);
-    for (int kt = sp.first; kt < live_end; ++kt) {
-      if (kt + 1 < live_end) request(kt + 1);
+    int kt = sp.first;
+    const bool two = kt + 1 < live_end;
+    request(codes_k, 0, kt);
+    request(codes_v, 1, kt);
+    put(codes_k, 0, kt);
+    put(codes_v, 1, kt);
+    if (two) {
+      request(codes_k, 0, kt + 1);
+      put(codes_k, 0, kt + 1);
+    }
+    arrive();
+    floatx16_t s[kSlabs];
+    float mx = kLowest;
+    if (!idle) {
+      logits(s, kt & 1);
+      mx = max_of(s);
+    }
+    __syncthreads();  // (the first tile's K rows are overwritten in the first step)
+    auto step = [&](const floatx16_t (&s)[kSlabs], floatx16_t (&sn)[kSlabs], int kt) {
+      request(codes_k, 0, kt + 2);
+      request(codes_v, 1, kt + 1);
       if (!idle) {
-        floatx16_t s[kSlabs];
-        logits(s, kt & 1);
+        follow_max(mx);
+        logits(sn, kt + 1 & 1);
+#pragma unroll
+        for (int sl = 0; sl < kSlabs; ++sl) outputs(s[sl], kt & 1, sl, false);
+        mx = max_of(sn);
+      }
+      put(codes_k, 0, kt + 2);
+      put(codes_v, 1, kt + 1);
+      arrive();
+    };
+    for (; kt + 3 < live_end; kt += 2) {
+      floatx16_t sn[kSlabs];
+      step(s, sn, kt);
+      step(sn, s, kt + 1);
+    }
+    for (; kt < live_end; ++kt) {
+      const bool more = kt + 1 < live_end, more_k = kt + 2 < live_end;
+      if (more_k) request(codes_k, 0, kt + 2);
+      if (more) request(codes_v, 1, kt + 1);
+      if (!idle) {
         if ((kt + 1) * kTile > n_live) {
 #pragma unroll
           for (int sl = 0; sl < kSlabs; ++sl)
@@ -296,11 +331,14 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
             for (int i = 0; i < 16; ++i)
               if (kt * kTile + (sl0 + sl) * 32 + 8 * (i / 4) + 4 * jh + i % 4 >= n_live) s[sl][i] = kNegInf;
         }
-        follow_max(s);
+        follow_max(max_of(s));
 #pragma unroll
         for (int sl = 0; sl < kSlabs; ++sl) outputs(s[sl], kt & 1, sl, false);
+        if (more) logits(s, kt + 1 & 1);
       }
-      if (kt + 1 < live_end) arrive(kt + 1);
+      if (more_k) put(codes_k, 0, kt + 2);
+      if (more) put(codes_v, 1, kt + 1);
+      arrive();
     }
   }
 
@@ -387,7 +425,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
           for (int i = 0; i < 16; ++i)
             if (!(seen[sl] >> (8 * (i / 4) + 4 * jh + i % 4) & 1)) s[sl][i] = kNegInf;
         }
-        follow_max(s);
+        follow_max(max_of(s));
 #pragma unroll
         for (int sl = 0; sl < kSlabs; ++sl) {
           outputs(s[sl], 0, sl, wild);
