@@ -101,7 +101,7 @@ __global__ __launch_bounds__(kThreads, 2) void accept_scores_kernel(AcceptParams
     return t.y > 0 ? (t.x + t.y + kTile - 1) / kTile : 0;
   };
   Span sp;
-  if (!find_span<kThreads>(p.n_caches, p.target, p.least, blockIdx.x, tiles, scan, sp)) return;
+  if (!find_span<kThreads>(p.n_caches, p.target, 1, blockIdx.x, tiles, scan, sp)) return;
   const int h = sp.c_rel % p.Hkv, s_rel = sp.c_rel / p.Hkv, b = s_rel % p.batch;
   const int2 t = p.table[sp.c_rel];
   const int n_old = __builtin_amdgcn_readfirstlane(t.x), n_path = __builtin_amdgcn_readfirstlane(t.y);
@@ -243,7 +243,6 @@ hipError_t launch_append_accepted(const AcceptParams& p_in, int type, int D, int
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.table) return e;
   p.target = 2 * n_cus;
-  p.least = 1;
   const unsigned grid = (unsigned)p.target + (unsigned)p.n_caches;
   if (grid > INT32_MAX / kThreads) return hipErrorInvalidValue;
   return type == 1   ? D == 128 ? launch_scores<1, 128>(p, grid, s) : launch_scores<1, 64>(p, grid, s)

@@ -1201,7 +1201,7 @@ extern "C" int baklava_tree_attn(baklava_ctx* ctx, int32_t layer_begin, int32_t 
   p.cache0 = layer_begin * ctx->cpl; p.n_caches = layer_count * ctx->cpl;
   p.rows = N * ctx->G;
   const TreeLaunch t = tree_launch(ctx->d.dtype, D, p.rows, ctx->n_cus);
-  p.row_tiles = t.row_tiles; p.target = t.target; p.least = 1;
+  p.row_tiles = t.row_tiles; p.target = t.target;
   p.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)D));
   if (!hip_ok(launch_tree_attn(p, t, ctx->d.dtype, D, p.n_caches, (hipStream_t)stream))) return BAKLAVA_EHIP;
   return BAKLAVA_OK;

@@ -249,13 +249,14 @@ struct TreeParams {
   int32_t rows;             // N * G
   int32_t row_tiles;        // workgroups of a work item
   int32_t target;           // work items of the launch, about
-  int32_t least;            // tiles of a work item, at least where its cache has several
   float scale_log2e;
 };
 // How a launch over query rows of this many is cut: wavefronts that share 32 of them, workgroups of a work item, work items.
 struct TreeLaunch {
-  int ks, row_tiles, target;
+  int ks, row_tiles, target;  // ks 0: the streaming kernel
 };
+constexpr int kMostTreeItems = 512;   // work items of a launch that are aimed at, and therefore of a cache, at most
+constexpr int kStreamRows = 64;       // query rows that the streaming kernel takes
 
 constexpr int kAcceptRows = kMostNodes * 16;  // query rows of a path
 struct AcceptParams {
@@ -276,7 +277,7 @@ struct AcceptParams {
   int2* table;              // [n_caches] of a cache: live rows before, new rows; null: scores are not tracked
   int32_t N, G, Hkv, batch;
   int32_t cache0, n_caches;
-  int32_t target, least;
+  int32_t target;
   float scale_log2e;
 };
 
@@ -390,6 +391,7 @@ hipError_t launch_prompt_attn(const PromptParams& p, int D, int tile_tokens, int
 hipError_t launch_append_prompt(const PromptRowsParams& p, int pieces, bool mx, int n_seq, int most, hipStream_t s);
 hipError_t launch_read_rows(const ReadRowsParams& p, int pieces, bool mx, int n_caches, hipStream_t s);
 TreeLaunch tree_launch(int type, int D, int rows, int n_cus);
+hipError_t launch_tree_stream(const TreeParams& p, int type, int D, int n_items, hipStream_t s);
 hipError_t launch_tree_attn(const TreeParams& p, const TreeLaunch& t, int type, int D, int n_caches, hipStream_t s);
 hipError_t launch_append_accepted(const AcceptParams& p, int type, int D, int n_cus, hipStream_t s);
 constexpr int kVerifyPart = 8192;  // elements of a row that a workgroup takes

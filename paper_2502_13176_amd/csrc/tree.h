@@ -19,15 +19,20 @@ struct Span {
   int c_rel, first, last, part, n_parts, slot;
 };
 
-// Sum of x over the workgroup's threads up to and with the calling one, and over all of them.
-template <int THREADS>
-__device__ __forceinline__ int scan_threads(int x, int32_t* lds, int& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__device__ __forceinline__ int scan_wave(int x) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int i = 1; i < 64; i *= 2) {
     const int y = __shfl_up(x, i);
     x += lane >= i ? y : 0;
   }
+  return x;
+}
+// Sum of x over the workgroup's threads up to and with the calling one, and over all of them.
+template <int THREADS>
+__device__ __forceinline__ int scan_threads(int x, int32_t* lds, int& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  x = scan_wave(x);
   __syncthreads();  // (lds may still be read)
   if (lane == 63) lds[wave] = x;
   __syncthreads();
@@ -42,59 +47,129 @@ __device__ __forceinline__ int scan_threads(int x, int32_t* lds, int& total) {
   return x + before;
 }
 
-// The item number `item` of n_caches caches of tiles(c) tiles each; false: there is none.  Items have at most `run` tiles: at least
-// `least`, and all tiles / target, so that there are at most target + n_caches.  Where there are few caches run grows until there
-// are at most target: a launch of one round of workgroups would otherwise take a second one for a few of them.  The items of a cache
-// are of equal length but for one tile.  Partial slots go to the caches of several items alone, which have fewer than 2 target of
-// them (ceil(x) < 2 x for x > 1).  lds: THREADS / 64 + 3 words, free for other use behind the next barrier.
+// The item number `item` of n_caches caches of tiles(c) tiles each; false: there is none.  Items have at most `run` tiles: a
+// multiple of `unit`, and all tiles / target at least, so that there are at most target + n_caches.  Where there are few caches run
+// grows until there are at most target: a launch of one round of workgroups would otherwise take a second one for a few of them.
+// The items of a cache are of equal length but for one tile.  Partial slots go to the caches of several items alone, which have
+// fewer than 2 target of them (ceil(x) < 2 x for x > 1).  lds: THREADS / 64 + 3 words, free for other use behind the next barrier.
 template <int THREADS, class Tiles>
-__device__ __forceinline__ bool find_span(int n_caches, int target, int least, int item, const Tiles& tiles, int32_t* lds, Span& sp) {
+__device__ __forceinline__ bool find_span(int n_caches, int target, int unit, int item, const Tiles& tiles, int32_t* lds, Span& sp) {
   constexpr int kAt = THREADS / 64;
-  const int tid = threadIdx.x;
-  const int mine = tid < n_caches ? tiles(tid) : 0;  // (of the first caches, often all of them)
-  int all = mine;
-  for (int c = tid + THREADS; c < n_caches; c += THREADS) all += tiles(c);
-  int total;
-  scan_threads<THREADS>(all, lds, total);
-  int run = max((total + target - 1) / target, least);
-  if (2 * n_caches <= target && n_caches <= THREADS) {
-    for (int i = 0; i < 4; ++i) {
-      int count;
-      scan_threads<THREADS>((mine + run - 1) / run, lds, count);
-      if (count <= target) break;
-      run += max(1, (int)((int64_t)run * (count - target) / target));
+  auto next_run = [&](int run, int count) { return (run + max(1, (int)((int64_t)run * (count - target) / target)) + unit - 1) / unit * unit; };
+  int run, t;
+  if (n_caches <= 64) {  // every wavefront for itself
+    const int lane = threadIdx.x & 63;
+    const int mine = lane < n_caches ? tiles(lane) : 0;
+    run = max((__builtin_amdgcn_readlane(scan_wave(mine), 63) + target - 1) / target, 1);
+    run = (run + unit - 1) / unit * unit;
+    int parts = (mine + run - 1) / run, end = scan_wave(parts);
+    if (2 * n_caches <= target) {
+      for (int i = 0; i < 4; ++i) {
+        const int count = __builtin_amdgcn_readlane(end, 63);
+        if (count <= target) break;
+        run = next_run(run, count);
+        parts = (mine + run - 1) / run;
+        end = scan_wave(parts);
+      }
     }
-  }
-  if (tid == 0) lds[kAt] = -1;
-  int items0 = 0, slots0 = 0;
-  for (int c0 = 0; c0 < n_caches; c0 += THREADS) {
-    const int c = c0 + tid;
-    const int t = c0 == 0 ? mine : c < n_caches ? tiles(c) : 0;
-    const int parts = (t + run - 1) / run;
-    int n_items, n_slots;
-    const int end = items0 + scan_threads<THREADS>(parts, lds, n_items);
-    const int slot_end = slots0 + scan_threads<THREADS>(parts > 1 ? parts : 0, lds, n_slots);
-    if (item < end && item >= end - parts) {
-      lds[kAt] = c;
-      lds[kAt + 1] = slot_end - (parts > 1 ? parts : 0);
-      lds[kAt + 2] = item - (end - parts);
+    const int slots = parts > 1 ? parts : 0, slot_end = scan_wave(slots);
+    const unsigned long long hit = __ballot(item < end && item >= end - parts);
+    if (!hit) return false;
+    const int c = __builtin_ctzll(hit);
+    sp.c_rel = c;
+    sp.slot = __builtin_amdgcn_readlane(slot_end - slots, c);
+    sp.part = item - __builtin_amdgcn_readlane(end - parts, c);
+    t = __builtin_amdgcn_readlane(mine, c);
+  } else {
+    const int tid = threadIdx.x;
+    const int mine = tid < n_caches ? tiles(tid) : 0;  // (of the first caches, often all of them)
+    int all = mine;
+    for (int c = tid + THREADS; c < n_caches; c += THREADS) all += tiles(c);
+    int total;
+    scan_threads<THREADS>(all, lds, total);
+    run = max((total + target - 1) / target, 1);
+    run = (run + unit - 1) / unit * unit;
+    if (2 * n_caches <= target && n_caches <= THREADS) {
+      for (int i = 0; i < 4; ++i) {
+        int count;
+        scan_threads<THREADS>((mine + run - 1) / run, lds, count);
+        if (count <= target) break;
+        run = next_run(run, count);
+      }
     }
-    items0 += n_items;
-    slots0 += n_slots;
-    if (item < items0) break;
+    if (tid == 0) lds[kAt] = -1;
+    int items0 = 0, slots0 = 0;
+    for (int c0 = 0; c0 < n_caches; c0 += THREADS) {
+      const int c = c0 + tid;
+      const int x = c0 == 0 ? mine : c < n_caches ? tiles(c) : 0;
+      const int parts = (x + run - 1) / run;
+      int n_items, n_slots;
+      const int end = items0 + scan_threads<THREADS>(parts, lds, n_items);
+      const int slot_end = slots0 + scan_threads<THREADS>(parts > 1 ? parts : 0, lds, n_slots);
+      if (item < end && item >= end - parts) {
+        lds[kAt] = c;
+        lds[kAt + 1] = slot_end - (parts > 1 ? parts : 0);
+        lds[kAt + 2] = item - (end - parts);
+      }
+      items0 += n_items;
+      slots0 += n_slots;
+      if (item < items0) break;
+    }
+    __syncthreads();
+    const int c = __builtin_amdgcn_readfirstlane(lds[kAt]);
+    if (c < 0) return false;
+    sp.c_rel = c;
+    sp.slot = __builtin_amdgcn_readfirstlane(lds[kAt + 1]);
+    sp.part = __builtin_amdgcn_readfirstlane(lds[kAt + 2]);
+    t = __builtin_amdgcn_readfirstlane(tiles(c));
   }
-  __syncthreads();
-  const int c = __builtin_amdgcn_readfirstlane(lds[kAt]);
-  if (c < 0) return false;
-  sp.c_rel = c;
-  sp.slot = __builtin_amdgcn_readfirstlane(lds[kAt + 1]);
-  sp.part = __builtin_amdgcn_readfirstlane(lds[kAt + 2]);
-  const int t = __builtin_amdgcn_readfirstlane(tiles(c));
-  sp.n_parts = (t + run - 1) / run;
-  const int per = t / sp.n_parts, more = t % sp.n_parts;  // the first `more` items have one tile more
+  run = __builtin_amdgcn_readfirstlane(run);
+  sp.n_parts = __builtin_amdgcn_readfirstlane((t + run - 1) / run);
+  const int per = __builtin_amdgcn_readfirstlane(t / sp.n_parts), more = t - per * sp.n_parts;  // the first `more` items have one tile more
   sp.first = sp.part * per + min(sp.part, more);
   sp.last = sp.first + per + (sp.part < more ? 1 : 0);
   return true;
+}
+
+__device__ __forceinline__ int tree_nodes(const TreeParams& p, int b) {
+  return p.n_nodes ? min(max(p.n_nodes[b], 0), p.N) : p.N;
+}
+
+// Who sees whom, as bits above[word][node]: a node's ancestors by doubling, all nodes at once.  up: parent of node threadIdx.x, or -1.
+// jump: kMostNodes words.  Threads beyond the nodes take part in the barriers.
+__device__ __forceinline__ void find_ancestors(int up, int n_nodes, unsigned long long (*above)[kMostNodes], int32_t* jump) {
+  constexpr int kWords = kMostNodes / 64;
+  const int tid = threadIdx.x;
+  const int words = (n_nodes + 63) / 64;
+  const bool node = tid < kMostNodes;
+  if (node) {
+    jump[tid] = up;
+    for (int w = 0; w < words; ++w) above[w][tid] = tid / 64 == w ? 1ull << (tid & 63) : 0ull;
+  }
+  __syncthreads();
+  for (int reach = 1; reach < n_nodes; reach *= 2) {
+    unsigned long long more[kWords];
+    const int to = node ? jump[tid] : -1;
+    int next = -1;
+    if (to >= 0) {
+      next = jump[to];
+#pragma unroll
+      for (int w = 0; w < kWords; ++w) more[w] = w < words ? above[w][to] : 0;
+    }
+    if (!__syncthreads_or(to >= 0)) break;
+    if (to >= 0) {
+      jump[tid] = next;
+#pragma unroll
+      for (int w = 0; w < kWords; ++w)
+        if (w < words) above[w][tid] |= more[w];
+    }
+    __syncthreads();
+  }
+}
+
+// Row (s_rel, node, head) of rows by byte strides.
+__device__ __forceinline__ unsigned char* row_of(const Rows& r, int s_rel, int node, int head) {
+  return reinterpret_cast<unsigned char*>(r.data) + s_rel * r.seq + node * r.tok + head * r.head;
 }
 #endif
 

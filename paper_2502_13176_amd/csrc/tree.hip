@@ -34,7 +34,6 @@ typedef short s16x8_t __attribute__((ext_vector_type(8)));
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLowest = -3.402823466e38f;
-constexpr int kMostParts = 512;   // work items of a launch that are aimed at, and therefore of a cache, at most
 constexpr float kMaxSlack = 8.f;  // a logit may exceed its row's reference maximum by this much (log2 units)
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -46,10 +45,6 @@ constexpr bool tree_shares_four(int type, int D) { return !(type == 1 && D == 12
 // Workgroups that fit a compute unit.
 constexpr int tree_resident(int type, int D, int ks) {
   return 4 * tree_tile(ks) * D * (type == 1 ? 4 : 2) > 72 * 1024 ? 1 : 2;
-}
-
-__device__ __forceinline__ int tree_nodes(const TreeParams& p, int b) {
-  return p.n_nodes ? min(max(p.n_nodes[b], 0), p.N) : p.N;
 }
 
 // What follows from the rows' type (BAKLAVA_BF16, F32, MXFP4), the head dimension and KS, the wavefronts that share 32 query rows.
@@ -99,7 +94,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
     return n > 0 ? (p.len[p.cache0 + c] + kTile - 1) / kTile + (n + kTile - 1) / kTile : 0;
   };
   Span sp;
-  if (!find_span<kThreads>(p.n_caches, p.target, p.least, item, tiles, scan, sp)) return;
+  if (!find_span<kThreads>(p.n_caches, p.target, 1, item, tiles, scan, sp)) return;
   const int h = sp.c_rel % p.Hkv, s_rel = sp.c_rel / p.Hkv, b = s_rel % p.batch;
   const int n_nodes = __builtin_amdgcn_readfirstlane(tree_nodes(p, b)), n_rows = n_nodes * p.G;
   const int n_live = __builtin_amdgcn_readfirstlane(p.len[p.cache0 + sp.c_rel]), live_tiles = (n_live + kTile - 1) / kTile;
@@ -161,7 +156,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
   auto follow_max = [&](float mx) {
     if (__any(mx > m_ref + kMaxSlack)) {
       mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float mn = fmaxf(m_ref, mx);
+      const float mn = mx > m_ref + kMaxSlack ? mx : m_ref;  // (a row's bits do not depend on the others)
       const float alpha = fast_exp2(m_ref - mn);
       m_ref = mn;
       l_part *= alpha;
@@ -344,35 +339,12 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
 
   // ---- drafted rows ----------------------------------------------------------------------------
   if (sp.last > live_tiles) {
-    // Who sees whom: bits of a node's ancestors by doubling, all nodes at once.  A parent that is no earlier node is none.
     static_assert(kMostNodes == kThreads, "a thread for every node");
-    const int words = (n_nodes + 63) / 64;
-    int32_t* const jump = reinterpret_cast<int32_t*>(lds_k[0]);
-    __syncthreads();  // (the last tile has been read)
-    int up = -1;
+    int up = -1;  // (a parent that is no earlier node is none)
     if (tid < n_nodes) up = p.parent[(int64_t)b * p.N + tid];
     if (up < 0 || up >= tid) up = -1;
-    jump[tid] = up;
-    for (int w = 0; w < words; ++w) above[w][tid] = tid / 64 == w ? 1ull << (tid & 63) : 0ull;
-    __syncthreads();
-    for (int reach = 1; reach < n_nodes; reach *= 2) {
-      unsigned long long more[kMostNodes / 64];
-      const int to = jump[tid];
-      int next = -1;
-      if (to >= 0) {
-        next = jump[to];
-#pragma unroll
-        for (int w = 0; w < kMostNodes / 64; ++w) more[w] = w < words ? above[w][to] : 0;
-      }
-      __syncthreads();
-      if (to >= 0) {
-        jump[tid] = next;
-#pragma unroll
-        for (int w = 0; w < kMostNodes / 64; ++w)
-          if (w < words) above[w][tid] |= more[w];
-      }
-      __syncthreads();
-    }
+    __syncthreads();  // (the last tile has been read)
+    find_ancestors(up, n_nodes, above, reinterpret_cast<int32_t*>(lds_k[0]));
     const int first_dt = max(sp.first - live_tiles, 0), last_dt = sp.last - live_tiles;
     const unsigned char* Kd = reinterpret_cast<const unsigned char*>(p.k.data) + s_rel * p.k.seq + h * p.k.head;
     const unsigned char* Vd = reinterpret_cast<const unsigned char*>(p.v.data) + s_rel * p.v.seq + h * p.v.head;
@@ -535,7 +507,7 @@ constexpr int kMergeRows = 2;
 template <int D, bool F32>
 __global__ __launch_bounds__(kThreads) void tree_merge_kernel(TreeParams p) {
   constexpr int kLanes = D / 4, kPer = kThreads / kMergeRows, kGroups = kPer / kLanes;
-  __shared__ float weight[kMergeRows][kMostParts];
+  __shared__ float weight[kMergeRows][kMostTreeItems];
   __shared__ float2 sums[kMergeRows][kPer / 64];
   __shared__ floatx4_t part_sum[kMergeRows][kGroups][kLanes];
   const int c_rel = blockIdx.x, s_rel = c_rel / p.Hkv, h = c_rel % p.Hkv, b = s_rel % p.batch;
@@ -620,20 +592,27 @@ hipError_t launch(const TreeParams& p, int ks, unsigned grid, hipStream_t s) {
 
 TreeLaunch tree_launch(int type, int D, int rows, int n_cus) {
   TreeLaunch t;
-  t.ks = rows <= 32 && tree_shares_four(type, D) ? 4 : rows <= 64 ? 2 : 1;
+  if (rows <= kStreamRows) {
+    t.ks = 0;
+    t.row_tiles = 1;
+    t.target = n_cus < kMostTreeItems ? n_cus : kMostTreeItems;
+    return t;
+  }
+  t.ks = 1;
   const int per = 32 * kWaves / t.ks;
   t.row_tiles = (rows + per - 1) / per;
   const int resident = tree_resident(type, D, t.ks);
-  const int all = resident * n_cus < kMostParts ? resident * n_cus : kMostParts;
+  const int all = resident * n_cus < kMostTreeItems ? resident * n_cus : kMostTreeItems;
   t.target = all / t.row_tiles > 1 ? all / t.row_tiles : 1;
   return t;
 }
 
 hipError_t launch_tree_attn(const TreeParams& p, const TreeLaunch& t, int type, int D, int n_caches, hipStream_t s) {
-  const int64_t grid = ((int64_t)t.target + n_caches + 7) / 8 * 8 * t.row_tiles;
+  const int64_t grid = ((int64_t)t.target + n_caches + 7) / 8 * 8 * t.row_tiles;  // (of 512 threads at most)
   const int merge_rows = (p.rows + kMergeRows - 1) / kMergeRows;
-  if (grid > INT32_MAX / kThreads || merge_rows > 65535) return hipErrorInvalidValue;
-  hipError_t e = type == 1   ? D == 128 ? launch<1, 128>(p, t.ks, (unsigned)grid, s) : launch<1, 64>(p, t.ks, (unsigned)grid, s)
+  if (grid > INT32_MAX / 512 || merge_rows > 65535) return hipErrorInvalidValue;
+  hipError_t e = t.ks == 0   ? launch_tree_stream(p, type, D, t.target + n_caches, s)
+                 : type == 1 ? D == 128 ? launch<1, 128>(p, t.ks, (unsigned)grid, s) : launch<1, 64>(p, t.ks, (unsigned)grid, s)
                  : type == 2 ? D == 128 ? launch<2, 128>(p, t.ks, (unsigned)grid, s) : launch<2, 64>(p, t.ks, (unsigned)grid, s)
                              : D == 128 ? launch<0, 128>(p, t.ks, (unsigned)grid, s) : launch<0, 64>(p, t.ks, (unsigned)grid, s);
   if (e != hipSuccess) return e;
