@@ -67,15 +67,28 @@ __device__ __forceinline__ const void* row_at(const void* data, int64_t row) {
   return reinterpret_cast<const char*>(data) + row * (F32 ? 4 : 2);
 }
 
-// exp((x - top) inv) for x <= top; 0 where x is -inf (top may be, too).
-__device__ __forceinline__ double weight(float x, float top, double inv) {
-  return x > kNegInf ? exp(((double)x - (double)top) * inv) : 0.0;
+// 2^((x - top) c) for x <= top, 0 where x is -inf (top may be, too); c = log2(e) / temperature.  The fraction f of the exponent, at most
+// 1/2, goes into the series sum (f ln 2)^k / k!, whose next term is below 2^-47 of it; equal logits give exactly 1.
+__device__ __forceinline__ double weight(float x, float top, double c) {
+  const double y = ((double)x - (double)top) * c, n = __builtin_rint(y), f = y - n;
+  double s = 7.0549116208011233e-9;                  // ln2^10 / 10!
+  s = __builtin_fma(s, f, 1.0178086009239699e-7);    // ln2^9 / 9!
+  s = __builtin_fma(s, f, 1.3215486790144307e-6);
+  s = __builtin_fma(s, f, 1.5252733804059840e-5);
+  s = __builtin_fma(s, f, 1.5403530393381608e-4);
+  s = __builtin_fma(s, f, 1.3333558146428443e-3);
+  s = __builtin_fma(s, f, 9.6181291076284771e-3);
+  s = __builtin_fma(s, f, 5.5504108664821579e-2);
+  s = __builtin_fma(s, f, 2.4022650695910071e-1);
+  s = __builtin_fma(s, f, 6.9314718055994531e-1);
+  s = __builtin_fma(s, f, 1.0);
+  return x > kNegInf ? __builtin_amdgcn_ldexp(s, (int)__builtin_fmax(n, -2000.0)) : 0.0;
 }
 
 __device__ __forceinline__ int nodes_of(const VerifyParams& p, int b) { return p.n_nodes ? min(max(p.n_nodes[b], 0), p.N) : p.N; }
-__device__ __forceinline__ double inverse_temp(const VerifyParams& p, int b) {  // 0: greedy
+__device__ __forceinline__ double exponent_scale(const VerifyParams& p, int b) {  // log2(e) / temperature; 0: greedy
   const float t = p.temp ? p.temp[b] : 1.f;
-  return t > 0.f ? 1.0 / (double)t : 0.0;
+  return t > 0.f ? 1.4426950408889634 / (double)t : 0.0;
 }
 
 // Sums over the workgroup, in an order that does not change.
@@ -117,7 +130,7 @@ __global__ __launch_bounds__(kThreads) void verify_stat_kernel(VerifyParams p) {
   const bool draft = r >= p.n_seq * p.N;
   const int at = draft ? r - p.n_seq * p.N : r, b = (uint32_t)at / (uint32_t)p.N, i = (uint32_t)at % (uint32_t)p.N;
   const int n = nodes_of(p, b), tid = threadIdx.x;
-  const double inv = inverse_temp(p, b);
+  const double inv = exponent_scale(p, b);
   if (i >= n) return;
   if (draft) {
     if (i == 0 || inv == 0.0) return;
@@ -151,29 +164,57 @@ __global__ __launch_bounds__(kThreads) void verify_stat_kernel(VerifyParams p) {
   if (tid == 0) p.stat[(int64_t)r * p.parts + part] = VerifyStat{s, t.x, t.first};
 }
 
-__device__ __forceinline__ VerifyStat merged(const VerifyStat* s, int parts, double inv) {
+// All of a row from its parts, by 16 neighbouring lanes; the same in each.
+__device__ __forceinline__ VerifyStat merged(const VerifyStat* s, int parts, double c) {
+  const int l = threadIdx.x & 15;
   Top t{kNegInf, INT32_MAX};
-  for (int i = 0; i < parts; ++i) t = higher(t, Top{s[i].top, s[i].first});
+  for (int i = l; i < parts; i += 16) t = higher(t, Top{s[i].top, s[i].first});
+#pragma unroll
+  for (int i = 8; i >= 1; i /= 2) t = higher(t, Top{__shfl_xor(t.x, i), __shfl_xor(t.first, i)});
   double sum = 0.0;
-  if (inv > 0.0)
-    for (int i = 0; i < parts; ++i) sum += s[i].sum * weight(s[i].top, t.x, inv);
+  if (c > 0.0) {
+    for (int i = l; i < parts; i += 16) sum += s[i].sum * weight(s[i].top, t.x, c);
+#pragma unroll
+    for (int i = 8; i >= 1; i /= 2) sum += __shfl_xor(sum, i);
+  }
   return VerifyStat{sum, t.x, t.first};
 }
 
-// Probability of element v of node `cur`'s row when what n_tried children have left of it is known: of all but the last one
-// divided by its sum.  *before: without the last one.  (target, drafts: merged statistics of the node's row and of the draft rows.)
+// Probabilities of elements v .. v + 7 of a node's row (logits x) when what n_tried children have left of it is known: of all but the
+// last one divided by its sum.  before: without the last one.  (target, drafts: merged statistics of the node's row and of the draft
+// rows.)  Elements behind the row: 0.
 template <bool F32>
-__device__ __forceinline__ double rest_of(const VerifyParams& p, int64_t node0, const VerifyStat& target, const VerifyStat* drafts, float x,
-                                          int v, const int32_t* tried, const double* left, int n_tried, double inv, double* before) {
-  double r = target.sum > 0.0 ? weight(x, target.top, inv) / target.sum : 0.0;
-  *before = r;
+__device__ __forceinline__ void rest_of(double (&r)[8], double (&before)[8], const VerifyParams& p, int64_t node0, const VerifyStat& target,
+                                        const VerifyStat* drafts, const float (&x)[8], int v, const int32_t* tried, const double* left,
+                                        int n_tried, double c) {
+  const double one = target.sum > 0.0 ? 1.0 / target.sum : 0.0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) before[e] = r[e] = weight(x[e], target.top, c) * one;
+#pragma unroll 1
   for (int k = 0; k < n_tried; ++k) {
     const int j = tried[k];
     const VerifyStat d = drafts[j];
-    const double q = d.sum > 0.0 ? weight(load1<F32>(row_at<F32>(p.draft, (node0 + j) * p.draft_row), v), d.top, inv) / d.sum : 0.0;
-    *before = r;
-    r = fmax(r - q, 0.0);
-    if (k + 1 < n_tried) r /= left[k];
+    const double unit = d.sum > 0.0 ? 1.0 / d.sum : 0.0, open = k + 1 < n_tried ? 1.0 / left[k] : 1.0;
+    float y[8];
+    load8<F32>(y, row_at<F32>(p.draft, (node0 + j) * p.draft_row), v, p.V);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      before[e] = r[e];
+      r[e] = __builtin_fmax(r[e] - weight(y[e], d.top, c) * unit, 0.0) * open;
+    }
+  }
+}
+// ... of one element, all divided.
+template <bool F32>
+__device__ __forceinline__ double rest_of_one(const VerifyParams& p, int64_t node0, const VerifyStat& target, const VerifyStat* drafts, int v,
+                                              const void* row, const int32_t* tried, const double* left, int n_tried, double c) {
+  double r = target.sum > 0.0 ? weight(load1<F32>(row, v), target.top, c) * (1.0 / target.sum) : 0.0;
+#pragma unroll 1
+  for (int k = 0; k < n_tried; ++k) {
+    const int j = tried[k];
+    const VerifyStat d = drafts[j];
+    const double q = d.sum > 0.0 ? weight(load1<F32>(row_at<F32>(p.draft, (node0 + j) * p.draft_row), v), d.top, c) * (1.0 / d.sum) : 0.0;
+    r = __builtin_fmax(r - q, 0.0) / left[k];
   }
   return r;
 }
@@ -197,7 +238,7 @@ __global__ __launch_bounds__(kThreads) void verify_walk_kernel(VerifyParams p) {
     }
     return;
   }
-  const double inv = inverse_temp(p, b);
+  const double inv = exponent_scale(p, b);
   const bool rows = p.draft && inv > 0.0;
   int up = -1, mine = -1;
   if (tid < n && tid > 0) {
@@ -209,27 +250,29 @@ __global__ __launch_bounds__(kThreads) void verify_walk_kernel(VerifyParams p) {
   parent[tid] = up;
   token[tid] = mine;
   u[tid] = tid < n ? p.u[node0 + tid] : 0.f;
+  tried[tid] = 0;                    // (until the walk: whether node tid has children)
   __syncthreads();
-  bool inner = false;
-  if (tid < n)
-    for (int j = tid + 1; j < n; ++j) inner = inner || parent[j] == tid;
-  if (inner) {
-    target[tid] = merged(p.stat + (node0 + tid) * p.parts, p.parts, inv);
-    p.all[node0 + tid] = target[tid];
-  }
-  if (rows && up >= 0) {
-    drafts[tid] = merged(p.stat + ((int64_t)p.n_seq * p.N + node0 + tid) * p.parts, p.parts, inv);
-    p.draft_all[node0 + tid] = drafts[tid];
+  if (up >= 0) tried[up] = 1;
+  __syncthreads();
+  for (int i = tid / 16; i < n; i += kThreads / 16) {
+    if (tried[i]) {
+      const VerifyStat s = merged(p.stat + (node0 + i) * p.parts, p.parts, inv);
+      if (tid % 16 == 0) target[i] = p.all[node0 + i] = s;
+    }
+    if (rows && parent[i] >= 0) {
+      const VerifyStat s = merged(p.stat + ((int64_t)p.n_seq * p.N + node0 + i) * p.parts, p.parts, inv);
+      if (tid % 16 == 0) drafts[i] = p.draft_all[node0 + i] = s;
+    }
   }
   __syncthreads();
   double pr = 0.0, q = 1.0;
   if (up >= 0 && mine >= 0) {
     const VerifyStat s = target[up];
     if (inv == 0.0) pr = s.top > kNegInf && s.first == mine ? 1.0 : 0.0;
-    else if (s.sum > 0.0) pr = weight(load1<F32>(row_at<F32>(p.logits, (node0 + up) * p.row), mine), s.top, inv) / s.sum;
+    else if (s.sum > 0.0) pr = weight(load1<F32>(row_at<F32>(p.logits, (node0 + up) * p.row), mine), s.top, inv) * (1.0 / s.sum);
     if (rows) {
       const VerifyStat d = drafts[tid];
-      q = d.sum > 0.0 ? weight(load1<F32>(row_at<F32>(p.draft, (node0 + tid) * p.draft_row), mine), d.top, inv) / d.sum : 0.0;
+      q = d.sum > 0.0 ? weight(load1<F32>(row_at<F32>(p.draft, (node0 + tid) * p.draft_row), mine), d.top, inv) * (1.0 / d.sum) : 0.0;
     }
   }
   prob[tid] = pr;
@@ -254,9 +297,16 @@ __global__ __launch_bounds__(kThreads) void verify_walk_kernel(VerifyParams p) {
       if (rows && n_tried > 0) {     // the sum that the child before has left
         const VerifyStat s = target[cur];
         const void* row = row_at<F32>(p.logits, (node0 + cur) * p.row);
-        double z = 0.0, unused;
-        for (int v = tid; v < p.V; v += kThreads)
-          z += rest_of<F32>(p, node0, s, drafts, load1<F32>(row, v), v, tried, left, n_tried, inv, &unused);
+        double z = 0.0;
+#pragma unroll 1
+        for (int v = tid * 8; v < p.V; v += kThreads * 8) {
+          float x[8];
+          double y[8], unused[8];
+          load8<F32>(x, row, v, p.V);
+          rest_of<F32>(y, unused, p, node0, s, drafts, x, v, tried, left, n_tried, inv);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) z += y[e];
+        }
         z = sum_threads(z, sums);
         if (z > 0.0) {
           if (tid == 0) left[n_tried - 1] = z;
@@ -264,8 +314,7 @@ __global__ __launch_bounds__(kThreads) void verify_walk_kernel(VerifyParams p) {
           n_tried -= 1;              // nothing: it stays as it was before
         }
         __syncthreads();
-        if (n_tried > 0)
-          r = rest_of<F32>(p, node0, s, drafts, load1<F32>(row, t), t, tried, left, n_tried, inv, &unused) / left[n_tried - 1];
+        if (n_tried > 0) r = rest_of_one<F32>(p, node0, s, drafts, t, row, tried, left, n_tried, inv);
       } else if (!rows) {
         for (int k = 0; k < n_tried; ++k) again = again || token[tried[k]] == t;
         r = again ? 0.0 : r / (1.0 - off);
@@ -301,6 +350,20 @@ __global__ __launch_bounds__(kThreads) void verify_walk_kernel(VerifyParams p) {
   }
 }
 
+// Tokens whose point masses were taken off have no weight: -inf in their place.  x[k][e]: element v0 + k kThreads 8 + e.
+template <int K>
+__device__ __forceinline__ void take_off(const VerifyParams& p, int64_t node0, int n_tried, float (&x)[K][8], int v0) {
+#pragma unroll 1
+  for (int j = 0; j < n_tried; ++j) {
+    const int at = p.token[node0 + p.tried[node0 + j]] - v0;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (at == k * kThreads * 8 + e) x[k][e] = kNegInf;
+  }
+}
+
 // Weights of the last node's row, a part each.
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void verify_mass_kernel(VerifyParams p) {
@@ -310,44 +373,45 @@ __global__ __launch_bounds__(kThreads) void verify_mass_kernel(VerifyParams p) {
   const VerifyEnd e = p.end[b];
   if (e.last < 0) return;
   const int64_t node0 = (int64_t)b * p.N;
-  const double inv = inverse_temp(p, b);
+  const double inv = exponent_scale(p, b);
   const void* row = row_at<F32>(p.logits, (node0 + e.last) * p.row);
   const int v0 = part * kVerifyPart + tid * 8;
   float x[kPer / 8][8];
 #pragma unroll
   for (int k = 0; k < kPer / 8; ++k) load8<F32>(x[k], row, v0 + k * kThreads * 8, p.V);
+  const bool rows = p.draft && inv > 0.0 && e.n_tried > 0;
+  if (!rows && inv > 0.0) take_off(p, node0, e.n_tried, x, v0);
   Top t{kNegInf, INT32_MAX};
 #pragma unroll
   for (int k = 0; k < kPer / 8; ++k)
 #pragma unroll
-    for (int e8 = 0; e8 < 8; ++e8)
-      if (x[k][e8] > t.x) t = Top{x[k][e8], v0 + k * kThreads * 8 + e8};
+    for (int i = 0; i < 8; ++i)
+      if (x[k][i] > t.x) t = Top{x[k][i], v0 + k * kThreads * 8 + i};
   t = top_of_threads(t, tops);
   double all = 0.0, without = 0.0;
   if (inv > 0.0) {
-    if (p.draft && e.n_tried > 0) {
+    if (rows) {
       const VerifyStat s = p.all[node0 + e.last];
+#pragma unroll 1
+      for (int k = 0; k < kPer / 8; ++k) {
+        const int v = v0 + k * kThreads * 8;
+        if (v >= p.V) break;
+        float y[8];
+        double r[8], before[8];
+        load8<F32>(y, row, v, p.V);
+        rest_of<F32>(r, before, p, node0, s, p.draft_all + node0, y, v, p.tried + node0, p.left + node0, e.n_tried, inv);
 #pragma unroll
-      for (int k = 0; k < kPer / 8; ++k)
-        for (int e8 = 0; e8 < 8; ++e8) {
-          const int v = v0 + k * kThreads * 8 + e8;
-          double before;
-          if (v < p.V) {
-            all += rest_of<F32>(p, node0, s, p.draft_all + node0, x[k][e8], v, p.tried + node0, p.left + node0, e.n_tried, inv, &before);
-            without += before;
-          }
+        for (int i = 0; i < 8; ++i) {
+          all += r[i];
+          without += before[i];
         }
+      }
     } else {
-      // relative to the part's largest logit, so that the whole row's is not needed; tokens whose point masses were taken off have none
+      // relative to the part's largest logit, so that the whole row's is not needed
 #pragma unroll
       for (int k = 0; k < kPer / 8; ++k)
 #pragma unroll
-        for (int e8 = 0; e8 < 8; ++e8) {
-          double w = weight(x[k][e8], t.x, inv);
-          for (int j = 0; j < e.n_tried; ++j)
-            if (p.token[node0 + p.tried[node0 + j]] == v0 + k * kThreads * 8 + e8) w = 0.0;
-          all += w;
-        }
+        for (int i = 0; i < 8; ++i) all += weight(x[k][i], t.x, inv);
       without = all;
     }
     all = sum_threads(all, sums);
@@ -362,6 +426,7 @@ __global__ __launch_bounds__(kThreads) void verify_mass_kernel(VerifyParams p) {
 
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyParams p) {
+  __shared__ double w[kVerifyPart + kThreads];  // weights of the part's elements: a place is left out behind every kPer
   __shared__ double sums[kWaves];
   __shared__ Top tops[kWaves];
   __shared__ int found;
@@ -372,7 +437,7 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyParams p) {
     return;
   }
   const int64_t node0 = (int64_t)b * p.N;
-  const double inv = inverse_temp(p, b);
+  const double inv = exponent_scale(p, b);
   const VerifyStat* tops_of = p.top + (int64_t)b * p.parts;
   Top t{kNegInf, INT32_MAX};
   for (int i = tid; i < p.parts; i += kThreads) t = higher(t, Top{tops_of[i].top, tops_of[i].first});
@@ -381,90 +446,99 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyParams p) {
     if (tid == 0) p.next[b] = t.x == kNegInf ? -1 : t.first;
     return;
   }
+  // The part, by every wavefront for itself.
   const bool rows = p.draft && e.n_tried > 0;
   const double* mass = p.mass + (int64_t)b * p.parts * 2;
-  // (few parts: every thread goes over all of them)
-  double total = 0.0;
-  for (int i = 0; i < p.parts; ++i) total += rows ? mass[2 * i] : mass[2 * i] * weight(tops_of[i].top, t.x, inv);
+  auto mass_of = [&](int i, int which) { return i >= p.parts ? 0.0 : rows ? mass[2 * i + which] : mass[2 * i] * weight(tops_of[i].top, t.x, inv); };
+  auto total_of = [&](int which) {
+    double s = 0.0;
+    for (int i = lane; i < p.parts; i += 64) s += mass_of(i, which);
+#pragma unroll
+    for (int i = 32; i >= 1; i /= 2) s += __shfl_xor(s, i);
+    return s;
+  };
+  auto scan = [&](double x) {
+#pragma unroll
+    for (int i = 1; i < 64; i *= 2) {
+      const double y = __shfl_up(x, i);
+      x += lane >= i ? y : 0.0;
+    }
+    return x;
+  };
+  double total = total_of(0);
   int which = 0;
   if (rows && !(total > 0.0)) {  // nothing was left by the last child that was tried: as it was before
     which = 1;
-    for (int i = 0; i < p.parts; ++i) total += mass[2 * i + 1];
+    total = total_of(1);
   }
-  const double u = fmin(fmax((double)p.u[node0], 0.0), 1.0), want = u * total;
+  const double want = fmin(fmax((double)p.u[node0], 0.0), 1.0) * total;
   int part = -1;
-  double before = 0.0;
-  {
-    double c = 0.0;
-    for (int i = 0; i < p.parts; ++i) {
-      const double m = rows ? mass[2 * i + which] : mass[2 * i] * weight(tops_of[i].top, t.x, inv);
-      if (m > 0.0) {
-        part = i;
-        before = c;
-      }
-      c += m;
-      if (c > want && m > 0.0) break;
+  double before = 0.0, c0 = 0.0;
+  for (int i0 = 0; i0 < p.parts; i0 += 64) {
+    const double m = mass_of(i0 + lane, which), c = c0 + scan(m);
+    const unsigned long long over = __ballot(m > 0.0 && c > want), some = __ballot(m > 0.0);
+    if (over | some) {
+      const int l = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some);  // (without one: the last that has any weight)
+      part = i0 + l;
+      before = __shfl(c - m, l);
     }
+    if (over) break;
+    c0 = __shfl(c, 63);
   }
   if (part < 0) {
     if (tid == 0) p.next[b] = -1;
     return;
   }
   const void* row = row_at<F32>(p.logits, (node0 + e.last) * p.row);
-  VerifyStat s{0.0, t.x, 0};
-  if (rows) s = p.all[node0 + e.last];
-  // a thread's elements follow each other here
-  const int v0 = part * kVerifyPart + tid * kPer;
-  double w[kPer], mine = 0.0;
-#pragma unroll
+  auto place = [](int i) { return i + i / kPer; };
+#pragma unroll 1
   for (int k = 0; k < kPer / 8; ++k) {
-    float x[8];
-    load8<F32>(x, row, v0 + k * 8, p.V);
+    const int at = k * kThreads * 8 + tid * 8, v = part * kVerifyPart + at;
+    float x[1][8];
+    double y[8];
+    load8<F32>(x[0], row, v, p.V);
+    if (rows) {
+      double prev[8];
+      rest_of<F32>(y, prev, p, node0, p.all[node0 + e.last], p.draft_all + node0, x[0], v, p.tried + node0, p.left + node0, e.n_tried, inv);
 #pragma unroll
-    for (int e8 = 0; e8 < 8; ++e8) {
-      const int v = v0 + k * 8 + e8;
-      double y = 0.0;
-      if (v < p.V) {
-        if (rows) {
-          double prev;
-          y = rest_of<F32>(p, node0, s, p.draft_all + node0, x[e8], v, p.tried + node0, p.left + node0, e.n_tried, inv, &prev);
-          if (which) y = prev;
-        } else {
-          y = weight(x[e8], t.x, inv);
-          for (int j = 0; j < e.n_tried; ++j)
-            if (p.token[node0 + p.tried[node0 + j]] == v) y = 0.0;
-        }
-      }
-      w[k * 8 + e8] = y;
-      mine += y;
+      for (int i = 0; i < 8; ++i) y[i] = which ? prev[i] : y[i];
+    } else {
+      take_off(p, node0, e.n_tried, x, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = weight(x[0][i], t.x, inv);
     }
-  }
-  double end = mine;
 #pragma unroll
-  for (int i = 1; i < 64; i *= 2) {
-    const double y = __shfl_up(end, i);
-    end += lane >= i ? y : 0.0;
+    for (int i = 0; i < 8; ++i) w[place(at + i)] = y[i];
   }
-  if (lane == 63) sums[wave] = end;
   if (tid == 0) found = INT32_MAX;
   __syncthreads();
+  const double* mine = w + tid * (kPer + 1);
+  double sum = 0.0;
+#pragma unroll 8
+  for (int i = 0; i < kPer; ++i) sum += mine[i];
+  double end = scan(sum);
+  if (lane == 63) sums[wave] = end;
+  __syncthreads();
   for (int x = 0; x < wave; ++x) end += sums[x];
-  double c = before + end - mine;
+  // The first element whose sum exceeds; where rounding leaves none, the last one that has any weight.
+  double c = before + end - sum;
   int last = -1, hit = -1;
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    c += w[k];
-    if (w[k] > 0.0) last = v0 + k;
-    if (hit < 0 && w[k] > 0.0 && c > want) hit = v0 + k;
+#pragma unroll 8
+  for (int i = 0; i < kPer; ++i) {
+    const double y = mine[i];
+    c += y;
+    if (y > 0.0) last = i;
+    if (hit < 0 && y > 0.0 && c > want) hit = i;
   }
-  if (hit >= 0) atomicMin(&found, hit);
+  const int v0 = part * kVerifyPart + tid * kPer;
+  if (hit >= 0) atomicMin(&found, v0 + hit);
   __syncthreads();
-  const int got = found;
+  const bool none = found == INT32_MAX;
   __syncthreads();
-  if (got == INT32_MAX) {  // rounding: the last token that has any weight
+  if (none) {
     if (tid == 0) found = -1;
     __syncthreads();
-    if (last >= 0) atomicMax(&found, last);
+    if (last >= 0) atomicMax(&found, v0 + last);
     __syncthreads();
   }
   if (tid == 0) p.next[b] = found;
