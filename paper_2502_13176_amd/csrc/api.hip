@@ -1241,28 +1241,29 @@ extern "C" int baklava_append_accepted(baklava_ctx* ctx, int32_t layer_begin, in
 namespace {
 
 struct VerifySpace {
-  int64_t parts;
-  size_t all, draft_all, end, tried, left, mass, top, total;  // (the statistics are in front)
+  int64_t parts, picks;
+  size_t exact, end, tried, left, mass, ticket, total;  // (the statistics are in front)
 };
 VerifySpace verify_space(int32_t n_seq, int32_t N, int32_t V, bool draft) {
   const size_t nodes = (size_t)n_seq * N;
   VerifySpace w;
   w.parts = ((int64_t)V + kVerifyPart - 1) / kVerifyPart;
-  w.all = align256(nodes * w.parts * (draft ? 2 : 1) * sizeof(VerifyStat));
-  w.draft_all = align256(w.all + nodes * sizeof(VerifyStat));
-  w.end = align256(w.draft_all + (draft ? nodes : 0) * sizeof(VerifyStat));
-  w.tried = align256(w.end + (size_t)n_seq * sizeof(VerifyEnd));
-  w.left = align256(w.tried + nodes * sizeof(int32_t));
-  w.mass = align256(w.left + nodes * sizeof(double));
-  w.top = align256(w.mass + (size_t)n_seq * w.parts * 2 * sizeof(double));
-  w.total = align256(w.top + (size_t)n_seq * w.parts * sizeof(VerifyStat));
+  w.picks = ((int64_t)V + kVerifyPick - 1) / kVerifyPick;
+  const size_t stats = nodes * w.parts * (draft ? 2 : 1) * sizeof(VerifyStat);
+  w.exact = align256(stats);
+  w.end = align256(w.exact + (draft ? stats : 0));
+  w.tried = align256(w.end + (draft ? (size_t)n_seq * sizeof(VerifyEnd) : 0));
+  w.left = align256(w.tried + (draft ? nodes * sizeof(int32_t) : 0));
+  w.mass = align256(w.left + (draft ? nodes * sizeof(double) : 0));
+  w.ticket = align256(w.mass + (size_t)n_seq * w.picks * sizeof(VerifyMass));
+  w.total = align256(w.ticket + (size_t)n_seq * sizeof(int32_t));
   return w;
 }
 
 bool verify_shape_ok(int32_t n_seq, int32_t N, int32_t V, bool draft) {
   if (n_seq < 1 || N < 1 || N > kMostNodes || V < 1 || V > kMostVocabulary) return false;
   const int64_t parts = ((int64_t)V + kVerifyPart - 1) / kVerifyPart;
-  return (int64_t)n_seq * N <= INT32_MAX / 1024 && (int64_t)n_seq * N * (draft ? 2 : 1) * parts <= INT32_MAX / 1024;
+  return (int64_t)n_seq * N <= INT32_MAX / 1024 && (int64_t)n_seq * N * (draft ? 2 : 1) * parts <= INT32_MAX / 1024 && (int64_t)n_seq * parts * (kVerifyPart / kVerifyPick) <= INT32_MAX / 1024;
 }
 
 }  // namespace
@@ -1297,14 +1298,14 @@ extern "C" int baklava_verify_draft(const void* logits, int64_t row_stride, cons
   p.path = path; p.n_path = n_path; p.next = next_token;
   char* const ws = reinterpret_cast<char*>(workspace);
   p.stat = reinterpret_cast<VerifyStat*>(ws);
-  p.all = reinterpret_cast<VerifyStat*>(ws + w.all);
-  p.draft_all = reinterpret_cast<VerifyStat*>(ws + w.draft_all);
+  p.exact = reinterpret_cast<VerifyStat*>(ws + w.exact);
   p.end = reinterpret_cast<VerifyEnd*>(ws + w.end);
   p.tried = reinterpret_cast<int32_t*>(ws + w.tried);
   p.left = reinterpret_cast<double*>(ws + w.left);
-  p.mass = reinterpret_cast<double*>(ws + w.mass);
-  p.top = reinterpret_cast<VerifyStat*>(ws + w.top);
-  p.n_seq = n_seq; p.N = N; p.V = V; p.parts = (int32_t)w.parts;
+  p.mass = reinterpret_cast<VerifyMass*>(ws + w.mass);
+  p.ticket = reinterpret_cast<int32_t*>(ws + w.ticket);
+  p.n_seq = n_seq; p.N = N; p.V = V;
+  p.parts = (int32_t)w.parts; p.picks = (int32_t)w.picks;
   if (!hip_ok(launch_verify_draft(p, dtype, (hipStream_t)stream))) return BAKLAVA_EHIP;
   return BAKLAVA_OK;
 }

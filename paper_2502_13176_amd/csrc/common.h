@@ -291,6 +291,11 @@ struct VerifyEnd {        // where the walk of a sequence has ended
   int32_t last;           // node
   int32_t n_tried;        // its children that were tried and not accepted, and have an effect on what may follow
 };
+struct VerifyMass {       // of a part of the last node's row
+  double all, without;    // weights of what is left by all of those children, without the last of them
+  float top;              // the largest logit and where the first of them is
+  int32_t first;
+};
 struct VerifyParams {
   const void* logits;     // [n_seq * N] rows of V elements
   const void* draft;      // the same, or null
@@ -304,14 +309,14 @@ struct VerifyParams {
   int32_t* n_path;        // [n_seq]
   int32_t* next;          // [n_seq]
   VerifyStat* stat;       // [target, then draft rows][n_seq * N][parts]
-  VerifyStat* all;        // [n_seq * N] merged over the parts: target rows
-  VerifyStat* draft_all;  // [n_seq * N] draft rows
+  VerifyStat* exact;      // the same, of the rows the walk has ended with (draft rows only, as the next three)
   VerifyEnd* end;         // [n_seq]
   int32_t* tried;         // [n_seq, N] those children
   double* left;           // [n_seq, N] what each left of the distribution
-  double* mass;           // [n_seq][parts][2] weights of a part of the last node's row: with all of them taken off, without the last
-  VerifyStat* top;        // [n_seq][parts] the largest logit of it
-  int32_t n_seq, N, V, parts;
+  VerifyMass* mass;       // [n_seq][picks]
+  int32_t* ticket;        // [n_seq] parts that are done
+  int32_t n_seq, N, V;
+  int32_t parts, picks;   // parts of a row, of kVerifyPart elements and of kVerifyPick
 };
 
 constexpr int kLengthsPerLaunch = 512;
@@ -394,7 +399,7 @@ TreeLaunch tree_launch(int type, int D, int rows, int n_cus);
 hipError_t launch_tree_stream(const TreeParams& p, int type, int D, int n_items, hipStream_t s);
 hipError_t launch_tree_attn(const TreeParams& p, const TreeLaunch& t, int type, int D, int n_caches, hipStream_t s);
 hipError_t launch_append_accepted(const AcceptParams& p, int type, int D, int n_cus, hipStream_t s);
-constexpr int kVerifyPart = 8192;  // elements of a row that a workgroup takes
+constexpr int kVerifyPart = 8192, kVerifyPick = 2048;  // elements of a row that a workgroup takes
 hipError_t launch_verify_draft(const VerifyParams& p, int dtype, hipStream_t s);
 hipError_t launch_set_lengths(const LengthsParams& p, hipStream_t s);
 hipError_t launch_fill_i32(int32_t* dst, int32_t value, int64_t n, hipStream_t s);

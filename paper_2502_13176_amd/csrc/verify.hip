@@ -9,10 +9,14 @@
 // and the next token is the first v with r(0) + ... + r(v) > u_0 (r(0) + ... + r(V - 1)).  So whatever the drafts are, the tokens
 // are distributed as if the target had been sampled one by one.
 //
-// Everything that decides is held in 64 bits: a vocabulary has 1e5 borders between tokens, and an error of 1e-7 in the sums
-// would hand one draw in a hundred to a neighbour.  Launches: the largest logit and the sum of exponentials of parts of the rows
-// that a decision can need (a node without children is none); the walk, a workgroup for each sequence; the weights of parts of
-// the last node's row; the part and the token in it.
+// What decides between tokens next to each other is held in 64 bits: a vocabulary has 1e5 borders, and an error of 1e-7 in the sums
+// would hand one draw in a hundred to a neighbour.  A probability that is only compared with a random number may be off by some
+// 1e-8: sums of the rows that may be visited take the hardware's exponential, with what its argument lacks put back.
+//
+// Launches: the largest logit and the sum of exponentials of parts of the rows that a decision can need (a node without children is
+// none); the walk, and the weights of parts of the last node's row, of which the last workgroup to end takes the token.  With
+// draft rows what is left of a distribution is a difference, so the walk is a launch of its own that also sums up the rows it
+// ends with in 64 bits.
 #include "common.h"
 
 namespace baklava {
@@ -121,26 +125,40 @@ __device__ __forceinline__ Top top_of_threads(Top t, Top* lds) {
   return t;
 }
 
+// The same by the hardware's exponential: c = hi + lo, and what the product with the difference lacks goes in behind it.
+__device__ __forceinline__ float quick_weight(float x, float top, float hi, float lo) {
+  const float d = x - top, y = d * hi, rest = fmaf(d, lo, fmaf(d, hi, -y));
+  const float w = __builtin_amdgcn_exp2f(y);
+  return x > kNegInf ? fmaf(w, rest * 0.69314718f, w) : 0.f;
+}
+
 // One part of one row: workgroups over the parts first, then the nodes, then target and draft rows.
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void verify_stat_kernel(VerifyParams p) {
   __shared__ double sums[kWaves];
   __shared__ Top tops[kWaves];
+  __shared__ int32_t children[kMostNodes];
   const int part = (uint32_t)blockIdx.x % (uint32_t)p.parts, r = (uint32_t)blockIdx.x / (uint32_t)p.parts;
   const bool draft = r >= p.n_seq * p.N;
   const int at = draft ? r - p.n_seq * p.N : r, b = (uint32_t)at / (uint32_t)p.N, i = (uint32_t)at % (uint32_t)p.N;
   const int n = nodes_of(p, b), tid = threadIdx.x;
-  const double inv = exponent_scale(p, b);
+  const double c = exponent_scale(p, b);
+  if (!draft && i == 0 && part == 0 && tid == 0) p.ticket[b] = 0;
   if (i >= n) return;
+  children[tid] = 0;
+  int up = -1;
+  if (tid < n) up = p.parent[(int64_t)b * p.N + tid];
+  if (up < 0 || up >= tid) up = -1;
+  __syncthreads();
+  if (up >= 0) atomicAdd(&children[up], 1);
   if (draft) {
-    if (i == 0 || inv == 0.0) return;
-    const int up = p.parent[(int64_t)b * p.N + i];
-    if (up < 0 || up >= i) return;
+    if (!__syncthreads_or(tid == i && up >= 0) || c == 0.0) return;
   } else {
-    bool child = false;
-    for (int j = i + 1 + tid; j < n; j += kThreads) child = child || p.parent[(int64_t)b * p.N + j] == i;
-    if (!__syncthreads_or(child)) return;
+    __syncthreads();
+    if (children[i] == 0) return;
   }
+  // Draft rows and nodes with several children: what they leave of a distribution is divided by its sum in the walk.
+  const bool precise = p.draft && __syncthreads_or(children[tid] > 1);
   const void* row = row_at<F32>(draft ? p.draft : p.logits, at * (draft ? p.draft_row : p.row));
   const int v0 = part * kVerifyPart + tid * 8;
   float x[kPer / 8][8];
@@ -154,11 +172,18 @@ __global__ __launch_bounds__(kThreads) void verify_stat_kernel(VerifyParams p) {
       if (x[k][e] > t.x) t = Top{x[k][e], v0 + k * kThreads * 8 + e};
   t = top_of_threads(t, tops);
   double s = 0.0;
-  if (inv > 0.0) {
+  if (precise) {
 #pragma unroll
     for (int k = 0; k < kPer / 8; ++k)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s += weight(x[k][e], t.x, inv);
+      for (int e = 0; e < 8; ++e) s += weight(x[k][e], t.x, c);
+    s = sum_threads(s, sums);
+  } else if (c > 0.0) {
+    const float hi = (float)c, lo = (float)(c - (double)hi);
+#pragma unroll
+    for (int k = 0; k < kPer / 8; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += (double)quick_weight(x[k][e], t.x, hi, lo);
     s = sum_threads(s, sums);
   }
   if (tid == 0) p.stat[(int64_t)r * p.parts + part] = VerifyStat{s, t.x, t.first};
@@ -219,109 +244,108 @@ __device__ __forceinline__ double rest_of_one(const VerifyParams& p, int64_t nod
   return r;
 }
 
+// What the walk of a sequence leaves.
+struct Walk {
+  int32_t parent[kMostNodes], token[kMostNodes], tried[kMostNodes];  // tried: children of the last node that have had an effect
+  double prob[kMostNodes], from[kMostNodes];  // of node i's token: under its parent's row, under its own draft row
+  double left[kMostNodes];                    // what is left by tried[k], before it is divided
+  VerifyStat target[kMostNodes], drafts[kMostNodes];
+  float u[kMostNodes];
+  double sums[kWaves];
+};
+
+// The walk, by all threads of a workgroup together; write: its path goes out.  n > 0.
 template <bool F32>
-__global__ __launch_bounds__(kThreads) void verify_walk_kernel(VerifyParams p) {
-  __shared__ int32_t parent[kMostNodes], token[kMostNodes], tried[kMostNodes];
-  __shared__ double prob[kMostNodes], from[kMostNodes], left[kMostNodes];  // of node i's token: under its parent's row, under its own draft row
-  __shared__ VerifyStat target[kMostNodes], drafts[kMostNodes];
-  __shared__ float u[kMostNodes];
-  __shared__ double sums[kWaves];
+__device__ __forceinline__ VerifyEnd take_walk(const VerifyParams& p, int b, int n, double c, Walk& w, bool write) {
   static_assert(kMostNodes == kThreads, "a thread for every node");
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
-  const int n = nodes_of(p, b);
+  const int tid = threadIdx.x, lane = tid & 63;
   const int64_t node0 = (int64_t)b * p.N;
-  if (n == 0) {
-    if (tid < p.N) p.path[node0 + tid] = -1;
-    if (tid == 0) {
-      p.n_path[b] = 0;
-      p.end[b] = VerifyEnd{-1, 0};
-    }
-    return;
-  }
-  const double inv = exponent_scale(p, b);
-  const bool rows = p.draft && inv > 0.0;
+  const bool rows = p.draft && c > 0.0;
   int up = -1, mine = -1;
-  if (tid < n && tid > 0) {
+  if (tid < n) {
+    w.u[tid] = p.u[node0 + tid];
     up = p.parent[node0 + tid];
-    if (up < 0 || up >= tid) up = -1;
     mine = p.token[node0 + tid];
-    if (mine < 0 || mine >= p.V) mine = -1;  // (never accepted, and takes nothing off)
   }
-  parent[tid] = up;
-  token[tid] = mine;
-  u[tid] = tid < n ? p.u[node0 + tid] : 0.f;
-  tried[tid] = 0;                    // (until the walk: whether node tid has children)
+  if (tid == 0 || up < 0 || up >= tid) up = -1;
+  if (mine < 0 || mine >= p.V) mine = -1;     // (never accepted, and takes nothing off)
+  w.parent[tid] = up;
+  w.token[tid] = mine;
+  w.tried[tid] = 0;                           // (for now: whether node tid has children)
   __syncthreads();
-  if (up >= 0) tried[up] = 1;
+  if (up >= 0) w.tried[up] = 1;
+  float x = 0.f, y = 0.f;                     // logits of the node's token
+  if (up >= 0 && mine >= 0) {
+    x = load1<F32>(row_at<F32>(p.logits, (node0 + up) * p.row), mine);
+    if (rows) y = load1<F32>(row_at<F32>(p.draft, (node0 + tid) * p.draft_row), mine);
+  }
   __syncthreads();
   for (int i = tid / 16; i < n; i += kThreads / 16) {
-    if (tried[i]) {
-      const VerifyStat s = merged(p.stat + (node0 + i) * p.parts, p.parts, inv);
-      if (tid % 16 == 0) target[i] = p.all[node0 + i] = s;
+    if (w.tried[i]) {
+      const VerifyStat s = merged(p.stat + (node0 + i) * p.parts, p.parts, c);
+      if (tid % 16 == 0) w.target[i] = s;
     }
-    if (rows && parent[i] >= 0) {
-      const VerifyStat s = merged(p.stat + ((int64_t)p.n_seq * p.N + node0 + i) * p.parts, p.parts, inv);
-      if (tid % 16 == 0) drafts[i] = p.draft_all[node0 + i] = s;
+    if (rows && w.parent[i] >= 0) {
+      const VerifyStat s = merged(p.stat + ((int64_t)p.n_seq * p.N + node0 + i) * p.parts, p.parts, c);
+      if (tid % 16 == 0) w.drafts[i] = s;
     }
   }
   __syncthreads();
   double pr = 0.0, q = 1.0;
   if (up >= 0 && mine >= 0) {
-    const VerifyStat s = target[up];
-    if (inv == 0.0) pr = s.top > kNegInf && s.first == mine ? 1.0 : 0.0;
-    else if (s.sum > 0.0) pr = weight(load1<F32>(row_at<F32>(p.logits, (node0 + up) * p.row), mine), s.top, inv) * (1.0 / s.sum);
+    const VerifyStat s = w.target[up];
+    if (c == 0.0) pr = s.top > kNegInf && s.first == mine ? 1.0 : 0.0;
+    else if (s.sum > 0.0) pr = weight(x, s.top, c) * (1.0 / s.sum);
     if (rows) {
-      const VerifyStat d = drafts[tid];
-      q = d.sum > 0.0 ? weight(load1<F32>(row_at<F32>(p.draft, (node0 + tid) * p.draft_row), mine), d.top, inv) * (1.0 / d.sum) : 0.0;
+      const VerifyStat d = w.drafts[tid];
+      q = d.sum > 0.0 ? weight(y, d.top, c) * (1.0 / d.sum) : 0.0;
     }
   }
-  prob[tid] = pr;
-  from[tid] = q;
+  w.prob[tid] = pr;
+  w.from[tid] = q;
   __syncthreads();
-
-  // The walk, the same in all threads.
   int cur = 0, n_path = 1, n_tried = 0;
-  double off = 0.0;                  // what the point masses of those tried have taken off
-  if (tid == 0) p.path[node0] = 0;
-  for (int w = 0; w * 64 < n;) {     // the children of cur among nodes 64 w .. + 63
-    const int j = w * 64 + lane;
-    unsigned long long todo = __ballot(j > cur && j < n && parent[j < n ? j : 0] == cur);
+  double off = 0.0;                           // what the point masses of those tried have taken off
+  if (write && tid == 0) p.path[node0] = 0;
+  for (int g = 0; g * 64 < n;) {              // the children of cur among nodes 64 g .. + 63
+    const int j = g * 64 + lane;
+    unsigned long long todo = __ballot(j > cur && j < n && w.parent[j < n ? j : 0] == cur);
     bool moved = false;
     while (todo) {
-      const int i = w * 64 + __builtin_ctzll(todo);
+      const int i = g * 64 + __builtin_ctzll(todo);
       todo &= todo - 1;
-      const int t = token[i];
+      const int t = w.token[i];
       if (t < 0) continue;
-      double r = prob[i];
-      bool again = false;            // a point mass on this token has been taken off already
-      if (rows && n_tried > 0) {     // the sum that the child before has left
-        const VerifyStat s = target[cur];
+      double r = w.prob[i];
+      bool again = false;                     // a point mass on this token has been taken off already
+      if (rows && n_tried > 0) {              // the sum that the child before has left
+        const VerifyStat s = w.target[cur];
         const void* row = row_at<F32>(p.logits, (node0 + cur) * p.row);
         double z = 0.0;
 #pragma unroll 1
         for (int v = tid * 8; v < p.V; v += kThreads * 8) {
-          float x[8];
-          double y[8], unused[8];
-          load8<F32>(x, row, v, p.V);
-          rest_of<F32>(y, unused, p, node0, s, drafts, x, v, tried, left, n_tried, inv);
+          float x8[8];
+          double y8[8], unused[8];
+          load8<F32>(x8, row, v, p.V);
+          rest_of<F32>(y8, unused, p, node0, s, w.drafts, x8, v, w.tried, w.left, n_tried, c);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) z += y[e];
+          for (int e = 0; e < 8; ++e) z += y8[e];
         }
-        z = sum_threads(z, sums);
+        z = sum_threads(z, w.sums);
         if (z > 0.0) {
-          if (tid == 0) left[n_tried - 1] = z;
+          if (tid == 0) w.left[n_tried - 1] = z;
         } else {
-          n_tried -= 1;              // nothing: it stays as it was before
+          n_tried -= 1;                       // nothing: it stays as it was before
         }
         __syncthreads();
-        if (n_tried > 0) r = rest_of_one<F32>(p, node0, s, drafts, t, row, tried, left, n_tried, inv);
+        if (n_tried > 0) r = rest_of_one<F32>(p, node0, s, w.drafts, t, row, w.tried, w.left, n_tried, c);
       } else if (!rows) {
-        for (int k = 0; k < n_tried; ++k) again = again || token[tried[k]] == t;
+        for (int k = 0; k < n_tried; ++k) again = again || w.token[w.tried[k]] == t;
         r = again ? 0.0 : r / (1.0 - off);
       }
-      if ((double)u[i] * from[i] < r) {
+      if ((double)w.u[i] * w.from[i] < r) {
         cur = i;
-        if (tid == 0) p.path[node0 + n_path] = i;
+        if (write && tid == 0) p.path[node0 + n_path] = i;
         n_path += 1;
         n_tried = 0;
         off = 0.0;
@@ -329,141 +353,183 @@ __global__ __launch_bounds__(kThreads) void verify_walk_kernel(VerifyParams p) {
         break;
       }
       // (a token without weight takes nothing off, and one that has all of it leaves it as it is)
-      if (rows || (!again && r > 0.0 && 1.0 - off - prob[i] > 0.0)) {
-        off += prob[i];
-        __syncthreads();             // (tried has been read)
-        if (tid == 0) tried[n_tried] = i;
+      if (rows || (!again && r > 0.0 && 1.0 - off - w.prob[i] > 0.0)) {
+        off += w.prob[i];
+        __syncthreads();                      // (tried has been read)
+        if (tid == 0) w.tried[n_tried] = i;
         n_tried += 1;
         __syncthreads();
       }
     }
-    w = moved ? cur / 64 : w + 1;
+    g = moved ? cur / 64 : g + 1;
   }
-  if (tid >= n_path && tid < p.N) p.path[node0 + tid] = -1;
-  if (tid < n_tried) {
-    p.tried[node0 + tid] = tried[tid];
-    p.left[node0 + tid] = left[tid];
+  if (write) {
+    if (tid >= n_path && tid < p.N) p.path[node0 + tid] = -1;
+    if (tid == 0) p.n_path[b] = n_path;
   }
+  return VerifyEnd{cur, n_tried};
+}
+
+// A sequence without nodes.
+__device__ __forceinline__ void no_walk(const VerifyParams& p, int b) {
+  const int tid = threadIdx.x;
+  if (tid < p.N) p.path[(int64_t)b * p.N + tid] = -1;
   if (tid == 0) {
-    p.n_path[b] = n_path;
-    p.end[b] = VerifyEnd{cur, n_tried};
+    p.n_path[b] = 0;
+    p.next[b] = -1;
   }
 }
 
-// Tokens whose point masses were taken off have no weight: -inf in their place.  x[k][e]: element v0 + k kThreads 8 + e.
-template <int K>
-__device__ __forceinline__ void take_off(const VerifyParams& p, int64_t node0, int n_tried, float (&x)[K][8], int v0) {
-#pragma unroll 1
-  for (int j = 0; j < n_tried; ++j) {
-    const int at = p.token[node0 + p.tried[node0 + j]] - v0;
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (at == k * kThreads * 8 + e) x[k][e] = kNegInf;
-  }
-}
-
-// Weights of the last node's row, a part each.
+// With draft rows: the walk, by every workgroup of a sequence, and the sums over a part of the rows it has ended with, in 64 bits.
 template <bool F32>
-__global__ __launch_bounds__(kThreads) void verify_mass_kernel(VerifyParams p) {
-  __shared__ double sums[kWaves];
-  __shared__ Top tops[kWaves];
+__global__ __launch_bounds__(kThreads) void verify_walk_kernel(VerifyParams p) {
+  __shared__ Walk w;
   const int part = (uint32_t)blockIdx.x % (uint32_t)p.parts, b = (uint32_t)blockIdx.x / (uint32_t)p.parts, tid = threadIdx.x;
-  const VerifyEnd e = p.end[b];
-  if (e.last < 0) return;
-  const int64_t node0 = (int64_t)b * p.N;
-  const double inv = exponent_scale(p, b);
-  const void* row = row_at<F32>(p.logits, (node0 + e.last) * p.row);
-  const int v0 = part * kVerifyPart + tid * 8;
-  float x[kPer / 8][8];
-#pragma unroll
-  for (int k = 0; k < kPer / 8; ++k) load8<F32>(x[k], row, v0 + k * kThreads * 8, p.V);
-  const bool rows = p.draft && inv > 0.0 && e.n_tried > 0;
-  if (!rows && inv > 0.0) take_off(p, node0, e.n_tried, x, v0);
-  Top t{kNegInf, INT32_MAX};
-#pragma unroll
-  for (int k = 0; k < kPer / 8; ++k)
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (x[k][i] > t.x) t = Top{x[k][i], v0 + k * kThreads * 8 + i};
-  t = top_of_threads(t, tops);
-  double all = 0.0, without = 0.0;
-  if (inv > 0.0) {
-    if (rows) {
-      const VerifyStat s = p.all[node0 + e.last];
-#pragma unroll 1
-      for (int k = 0; k < kPer / 8; ++k) {
-        const int v = v0 + k * kThreads * 8;
-        if (v >= p.V) break;
-        float y[8];
-        double r[8], before[8];
-        load8<F32>(y, row, v, p.V);
-        rest_of<F32>(r, before, p, node0, s, p.draft_all + node0, y, v, p.tried + node0, p.left + node0, e.n_tried, inv);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          all += r[i];
-          without += before[i];
-        }
-      }
-    } else {
-      // relative to the part's largest logit, so that the whole row's is not needed
-#pragma unroll
-      for (int k = 0; k < kPer / 8; ++k)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) all += weight(x[k][i], t.x, inv);
-      without = all;
-    }
-    all = sum_threads(all, sums);
-    without = sum_threads(without, sums);
+  const int n = nodes_of(p, b);
+  const double c = exponent_scale(p, b);
+  if (n == 0) {
+    if (part == 0) no_walk(p, b);
+    return;
   }
-  if (tid == 0) {
-    p.mass[((int64_t)b * p.parts + part) * 2] = all;
-    p.mass[((int64_t)b * p.parts + part) * 2 + 1] = without;
-    p.top[(int64_t)b * p.parts + part] = VerifyStat{0.0, t.x, t.first};
+  const VerifyEnd e = take_walk<F32>(p, b, n, c, w, part == 0);
+  const int64_t node0 = (int64_t)b * p.N;
+  if (part == 0) {
+    if (tid < e.n_tried) {
+      p.tried[node0 + tid] = w.tried[tid];
+      p.left[node0 + tid] = w.left[tid];
+    }
+    if (tid == 0) p.end[b] = e;
+  }
+  if (c == 0.0) return;
+#pragma unroll 1
+  for (int k = -1; k < e.n_tried && e.n_tried > 0; ++k) {
+    const int i = k < 0 ? e.last : w.tried[k];
+    VerifyStat* st = p.exact + ((int64_t)(k < 0 ? 0 : p.n_seq * p.N) + node0 + i) * p.parts + part;
+    const VerifyStat was = p.stat[((int64_t)(k < 0 ? 0 : p.n_seq * p.N) + node0 + i) * p.parts + part];
+    const void* row = row_at<F32>(k < 0 ? p.logits : p.draft, (node0 + i) * (k < 0 ? p.row : p.draft_row));
+    float x[kPer / 8][8];
+    const int v0 = part * kVerifyPart + tid * 8;
+#pragma unroll
+    for (int g = 0; g < kPer / 8; ++g) load8<F32>(x[g], row, v0 + g * kThreads * 8, p.V);
+    double s = 0.0;
+#pragma unroll
+    for (int g = 0; g < kPer / 8; ++g)
+#pragma unroll
+      for (int e8 = 0; e8 < 8; ++e8) s += weight(x[g][e8], was.top, c);
+    s = sum_threads(s, w.sums);
+    if (tid == 0) *st = VerifyStat{s, was.top, was.first};
   }
 }
 
-template <bool F32>
+// Weights of the last node's row, a part of kPick elements each; the last workgroup of a sequence to end picks the token.  WALK: each
+// workgroup takes the walk itself first (there are no draft rows).
+constexpr int kPick = kVerifyPick;
+static_assert(kPick == kThreads * 8, "eight elements a thread");
+template <bool F32, bool WALK>
 __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyParams p) {
-  __shared__ double w[kVerifyPart + kThreads];  // weights of the part's elements: a place is left out behind every kPer
-  __shared__ double sums[kWaves];
+  __shared__ Walk w;
   __shared__ Top tops[kWaves];
-  __shared__ int found;
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const VerifyEnd e = p.end[b];
-  if (e.last < 0) {
-    if (tid == 0) p.next[b] = -1;
+  __shared__ int found, is_last;
+  const int part = (uint32_t)blockIdx.x % (uint32_t)p.picks, b = (uint32_t)blockIdx.x / (uint32_t)p.picks;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n = nodes_of(p, b);
+  const double c = exponent_scale(p, b);
+  if (n == 0) {
+    if (WALK && part == 0) no_walk(p, b);
     return;
   }
   const int64_t node0 = (int64_t)b * p.N;
-  const double inv = exponent_scale(p, b);
-  const VerifyStat* tops_of = p.top + (int64_t)b * p.parts;
+  VerifyEnd e;
+  if (WALK) e = take_walk<F32>(p, b, n, c, w, part == 0);
+  else e = p.end[b];
+  const bool rows = !WALK && c > 0.0 && e.n_tried > 0;
+  if (rows) {
+    if (tid < e.n_tried) {
+      w.tried[tid] = p.tried[node0 + tid];
+      w.left[tid] = p.left[node0 + tid];
+    }
+    __syncthreads();
+    for (int k = tid / 16 - 1; k < e.n_tried; k += kThreads / 16) {
+      const int i = k < 0 ? e.last : w.tried[k];
+      const VerifyStat s = merged(p.exact + ((int64_t)(k < 0 ? 0 : p.n_seq * p.N) + node0 + i) * p.parts, p.parts, c);
+      if (tid % 16 == 0) (k < 0 ? w.target : w.drafts)[i] = s;
+    }
+    __syncthreads();
+  }
+  const void* row = row_at<F32>(p.logits, (node0 + e.last) * p.row);
+  // Eight elements of a part as they count: point masses that were taken off are gone.
+  auto load = [&](float (&x)[8], int v) {
+    load8<F32>(x, row, v, p.V);
+    if (WALK && c > 0.0)
+      for (int j = 0; j < e.n_tried; ++j) {
+        const int at = w.token[w.tried[j]] - v;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = at == i ? kNegInf : x[i];
+      }
+  };
+  float x[8];
+  const int v0 = part * kPick + tid * 8;
+  load(x, v0);
   Top t{kNegInf, INT32_MAX};
-  for (int i = tid; i < p.parts; i += kThreads) t = higher(t, Top{tops_of[i].top, tops_of[i].first});
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (x[i] > t.x) t = Top{x[i], v0 + i};
   t = top_of_threads(t, tops);
-  if (t.x == kNegInf || inv == 0.0) {
+  double all = 0.0, without = 0.0;
+  if (rows) {
+    double r[8], before[8];
+    rest_of<F32>(r, before, p, node0, w.target[e.last], w.drafts, x, v0, w.tried, w.left, e.n_tried, c);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      all += r[i];
+      without += before[i];
+    }
+    without = sum_threads(without, w.sums);
+  } else if (c > 0.0) {  // relative to the part's largest logit, so that the whole row's is not needed
+#pragma unroll
+    for (int i = 0; i < 8; ++i) all += weight(x[i], t.x, c);
+  }
+  if (c > 0.0) all = sum_threads(all, w.sums);
+  // What other workgroups read is written and read past the caches that the chip's parts do not share.
+  VerifyMass* const parts = p.mass + (int64_t)b * p.picks;
+  if (tid == 0) {
+    __hip_atomic_store(&parts[part].all, all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(&parts[part].without, without, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(&parts[part].top, t.x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(&parts[part].first, t.first, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    is_last = __hip_atomic_fetch_add(p.ticket + b, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == p.picks - 1;
+    found = INT32_MAX;
+  }
+  __syncthreads();
+  if (!is_last) return;
+  auto top_of_part = [&](int i) { return __hip_atomic_load(&parts[i].top, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+  t = Top{kNegInf, INT32_MAX};
+  for (int i = tid; i < p.picks; i += kThreads) t = higher(t, Top{top_of_part(i), __hip_atomic_load(&parts[i].first, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)});
+  t = top_of_threads(t, tops);
+  if (t.x == kNegInf || c == 0.0) {
     if (tid == 0) p.next[b] = t.x == kNegInf ? -1 : t.first;
     return;
   }
   // The part, by every wavefront for itself.
-  const bool rows = p.draft && e.n_tried > 0;
-  const double* mass = p.mass + (int64_t)b * p.parts * 2;
-  auto mass_of = [&](int i, int which) { return i >= p.parts ? 0.0 : rows ? mass[2 * i + which] : mass[2 * i] * weight(tops_of[i].top, t.x, inv); };
+  auto mass_of = [&](int i, int which) {
+    if (i >= p.picks) return 0.0;
+    const double m = __hip_atomic_load(which ? &parts[i].without : &parts[i].all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return rows ? m : m * weight(top_of_part(i), t.x, c);
+  };
+  auto scan = [&](double y) {
+#pragma unroll
+    for (int i = 1; i < 64; i *= 2) {
+      const double z = __shfl_up(y, i);
+      y += lane >= i ? z : 0.0;
+    }
+    return y;
+  };
   auto total_of = [&](int which) {
     double s = 0.0;
-    for (int i = lane; i < p.parts; i += 64) s += mass_of(i, which);
+    for (int i = lane; i < p.picks; i += 64) s += mass_of(i, which);
 #pragma unroll
     for (int i = 32; i >= 1; i /= 2) s += __shfl_xor(s, i);
     return s;
-  };
-  auto scan = [&](double x) {
-#pragma unroll
-    for (int i = 1; i < 64; i *= 2) {
-      const double y = __shfl_up(x, i);
-      x += lane >= i ? y : 0.0;
-    }
-    return x;
   };
   double total = total_of(0);
   int which = 0;
@@ -471,74 +537,60 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyParams p) {
     which = 1;
     total = total_of(1);
   }
-  const double want = fmin(fmax((double)p.u[node0], 0.0), 1.0) * total;
-  int part = -1;
+  const double want = fmin(fmax((double)(WALK ? w.u[0] : p.u[node0]), 0.0), 1.0) * total;
+  int at = -1;
   double before = 0.0, c0 = 0.0;
-  for (int i0 = 0; i0 < p.parts; i0 += 64) {
-    const double m = mass_of(i0 + lane, which), c = c0 + scan(m);
-    const unsigned long long over = __ballot(m > 0.0 && c > want), some = __ballot(m > 0.0);
+  for (int i0 = 0; i0 < p.picks; i0 += 64) {
+    const double m = mass_of(i0 + lane, which), s = c0 + scan(m);
+    const unsigned long long over = __ballot(m > 0.0 && s > want), some = __ballot(m > 0.0);
     if (over | some) {
       const int l = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some);  // (without one: the last that has any weight)
-      part = i0 + l;
-      before = __shfl(c - m, l);
+      at = i0 + l;
+      before = __shfl(s - m, l);
     }
     if (over) break;
-    c0 = __shfl(c, 63);
+    c0 = __shfl(s, 63);
   }
-  if (part < 0) {
+  if (at < 0) {
     if (tid == 0) p.next[b] = -1;
     return;
   }
-  const void* row = row_at<F32>(p.logits, (node0 + e.last) * p.row);
-  auto place = [](int i) { return i + i / kPer; };
-#pragma unroll 1
-  for (int k = 0; k < kPer / 8; ++k) {
-    const int at = k * kThreads * 8 + tid * 8, v = part * kVerifyPart + at;
-    float x[1][8];
-    double y[8];
-    load8<F32>(x[0], row, v, p.V);
-    if (rows) {
-      double prev[8];
-      rest_of<F32>(y, prev, p, node0, p.all[node0 + e.last], p.draft_all + node0, x[0], v, p.tried + node0, p.left + node0, e.n_tried, inv);
+  const int v = at * kPick + tid * 8;
+  double y[8];
+  load(x, v);
+  if (rows) {
+    double prev[8];
+    rest_of<F32>(y, prev, p, node0, w.target[e.last], w.drafts, x, v, w.tried, w.left, e.n_tried, c);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = which ? prev[i] : y[i];
-    } else {
-      take_off(p, node0, e.n_tried, x, v);
+    for (int i = 0; i < 8; ++i) y[i] = which ? prev[i] : y[i];
+  } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = weight(x[0][i], t.x, inv);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[place(at + i)] = y[i];
+    for (int i = 0; i < 8; ++i) y[i] = weight(x[i], t.x, c);
   }
-  if (tid == 0) found = INT32_MAX;
-  __syncthreads();
-  const double* mine = w + tid * (kPer + 1);
   double sum = 0.0;
-#pragma unroll 8
-  for (int i = 0; i < kPer; ++i) sum += mine[i];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sum += y[i];
   double end = scan(sum);
-  if (lane == 63) sums[wave] = end;
+  if (lane == 63) w.sums[wave] = end;
   __syncthreads();
-  for (int x = 0; x < wave; ++x) end += sums[x];
+  for (int i = 0; i < wave; ++i) end += w.sums[i];
   // The first element whose sum exceeds; where rounding leaves none, the last one that has any weight.
-  double c = before + end - sum;
+  double s = before + end - sum;
   int last = -1, hit = -1;
-#pragma unroll 8
-  for (int i = 0; i < kPer; ++i) {
-    const double y = mine[i];
-    c += y;
-    if (y > 0.0) last = i;
-    if (hit < 0 && y > 0.0 && c > want) hit = i;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    s += y[i];
+    if (y[i] > 0.0) last = v + i;
+    if (hit < 0 && y[i] > 0.0 && s > want) hit = v + i;
   }
-  const int v0 = part * kVerifyPart + tid * kPer;
-  if (hit >= 0) atomicMin(&found, v0 + hit);
+  if (hit >= 0) atomicMin(&found, hit);
   __syncthreads();
   const bool none = found == INT32_MAX;
   __syncthreads();
   if (none) {
     if (tid == 0) found = -1;
     __syncthreads();
-    if (last >= 0) atomicMax(&found, v0 + last);
+    if (last >= 0) atomicMax(&found, last);
     __syncthreads();
   }
   if (tid == 0) p.next[b] = found;
@@ -547,11 +599,14 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyParams p) {
 template <bool F32>
 hipError_t launch(const VerifyParams& p, hipStream_t s) {
   const int64_t rows = (int64_t)p.n_seq * p.N * (p.draft ? 2 : 1);
-  if (rows * p.parts > INT32_MAX / kThreads) return hipErrorInvalidValue;
-  verify_stat_kernel<F32><<<dim3((unsigned)(rows * p.parts)), dim3(kThreads), 0, s>>>(p);
-  verify_walk_kernel<F32><<<dim3((unsigned)p.n_seq), dim3(kThreads), 0, s>>>(p);
-  verify_mass_kernel<F32><<<dim3((unsigned)(p.n_seq * p.parts)), dim3(kThreads), 0, s>>>(p);
-  verify_pick_kernel<F32><<<dim3((unsigned)p.n_seq), dim3(kThreads), 0, s>>>(p);
+  const dim3 b(kThreads), picks((unsigned)(p.n_seq * p.picks));
+  verify_stat_kernel<F32><<<dim3((unsigned)(rows * p.parts)), b, 0, s>>>(p);
+  if (p.draft) {
+    verify_walk_kernel<F32><<<dim3((unsigned)(p.n_seq * p.parts)), b, 0, s>>>(p);
+    verify_pick_kernel<F32, false><<<picks, b, 0, s>>>(p);
+  } else {
+    verify_pick_kernel<F32, true><<<picks, b, 0, s>>>(p);
+  }
   return hipGetLastError();
 }
 
