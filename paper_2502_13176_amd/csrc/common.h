@@ -277,7 +277,6 @@ struct AcceptParams {
   int2* table;              // [n_caches] of a cache: live rows before, new rows; null: scores are not tracked
   int32_t N, G, Hkv, batch;
   int32_t cache0, n_caches;
-  int32_t target;
   float scale_log2e;
 };
 

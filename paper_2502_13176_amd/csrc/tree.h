@@ -19,15 +19,18 @@ struct Span {
   int c_rel, first, last, part, n_parts, slot;
 };
 
+// Sum of x over the wavefront's lanes up to and with the calling one.
 __device__ __forceinline__ int scan_wave(int x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int i = 1; i < 64; i *= 2) {
-    const int y = __shfl_up(x, i);
-    x += lane >= i ? y : 0;
-  }
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);  // row_shr:2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);  // row_shr:4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);  // row_shr:8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15 into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31 into rows 2 and 3
   return x;
 }
+// x / y rounded up, 0 <= x < 2^31, y > 0, both in unsigned 32 bits.
+__device__ __forceinline__ int ceil_div(int x, int y) { return (int)(((uint32_t)x + (uint32_t)y - 1) / (uint32_t)y); }
 // Sum of x over the workgroup's threads up to and with the calling one, and over all of them.
 template <int THREADS>
 __device__ __forceinline__ int scan_threads(int x, int32_t* lds, int& total) {
@@ -55,20 +58,21 @@ __device__ __forceinline__ int scan_threads(int x, int32_t* lds, int& total) {
 template <int THREADS, class Tiles>
 __device__ __forceinline__ bool find_span(int n_caches, int target, int unit, int item, const Tiles& tiles, int32_t* lds, Span& sp) {
   constexpr int kAt = THREADS / 64;
-  auto next_run = [&](int run, int count) { return (run + max(1, (int)((int64_t)run * (count - target) / target)) + unit - 1) / unit * unit; };
+  // (any growth will do; float arithmetic is the same in every workgroup)
+  auto next_run = [&](int run, int count) { return run + unit * max(1, (int)((float)run * (float)(count - target) / (float)(target * unit))); };
   int run, t;
   if (n_caches <= 64) {  // every wavefront for itself
     const int lane = threadIdx.x & 63;
     const int mine = lane < n_caches ? tiles(lane) : 0;
-    run = max((__builtin_amdgcn_readlane(scan_wave(mine), 63) + target - 1) / target, 1);
-    run = (run + unit - 1) / unit * unit;
-    int parts = (mine + run - 1) / run, end = scan_wave(parts);
+    run = max(ceil_div(__builtin_amdgcn_readlane(scan_wave(mine), 63), target * unit), 1) * unit;
+    int parts = ceil_div(mine, run), end = scan_wave(parts);
     if (2 * n_caches <= target) {
+#pragma unroll 1
       for (int i = 0; i < 4; ++i) {
         const int count = __builtin_amdgcn_readlane(end, 63);
         if (count <= target) break;
         run = next_run(run, count);
-        parts = (mine + run - 1) / run;
+        parts = ceil_div(mine, run);
         end = scan_wave(parts);
       }
     }
@@ -87,12 +91,12 @@ __device__ __forceinline__ bool find_span(int n_caches, int target, int unit, in
     for (int c = tid + THREADS; c < n_caches; c += THREADS) all += tiles(c);
     int total;
     scan_threads<THREADS>(all, lds, total);
-    run = max((total + target - 1) / target, 1);
-    run = (run + unit - 1) / unit * unit;
+    run = max(ceil_div(total, target * unit), 1) * unit;
     if (2 * n_caches <= target && n_caches <= THREADS) {
+#pragma unroll 1
       for (int i = 0; i < 4; ++i) {
         int count;
-        scan_threads<THREADS>((mine + run - 1) / run, lds, count);
+        scan_threads<THREADS>(ceil_div(mine, run), lds, count);
         if (count <= target) break;
         run = next_run(run, count);
       }
@@ -102,7 +106,7 @@ __device__ __forceinline__ bool find_span(int n_caches, int target, int unit, in
     for (int c0 = 0; c0 < n_caches; c0 += THREADS) {
       const int c = c0 + tid;
       const int x = c0 == 0 ? mine : c < n_caches ? tiles(c) : 0;
-      const int parts = (x + run - 1) / run;
+      const int parts = ceil_div(x, run);
       int n_items, n_slots;
       const int end = items0 + scan_threads<THREADS>(parts, lds, n_items);
       const int slot_end = slots0 + scan_threads<THREADS>(parts > 1 ? parts : 0, lds, n_slots);
@@ -124,10 +128,50 @@ __device__ __forceinline__ bool find_span(int n_caches, int target, int unit, in
     t = __builtin_amdgcn_readfirstlane(tiles(c));
   }
   run = __builtin_amdgcn_readfirstlane(run);
-  sp.n_parts = __builtin_amdgcn_readfirstlane((t + run - 1) / run);
-  const int per = __builtin_amdgcn_readfirstlane(t / sp.n_parts), more = t - per * sp.n_parts;  // the first `more` items have one tile more
+  sp.n_parts = __builtin_amdgcn_readfirstlane(ceil_div(t, run));
+  const int per = __builtin_amdgcn_readfirstlane((int)((uint32_t)t / (uint32_t)sp.n_parts)), more = t - per * sp.n_parts;  // the first `more` items have one tile more
   sp.first = sp.part * per + min(sp.part, more);
   sp.last = sp.first + per + (sp.part < more ? 1 : 0);
+  return true;
+}
+
+// For launches whose work items need not be merged: tile number `at` of all, counted cache by cache, as cache and tile of it; false:
+// there are not as many.  total: all tiles (known before `at` has to be: at = f(total)).
+template <int THREADS, class Tiles, class At>
+__device__ __forceinline__ bool find_tile(int n_caches, const Tiles& tiles, const At& at_of, int32_t* lds, int& c_rel, int& tile, int& total) {
+  constexpr int kAt = THREADS / 64;
+  const int tid = threadIdx.x;
+  if (n_caches <= 64) {  // every wavefront for itself
+    const int lane = tid & 63, mine = lane < n_caches ? tiles(lane) : 0, end = scan_wave(mine);
+    total = __builtin_amdgcn_readlane(end, 63);
+    const int at = at_of(total);
+    if (at >= total) return false;
+    c_rel = __builtin_ctzll(__ballot(at < end));
+    tile = at - __builtin_amdgcn_readlane(end - mine, c_rel);
+    return true;
+  }
+  const int first = tid < n_caches ? tiles(tid) : 0;
+  int all = first;
+  for (int c = tid + THREADS; c < n_caches; c += THREADS) all += tiles(c);
+  scan_threads<THREADS>(all, lds, total);
+  total = __builtin_amdgcn_readfirstlane(total);
+  const int at = at_of(total);
+  if (at >= total) return false;
+  int before = 0;
+  for (int c0 = 0;; c0 += THREADS) {
+    const int mine = c0 == 0 ? first : c0 + tid < n_caches ? tiles(c0 + tid) : 0;
+    int sum;
+    const int end = before + scan_threads<THREADS>(mine, lds, sum);
+    if (at < end && at >= end - mine) {
+      lds[kAt] = c0 + tid;
+      lds[kAt + 1] = at - (end - mine);
+    }
+    before += sum;
+    if (at < before) break;
+  }
+  __syncthreads();
+  c_rel = __builtin_amdgcn_readfirstlane(lds[kAt]);
+  tile = __builtin_amdgcn_readfirstlane(lds[kAt + 1]);
   return true;
 }
 

@@ -592,13 +592,13 @@ hipError_t launch(const TreeParams& p, int ks, unsigned grid, hipStream_t s) {
 
 TreeLaunch tree_launch(int type, int D, int rows, int n_cus) {
   TreeLaunch t;
-  if (rows <= kStreamRows) {
+  if (rows <= (type == 2 ? kStreamRows / 2 : kStreamRows)) {  // (4-bit rows: two blocks take more registers than there are)
     t.ks = 0;
     t.row_tiles = 1;
     t.target = n_cus < kMostTreeItems ? n_cus : kMostTreeItems;
     return t;
   }
-  t.ks = 1;
+  t.ks = rows <= 64 ? 2 : 1;
   const int per = 32 * kWaves / t.ks;
   t.row_tiles = (rows + per - 1) / per;
   const int resident = tree_resident(type, D, t.ks);
