@@ -82,25 +82,37 @@ struct Shape {
   static constexpr int kWaves = score_waves(TYPE, D), kThreads = 64 * kWaves;
   static constexpr int kRow = D * (kF32 ? 4 : 2);       // bytes of a query row, and of a key row unless it has 4-bit elements
   static constexpr int kPieces = kRow / 16, kChunks = kPieces / 2;
-  static constexpr int kAhead = kMx ? 3 : 2;            // slabs of a wavefront on the way
-  static constexpr int kStage = kMx ? 0 : kSlab * kRow; // bytes of a staged slab
-  static constexpr int kRing = kMx ? 32 : 8;            // slabs of a wavefront whose new scores wait in LDS
-  static constexpr int kCopyRows = 64 / kPieces, kCopies = kSlab / kCopyRows;
+  static constexpr int kAhead = 2;                      // slabs of a wavefront on the way
+  // 4-bit rows are little to wait for and much to compute: query rows in LDS leave room for twice as many wavefronts.
+  static constexpr bool kQueriesInLds = kMx;
+  static constexpr int kResident = kMx ? 2 : 1;         // workgroups of a compute unit
+  static constexpr int kStored = kMx ? D / 2 : kRow;    // bytes of a row in the arena
+  static constexpr int kStage = kSlab * kStored;        // bytes of a staged slab
+  static constexpr int kRing = 8;                       // slabs of a wavefront whose new scores wait in LDS
+  static constexpr int kCopyPieces = kStored / 16, kCopyRows = 64 / kCopyPieces, kCopies = kSlab / kCopyRows;
+  static constexpr int kRequests = kCopies + (kMx ? 2 : 1);  // load instructions of a slab: rows, scores, scales
   // 4-bit rows: a lane takes one half of a row's codes, elements h D / 2 .. of it: chunk c is word c.
   static constexpr int kWords = D / 16;
   // piece of a row that lane half h takes as chunk c
   static __device__ __forceinline__ int piece(int c, int h) { return kMx ? h * kChunks + c : 2 * c + h; }
-  static __device__ __forceinline__ int slot(int row, int x) { return kF32 || D == 128 ? x ^ (row & 15) : x ^ (row >> 1 & 7); }
+  // where piece x of a stored row lies in LDS
+  static __device__ __forceinline__ int slot(int row, int x) {
+    if (kMx) return D == 128 ? x ^ (row >> 2 & 3) : x ^ (row >> 3 & 1);
+    return q_slot(row, x);
+  }
+  static __device__ __forceinline__ int q_slot(int row, int x) { return kF32 || D == 128 ? x ^ (row & 15) : x ^ (row >> 1 & 7); }
 };
 
 template <int TYPE, int D>
-__global__ __launch_bounds__(64 * score_waves(TYPE, D), score_waves(TYPE, D) / 4) void accept_scores_kernel(AcceptParams p) {
+__global__ __launch_bounds__(64 * score_waves(TYPE, D), score_waves(TYPE, D) / 4 * (TYPE == 2 ? 2 : 1)) void accept_scores_kernel(AcceptParams p) {
   using S = Shape<TYPE, D>;
   constexpr int kWaves = S::kWaves, kTile = kWaves * kSlab;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[S::kMx ? 16 : kWaves * S::kAhead * S::kStage];
-  __shared__ float lds_score[S::kMx ? 1 : kWaves * S::kAhead * 64];
+  __shared__ __attribute__((aligned(16))) unsigned char lds[kWaves * S::kAhead * S::kStage];
+  __shared__ float lds_score[kWaves * S::kAhead * 64];
+  __shared__ uint32_t lds_scale[S::kMx ? kWaves * S::kAhead * 64 : 1];
   __shared__ float ring[kWaves * S::kRing * kSlab];
-  __shared__ __attribute__((aligned(16))) float lse[kAcceptRows];
+  __shared__ __attribute__((aligned(16))) float lse[64];  // of the query rows in registers (or LDS)
+  __shared__ __attribute__((aligned(16))) unsigned char lds_q[S::kQueriesInLds ? 64 * S::kRow : 16];
   __shared__ int32_t scan[kWaves + 3];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n32 = lane & 31, jh = lane >> 5;
@@ -120,8 +132,8 @@ __global__ __launch_bounds__(64 * score_waves(TYPE, D), score_waves(TYPE, D) / 4
   uint32_t off[S::kCopies], c_row[S::kCopies];
 #pragma unroll
   for (int i = 0; i < S::kCopies; ++i) {
-    c_row[i] = i * S::kCopyRows + lane / S::kPieces;
-    off[i] = S::slot(c_row[i], lane % S::kPieces) * 16;
+    c_row[i] = i * S::kCopyRows + lane / S::kCopyPieces;
+    off[i] = S::slot(c_row[i], lane % S::kCopyPieces) * 16;
   }
   float* const mine = ring + wave * S::kRing * kSlab;
 
@@ -134,39 +146,38 @@ __global__ __launch_bounds__(64 * score_waves(TYPE, D), score_waves(TYPE, D) / 4
   const int tile_end = min(tile + left, (n + kTile - 1) / kTile);
   left -= tile_end - tile;
   const int slab_end = min(tile_end * kWaves, (n + kSlab - 1) / kSlab);
-  struct Request {  // 4-bit rows: a lane's codes with their scales, and the score of row n32; others are on their way to LDS
-    u32x4_t codes[S::kMx ? S::kWords / 4 : 1];
-    uint32_t bytes;
-    float score;
-  } rq[S::kAhead];
-  auto request = [&](Request& r, int buf, int slab) {
+  // Rows, scores and scales of a slab, straight to LDS.  (Codes are read with the ordinary hint: a cache line of theirs is asked for
+  // by two instructions, and is fetched twice without a stay in the cache, 53 / 58 us.)
+  auto request = [&](int buf, int slab) {
     const uint32_t most = n - 1 - slab * kSlab;  // rows past the last repeat it
     const int64_t first = row0 + (int64_t)slab * kSlab;
-    const uint32_t at = min((uint32_t)n32, most);
-    if constexpr (S::kMx) {
-      const unsigned char* src = Kp + first * (D / 2);
-      const uint8_t* scale = p.kv_scale + first * (D / 16);
+    const uint32_t at = wave * S::kAhead + buf;
+    const uint32_t dst = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds + at * S::kStage;
+    const uint32_t dst_score = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float*)lds_score + at * 256;
+    const unsigned char* src = Kp + first * S::kStored;
+    const float* src_score = p.score + first;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (what lay there has been read)
 #pragma unroll
-      for (int i = 0; i < S::kWords / 4; ++i) r.codes[i] = *reinterpret_cast<const u32x4_t*>(src + (at * (D / 2) + jh * (D / 4) + i * 16));
-      r.bytes = D == 128 ? *reinterpret_cast<const uint16_t*>(scale + (at * (D / 16) + jh * 2)) : scale[at * (D / 16) + jh];
-      r.score = p.score[first + at];
-    } else {
-      const uint32_t dst = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds + (wave * S::kAhead + buf) * S::kStage;
-      const uint32_t dst_score = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float*)lds_score + (wave * S::kAhead + buf) * 256;
-      const unsigned char* src = Kp + first * S::kRow;
-      const float* src_score = p.score + first;
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (what lay there has been read)
-#pragma unroll
-      for (int i = 0; i < S::kCopies; ++i)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                     :: "s"(dst + i * 1024), "v"(min(c_row[i], most) * (uint32_t)S::kRow + off[i]), "s"(src) : "memory", "m0");
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" :: "s"(dst_score), "v"(at * 4), "s"(src_score) : "memory", "m0");
+    for (int i = 0; i < S::kCopies; ++i) {
+      const uint32_t from = min(c_row[i], most) * (uint32_t)S::kStored + off[i];
+      if constexpr (S::kMx)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst + i * 1024), "v"(from), "s"(src) : "memory", "m0");
+      else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "s"(dst + i * 1024), "v"(from), "s"(src) : "memory", "m0");
+    }
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+                 :: "s"(dst_score), "v"(min((uint32_t)n32, most) * 4), "s"(src_score) : "memory", "m0");
+    if constexpr (S::kMx) {  // a row's D / 16 scale bytes: two words or one
+      const uint8_t* src_scale = p.kv_scale + first * (D / 16);
+      const uint32_t dst_scale = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint32_t*)lds_scale + at * 256;
+      const uint32_t r = D == 128 ? lane / 2 : n32, from = min(r, most) * (D / 16) + (D == 128 ? lane % 2 * 4 : 0);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" :: "s"(dst_scale), "v"(from), "s"(src_scale) : "memory", "m0");
     }
   };
   int slab = tile * kWaves + wave;
 #pragma unroll
   for (int a = 0; a < S::kAhead; ++a)
-    if (slab + a * kWaves < slab_end) request(rq[a], a, slab + a * kWaves);
+    if (slab + a * kWaves < slab_end) request(a, slab + a * kWaves);
 
   // Query row r of the path; rows past the last repeat it and weigh nothing.
   const int h = (uint32_t)c_rel % (uint32_t)p.Hkv, s_rel = (uint32_t)c_rel / (uint32_t)p.Hkv, b = (uint32_t)s_rel % (uint32_t)p.batch;
@@ -177,13 +188,24 @@ __global__ __launch_bounds__(64 * score_waves(TYPE, D), score_waves(TYPE, D) / 4
 #pragma unroll
     for (int c = 0; c < S::kChunks; ++c) qa[c] = *reinterpret_cast<const u32x4_t*>(src + S::piece(c, jh) * 16);
   };
-  u32x4_t qa[2][S::kChunks];
-  load_q(qa[0], 0);
-  if (n_blocks > 1) load_q(qa[1], 32);
-  __syncthreads();  // (the normalisers of the cache before have been read)
-  for (int r = tid; r < n_blocks * 32; r += S::kThreads)
-    lse[r] = r < n_rows ? *reinterpret_cast<const float*>(row_of(p.lse, s_rel, path[(uint32_t)r / (uint32_t)p.G], h * p.G + (uint32_t)r % (uint32_t)p.G))
-                        : __builtin_huge_valf();
+  auto lse_of = [&](int r) {
+    return r < n_rows ? *reinterpret_cast<const float*>(row_of(p.lse, s_rel, path[(uint32_t)r / (uint32_t)p.G], h * p.G + (uint32_t)r % (uint32_t)p.G))
+                      : __builtin_huge_valf();
+  };
+  u32x4_t qa[S::kQueriesInLds ? 1 : 2][S::kChunks];
+  if constexpr (!S::kQueriesInLds) {
+    load_q(qa[0], 0);
+    if (n_blocks > 1) load_q(qa[1], 32);
+  }
+  __syncthreads();  // (what the cache before needed has been read)
+  if (tid < 64) lse[tid] = lse_of(tid);
+  if constexpr (S::kQueriesInLds) {
+    for (int x = tid; x < min(n_blocks, 2) * 32 * S::kPieces; x += S::kThreads) {  // (rows past the last repeat it)
+      const uint32_t r = x / S::kPieces, piece = x % S::kPieces, at = min(r, (uint32_t)n_rows - 1);
+      *reinterpret_cast<u32x4_t*>(lds_q + r * S::kRow + S::q_slot(r, piece) * 16) =
+          *reinterpret_cast<const u32x4_t*>(row_of(p.q, s_rel, path[at / (uint32_t)p.G], h * p.G + at % (uint32_t)p.G) + piece * 16);
+    }
+  }
   __syncthreads();
   // register i of a block's logits: row 32 blk + 8 (i / 4) + 4 h + i % 4; a path's row j is seen by its nodes from j on
   auto product = [&](floatx16_t& s, const u32x4_t& q, const u32x4_t& k, bool first) {
@@ -198,20 +220,27 @@ __global__ __launch_bounds__(64 * score_waves(TYPE, D), score_waves(TYPE, D) / 4
   };
   auto weights = [&](const floatx16_t& s, int blk, int slab, float& sum) {
     const float* z = lse + blk * 32 + 4 * jh;
-    if ((slab + 1) * kSlab > n_old) {
-      const int first_row = (slab * kSlab + n32 - n_old) * p.G - blk * 32 - 4 * jh;
+    const bool fresh = (slab + 1) * kSlab > n_old;  // new rows among them
+    const int first_row = fresh ? (slab * kSlab + n32 - n_old) * p.G - blk * 32 - 4 * jh : INT32_MIN;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float w = fast_exp2(fmaf(s[i], cs, -z[8 * (i / 4) + i % 4]));
-        sum += 8 * (i / 4) + i % 4 >= first_row ? w : 0.f;
+    for (int q = 0; q < 4; ++q) {
+      if (blk * 32 + 8 * q >= n_rows) break;
+      const floatx4_t y = *reinterpret_cast<const floatx4_t*>(z + 8 * q);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float w = fast_exp2(fmaf(s[4 * q + i], cs, -y[i]));
+        sum += 8 * q + i >= first_row ? w : 0.f;
       }
-    } else {
+    }
+  };
+  // Blocks beyond those two, of long paths: their rows and normalisers come from memory, again for every slab.
+  auto weights_of_far_rows = [&](const floatx16_t& s, int blk, int slab, float& sum) {
+    const int first_row = (slab * kSlab + n32 - n_old) * p.G - blk * 32 - 4 * jh;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const floatx4_t y = *reinterpret_cast<const floatx4_t*>(z + 8 * q);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum += fast_exp2(fmaf(s[4 * q + i], cs, -y[i]));
-      }
+    for (int i = 0; i < 16; ++i) {
+      const int r = 8 * (i / 4) + i % 4;
+      const float w = fast_exp2(fmaf(s[i], cs, -lse_of(blk * 32 + 4 * jh + r)));
+      sum += r >= first_row ? w : 0.f;
     }
   };
   // New scores are stored several slabs at a time: whoever waits for a load also waits for the stores in front of it.
@@ -229,53 +258,73 @@ __global__ __launch_bounds__(64 * score_waves(TYPE, D), score_waves(TYPE, D) / 4
     waiting = 0;
   };
   for (int buf = 0; slab < slab_end; slab += kWaves) {
-    if constexpr (!S::kMx) {
-      // (loads come back in order: with that many outstanding, stores among them or not, this slab's are there)
-      if (slab + (S::kAhead - 1) * kWaves < slab_end) asm volatile("s_waitcnt vmcnt(%0)" :: "n"((S::kCopies + 1) * (S::kAhead - 1)) : "memory");
-      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // (loads come back in order: with as many outstanding as have been asked for behind them, stores among them or not, this slab's
+    // are there)
+    if (slab + (S::kAhead - 1) * kWaves < slab_end) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(S::kRequests * (S::kAhead - 1)) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const int at = wave * S::kAhead + buf;
+    const unsigned char* src = lds + at * S::kStage + n32 * S::kStored;
+    u32x4_t codes[S::kMx ? S::kWords / 4 : 1];  // half a row's
+    uint32_t bytes = 0;
+    if constexpr (S::kMx) {
+#pragma unroll
+      for (int i = 0; i < S::kWords / 4; ++i) codes[i] = *reinterpret_cast<const u32x4_t*>(src + S::slot(n32, jh * (S::kWords / 4) + i) * 16);
+      bytes = D == 128 ? lds_scale[at * 64 + n32 * 2] >> (16 * jh) : lds_scale[at * 64 + n32] >> (8 * jh);
     }
-    const unsigned char* src = lds + (wave * S::kAhead + buf) * S::kStage + n32 * S::kRow;
     auto key = [&](int c) {  // chunk c of row n32 of the slab
       if constexpr (S::kMx) {
-        const uint4 x = mx_values(rq[0].codes[c / 4][c % 4], mx_scale(rq[0].bytes >> (8 * (c / 4)) & 255));
+        const uint4 x = mx_values(codes[c / 4][c % 4], mx_scale(bytes >> (8 * (c / 4)) & 255));
         return u32x4_t{x.x, x.y, x.z, x.w};
       } else {
         return *reinterpret_cast<const u32x4_t*>(src + S::slot(n32, 2 * c + jh) * 16);
       }
     };
-    const float before = S::kMx ? rq[0].score : lds_score[(wave * S::kAhead + buf) * 64 + n32];
+    const float before = lds_score[at * 64 + n32];
     float sum = 0.f;
-    floatx16_t s0, s1;
-    if (n_blocks == 1) {
-#pragma unroll
-      for (int c = 0; c < S::kChunks; ++c) product(s0, qa[0][c], key(c), c == 0);
-    } else if (n_blocks == 2) {
-#pragma unroll
-      for (int c = 0; c < S::kChunks; ++c) {
-        const u32x4_t k = key(c);
-        product(s0, qa[0][c], k, c == 0);
-        product(s1, qa[1][c], k, c == 0);
-      }
-    } else {  // query rows beyond those in registers: from memory, again for every slab
+    floatx16_t s0;
+    auto far_rows = [&]() {
 #pragma unroll 1
-      for (int blk = 0; blk < n_blocks; ++blk) {
-        load_q(qa[0], blk * 32);
+      for (int blk = 2; blk < n_blocks; ++blk) {
+        u32x4_t q[S::kChunks];
+        load_q(q, blk * 32);
 #pragma unroll
-        for (int c = 0; c < S::kChunks; ++c) product(s0, qa[0][c], key(c), c == 0);
+        for (int c = 0; c < S::kChunks; ++c) product(s0, q[c], key(c), c == 0);
+        weights_of_far_rows(s0, blk, slab, sum);
+      }
+    };
+    const int ahead = slab + S::kAhead * kWaves;
+    if constexpr (S::kQueriesInLds) {  // (the codes are in registers)
+      if (ahead < slab_end) request(buf, ahead);
+#pragma unroll 1
+      for (int blk = 0; blk < min(n_blocks, 2); ++blk) {
+#pragma unroll
+        for (int c = 0; c < S::kChunks; ++c)
+          product(s0, *reinterpret_cast<const u32x4_t*>(lds_q + (blk * 32 + n32) * S::kRow + S::q_slot(n32, S::piece(c, jh)) * 16), key(c), c == 0);
         weights(s0, blk, slab, sum);
       }
-    }
-    const int ahead = slab + S::kAhead * kWaves;
-    if constexpr (S::kMx) {
-#pragma unroll
-      for (int a = 0; a + 1 < S::kAhead; ++a) rq[a] = rq[a + 1];
-      if (ahead < slab_end) request(rq[S::kAhead - 1], 0, ahead);
+      far_rows();
     } else {
-      if (ahead < slab_end) request(rq[0], buf, ahead);
-      buf = buf + 1 == S::kAhead ? 0 : buf + 1;
+      floatx16_t s1;
+      if (n_blocks == 1) {
+#pragma unroll
+        for (int c = 0; c < S::kChunks; ++c) product(s0, qa[0][c], key(c), c == 0);
+      } else {
+#pragma unroll
+        for (int c = 0; c < S::kChunks; ++c) {
+          const u32x4_t k = key(c);
+          product(s0, qa[0][c], k, c == 0);
+          product(s1, qa[1][c], k, c == 0);
+        }
+      }
+      if (n_blocks <= 2 && ahead < slab_end) request(buf, ahead);
+      weights(s0, 0, slab, sum);
+      if (n_blocks > 1) weights(s1, 1, slab, sum);
+      if (n_blocks > 2) {
+        far_rows();
+        if (ahead < slab_end) request(buf, ahead);
+      }
     }
-    if (n_blocks <= 2) weights(s0, 0, slab, sum);
-    if (n_blocks == 2) weights(s1, 1, slab, sum);
+    buf = buf + 1 == S::kAhead ? 0 : buf + 1;
     sum += __shfl_xor(sum, 32);
     if (jh == 0) mine[waiting * kSlab + n32] = before + sum;
     if (++waiting == S::kRing) store(slab - (S::kRing - 1) * kWaves);
@@ -287,6 +336,7 @@ __global__ __launch_bounds__(64 * score_waves(TYPE, D), score_waves(TYPE, D) / 4
 
 template <int TYPE, int D>
 hipError_t launch_scores(const AcceptParams& p, unsigned grid, hipStream_t s) {
+  static_assert(Shape<TYPE, D>::kResident == (TYPE == 2 ? 2 : 1), "");
   accept_scores_kernel<TYPE, D><<<dim3(grid), dim3(Shape<TYPE, D>::kThreads), 0, s>>>(p);
   return hipGetLastError();
 }
@@ -306,7 +356,7 @@ hipError_t launch_append_accepted(const AcceptParams& p, int type, int D, int n_
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.table) return e;
-  const unsigned grid = (unsigned)n_cus;
+  const unsigned grid = (unsigned)n_cus * (type == 2 ? 2 : 1);  // one round
   return type == 1   ? D == 128 ? launch_scores<1, 128>(p, grid, s) : launch_scores<1, 64>(p, grid, s)
          : type == 2 ? D == 128 ? launch_scores<2, 128>(p, grid, s) : launch_scores<2, 64>(p, grid, s)
                      : D == 128 ? launch_scores<0, 128>(p, grid, s) : launch_scores<0, 64>(p, grid, s);

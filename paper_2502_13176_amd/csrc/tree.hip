@@ -249,9 +249,13 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
       const uint32_t dst = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)(value ? lds_v[kt & 1] : lds_k[kt & 1]) +
                            wave * (kTile / kWaves) * kRow;
 #pragma unroll
-      for (int i = 0; i < S::kCopies; ++i)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                     :: "s"(dst + i * 1024), "v"(min(c_row[i], most) * (uint32_t)kStored + (value ? v_off[i] : k_off[i])), "s"(src) : "memory", "m0");
+      for (int i = 0; i < S::kCopies; ++i) {
+        const uint32_t at = min(c_row[i], most) * (uint32_t)kStored + (value ? v_off[i] : k_off[i]);
+        if (p.row_tiles == 1)  // read once
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "s"(dst + i * 1024), "v"(at), "s"(src) : "memory", "m0");
+        else
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst + i * 1024), "v"(at), "s"(src) : "memory", "m0");
+      }
     }
   };
   auto put_mx = [&](int buf, int value, int r, int piece, u32x4_t codes, uint32_t byte) {

@@ -141,7 +141,7 @@ __global__ __launch_bounds__(64 * stream_waves(TYPE, D), stream_waves(TYPE, D) /
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (what lay there has been read)
 #pragma unroll
       for (int i = 0; i < S::kCopies; ++i)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
                      :: "s"(dst + i * 1024), "v"(min(c_row[i], most) * (uint32_t)S::kStored + (value ? v_off[i] : k_off[i])), "s"(src) : "memory", "m0");
     }
   };
