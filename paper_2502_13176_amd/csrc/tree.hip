@@ -38,21 +38,16 @@ constexpr float kMaxSlack = 8.f;  // a logit may exceed its row's reference maxi
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Keys per LDS stage, by the rows' type, head dimension and the wavefronts that share 32 query rows.
-constexpr int tree_tile(int ks) { return ks == 4 ? 128 : 64; }
-// Whether four wavefronts may share 32 query rows: two stages of 128 rows of K and V have to fit the LDS.
-constexpr bool tree_shares_four(int type, int D) { return !(type == 1 && D == 128); }
+constexpr int kKeyTile = 64;  // keys per LDS stage
 // Workgroups that fit a compute unit.
-constexpr int tree_resident(int type, int D, int ks) {
-  return 4 * tree_tile(ks) * D * (type == 1 ? 4 : 2) > 72 * 1024 ? 1 : 2;
-}
+constexpr int tree_resident(int type, int D) { return 4 * kKeyTile * D * (type == 1 ? 4 : 2) > 72 * 1024 ? 1 : 2; }
 
 // What follows from the rows' type (BAKLAVA_BF16, F32, MXFP4), the head dimension and KS, the wavefronts that share 32 query rows.
 template <int TYPE, int D, int KS>
 struct Shape {
   static constexpr bool kF32 = TYPE == 1, kMx = TYPE == 2;
   static constexpr int kRows = 32 * kWaves / KS;             // query rows of a workgroup
-  static constexpr int kTile = tree_tile(KS);       // keys per LDS stage
+  static constexpr int kTile = kKeyTile;
   static constexpr int kSlabs = kTile / 32 / KS;             // slabs of 32 keys that a wavefront takes of it
   static constexpr int kRow = D * (kF32 ? 4 : 2);            // bytes of a row in LDS
   static constexpr int kPieces = kRow / 16;
@@ -69,11 +64,13 @@ struct Shape {
   }
   static __device__ __forceinline__ int v_slot(int row, int x) {
     if (kF32) return x ^ 8 * (row >> 2 & 1);
-    return D == 128 ? x ^ 4 * (row & 3) : x ^ 4 * (row >> 1 & 1);
+    // (values of 4-bit rows are written 16 bytes at a time, by lanes of few pieces of several rows: these spread, too)
+    return D == 128 ? x ^ 4 * (row & 3) ^ (kMx ? (row ^ row >> 2) & 3 : 0) : x ^ 4 * (row >> 1 & 1);
   }
 };
 
-template <int TYPE, int D, int KS>
+// ONCE: a work item's rows are read by one workgroup, past the caches (577 MB are read in 88 us so, in 101 with the ordinary hint).
+template <int TYPE, int D, int KS, bool ONCE>
 __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
   using S = Shape<TYPE, D, KS>;
   constexpr int kSlabs = S::kSlabs, kBlocks = S::kBlocks, kRow = S::kRow, kTile = S::kTile;
@@ -184,7 +181,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
       // A transposed read hands lane m of a 16-lane group element m of the 16 d values the group points at, for 4 consecutive
       // keys: the group (h, d half) reads keys 4 h .. + 3 of each 8, two reads per 16 keys.
       const int n16 = lane & 15, half = (lane >> 4) & 1, k4 = n16 >> 2;
-      const unsigned char* at0 = base + (4 * jh + k4) * kRow + half * 32 + (n16 & 3) * 8;
+      const unsigned char* at0 = base + (4 * jh + k4) * kRow + (n16 & 1) * 8;
+      const int piece = 2 * half + (n16 >> 1 & 1);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         bf16x8_t pb;
@@ -197,9 +195,9 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
 #pragma unroll
         for (int x = 0; x < kBlocks; ++x) {
           typedef __attribute__((address_space(3))) s16x4_t* lds_ptr_t;
-          const unsigned char* at = at0 + u * 16 * kRow + (D == 128 ? x ^ k4 : x ^ (k4 >> 1)) * 64;
-          const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)at);
-          const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(at + 8 * kRow));
+          const unsigned char* at = at0 + u * 16 * kRow;  // (keys 16 u + 4 h + k4 and 8 further)
+          const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(at + S::v_slot(4 * jh + k4, 4 * x + piece) * 16));
+          const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(at + 8 * kRow + S::v_slot(8 + 4 * jh + k4, 4 * x + piece) * 16));
           s16x8_t v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
           if (finite) {
 #pragma unroll
@@ -232,7 +230,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
   struct Codes {
     u32x4_t c[S::kMx ? S::kMxPer : 1];
     uint32_t byte[S::kMx ? S::kMxPer : 1];
-  } codes_k, codes_v;
+  };
   auto request = [&](Codes& codes, int value, int kt) {
     const uint32_t most = n_live - 1 - kt * kTile;
     const int64_t first = row0 + (int64_t)kt * kTile;
@@ -251,7 +249,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
 #pragma unroll
       for (int i = 0; i < S::kCopies; ++i) {
         const uint32_t at = min(c_row[i], most) * (uint32_t)kStored + (value ? v_off[i] : k_off[i]);
-        if (p.row_tiles == 1)  // read once
+        if constexpr (ONCE)
           asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "s"(dst + i * 1024), "v"(at), "s"(src) : "memory", "m0");
         else
           asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst + i * 1024), "v"(at), "s"(src) : "memory", "m0");
@@ -279,18 +277,25 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
   };
 
   // ---- live rows: a software pipeline, the first product of tile kt + 1 beside the exponentials of tile kt -------------------
+  // In a step the K rows of tile kt + 2 and the V rows of kt + 1 come in.  Copies to LDS are asked for at its start; codes, which
+  // wait in registers until their values can go to LDS, a step earlier.
   const int live_end = min(sp.last, live_tiles);
   if (sp.first < live_end) {
     int kt = sp.first;
-    const bool two = kt + 1 < live_end;
-    request(codes_k, 0, kt);
-    request(codes_v, 1, kt);
-    put(codes_k, 0, kt);
-    put(codes_v, 1, kt);
-    if (two) {
-      request(codes_k, 0, kt + 1);
-      put(codes_k, 0, kt + 1);
+    Codes ck, cv, nk, nv;
+    request(ck, 0, kt);
+    request(cv, 1, kt);
+    put(ck, 0, kt);
+    put(cv, 1, kt);
+    if (kt + 1 < live_end) {
+      request(ck, 0, kt + 1);
+      put(ck, 0, kt + 1);
     }
+    auto ask = [&](Codes& k, Codes& v, int kt) {
+      if (kt + 2 < live_end) request(k, 0, kt + 2);
+      if (kt + 1 < live_end) request(v, 1, kt + 1);
+    };
+    if constexpr (S::kMx) ask(ck, cv, kt);
     arrive();
     floatx16_t s[kSlabs];
     float mx = kLowest;
@@ -299,9 +304,14 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
       mx = max_of(s);
     }
     __syncthreads();  // (the first tile's K rows are overwritten in the first step)
-    auto step = [&](const floatx16_t (&s)[kSlabs], floatx16_t (&sn)[kSlabs], int kt) {
-      request(codes_k, 0, kt + 2);
-      request(codes_v, 1, kt + 1);
+    auto step = [&](const floatx16_t (&s)[kSlabs], floatx16_t (&sn)[kSlabs], int kt, Codes& ck, Codes& cv, Codes& nk, Codes& nv) {
+      if constexpr (S::kMx) {
+        request(nk, 0, kt + 3);
+        request(nv, 1, kt + 2);
+      } else {
+        request(ck, 0, kt + 2);
+        request(cv, 1, kt + 1);
+      }
       if (!idle) {
         follow_max(mx);
         logits(sn, kt + 1 & 1);
@@ -309,19 +319,17 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
         for (int sl = 0; sl < kSlabs; ++sl) outputs(s[sl], kt & 1, sl, false);
         mx = max_of(sn);
       }
-      put(codes_k, 0, kt + 2);
-      put(codes_v, 1, kt + 1);
+      put(ck, 0, kt + 2);
+      put(cv, 1, kt + 1);
       arrive();
     };
-    for (; kt + 3 < live_end; kt += 2) {
+    for (; kt + 4 < live_end; kt += 2) {
       floatx16_t sn[kSlabs];
-      step(s, sn, kt);
-      step(sn, s, kt + 1);
+      step(s, sn, kt, ck, cv, nk, nv);
+      step(sn, s, kt + 1, nk, nv, ck, cv);
     }
     for (; kt < live_end; ++kt) {
-      const bool more = kt + 1 < live_end, more_k = kt + 2 < live_end;
-      if (more_k) request(codes_k, 0, kt + 2);
-      if (more) request(codes_v, 1, kt + 1);
+      if constexpr (!S::kMx) ask(ck, cv, kt);
       if (!idle) {
         if ((kt + 1) * kTile > n_live) {
 #pragma unroll
@@ -333,10 +341,11 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
         follow_max(max_of(s));
 #pragma unroll
         for (int sl = 0; sl < kSlabs; ++sl) outputs(s[sl], kt & 1, sl, false);
-        if (more) logits(s, kt + 1 & 1);
+        if (kt + 1 < live_end) logits(s, kt + 1 & 1);
       }
-      if (more_k) put(codes_k, 0, kt + 2);
-      if (more) put(codes_v, 1, kt + 1);
+      if (kt + 2 < live_end) put(ck, 0, kt + 2);
+      if (kt + 1 < live_end) put(cv, 1, kt + 1);
+      if constexpr (S::kMx) ask(ck, cv, kt + 1);
       arrive();
     }
   }
@@ -586,9 +595,9 @@ __global__ __launch_bounds__(kThreads) void tree_merge_kernel(TreeParams p) {
 
 template <int TYPE, int D>
 hipError_t launch(const TreeParams& p, int ks, unsigned grid, hipStream_t s) {
-  if (ks == 1) tree_attn_kernel<TYPE, D, 1><<<dim3(grid), dim3(kThreads), 0, s>>>(p);
-  else if (ks == 2 || !tree_shares_four(TYPE, D)) tree_attn_kernel<TYPE, D, 2><<<dim3(grid), dim3(kThreads), 0, s>>>(p);
-  else if constexpr (tree_shares_four(TYPE, D)) tree_attn_kernel<TYPE, D, 4><<<dim3(grid), dim3(kThreads), 0, s>>>(p);
+  if (ks == 2) tree_attn_kernel<TYPE, D, 2, true><<<dim3(grid), dim3(kThreads), 0, s>>>(p);
+  else if (p.row_tiles == 1) tree_attn_kernel<TYPE, D, 1, true><<<dim3(grid), dim3(kThreads), 0, s>>>(p);
+  else tree_attn_kernel<TYPE, D, 1, false><<<dim3(grid), dim3(kThreads), 0, s>>>(p);
   return hipGetLastError();
 }
 
@@ -605,7 +614,7 @@ TreeLaunch tree_launch(int type, int D, int rows, int n_cus) {
   t.ks = rows <= 64 ? 2 : 1;
   const int per = 32 * kWaves / t.ks;
   t.row_tiles = (rows + per - 1) / per;
-  const int resident = tree_resident(type, D, t.ks);
+  const int resident = tree_resident(type, D);
   const int all = resident * n_cus < kMostTreeItems ? resident * n_cus : kMostTreeItems;
   t.target = all / t.row_tiles > 1 ? all / t.row_tiles : 1;
   return t;

@@ -1,4 +1,5 @@
-// Attention of a tree of drafted tokens over ragged caches, few query rows: up to 64 (nodes times query heads of a KV head).
+// Attention of a tree of drafted tokens over ragged caches, few query rows (nodes times query heads of a KV head): up to 64, of 4-bit
+// rows up to 32.
 //
 // Products, layouts and work items are those of tree.hip.  Here every wavefront takes all query rows, in one or two blocks of 32, and
 // streams slabs of 32 keys of its own, without a barrier: the K rows of its next slab are requested as soon as the first product
@@ -52,7 +53,8 @@ struct Shape {
   static __device__ __forceinline__ int k_slot(int r, int x) { return kF32 || D == 128 ? x ^ (r & 15) : x ^ (r >> 1 & 7); }
   static __device__ __forceinline__ int v_slot(int r, int x) {
     if (kF32) return x ^ 8 * (r >> 2 & 1);
-    return D == 128 ? x ^ 4 * (r & 3) : x ^ 4 * (r >> 1 & 1);
+    // (values of 4-bit rows are written 16 bytes at a time, by lanes of few pieces of several rows: these spread, too)
+    return D == 128 ? x ^ 4 * (r & 3) ^ (kMx ? (r ^ r >> 2) & 3 : 0) : x ^ 4 * (r >> 1 & 1);
   }
 };
 
@@ -248,7 +250,8 @@ __global__ __launch_bounds__(64 * stream_waves(TYPE, D), stream_waves(TYPE, D) /
       }
     } else {
       const int n16 = lane & 15, half = (lane >> 4) & 1, k4 = n16 >> 2;
-      const unsigned char* at0 = my_v + (4 * jh + k4) * kRow + half * 32 + (n16 & 3) * 8;
+      const unsigned char* at0 = my_v + (4 * jh + k4) * kRow + (n16 & 1) * 8;
+      const int piece = 2 * half + (n16 >> 1 & 1);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         bf16x8_t pb[RB];
@@ -259,9 +262,9 @@ __global__ __launch_bounds__(64 * stream_waves(TYPE, D), stream_waves(TYPE, D) /
 #pragma unroll
         for (int x = 0; x < kBlocks; ++x) {
           typedef __attribute__((address_space(3))) s16x4_t* lds_ptr_t;
-          const unsigned char* at = at0 + u * 16 * kRow + (D == 128 ? x ^ k4 : x ^ (k4 >> 1)) * 64;
-          const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)at);
-          const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(at + 8 * kRow));
+          const unsigned char* at = at0 + u * 16 * kRow;  // (keys 16 u + 4 h + k4 and 8 further)
+          const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(at + S::v_slot(4 * jh + k4, 4 * x + piece) * 16));
+          const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(at + 8 * kRow + S::v_slot(8 + 4 * jh + k4, 4 * x + piece) * 16));
           s16x8_t v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
           if (finite) {
 #pragma unroll
@@ -466,8 +469,8 @@ __global__ __launch_bounds__(64 * stream_waves(TYPE, D), stream_waves(TYPE, D) /
 
 template <int TYPE, int D>
 hipError_t launch(const TreeParams& p, unsigned grid, hipStream_t s) {
-  if (p.rows <= 32) tree_stream_kernel<TYPE, D, 1><<<dim3(grid), dim3(Shape<TYPE, D, 1>::kThreads), 0, s>>>(p);
-  else tree_stream_kernel<TYPE, D, 2><<<dim3(grid), dim3(Shape<TYPE, D, 2>::kThreads), 0, s>>>(p);
+  if (TYPE == 2 || p.rows <= 32) tree_stream_kernel<TYPE, D, 1><<<dim3(grid), dim3(Shape<TYPE, D, 1>::kThreads), 0, s>>>(p);
+  else if constexpr (TYPE != 2) tree_stream_kernel<TYPE, D, 2><<<dim3(grid), dim3(Shape<TYPE, D, 2>::kThreads), 0, s>>>(p);
   return hipGetLastError();
 }
 
