@@ -551,6 +551,7 @@ int baklava_read_rows(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count
  * be empty.
  * q, out rows of Hq heads, k, v rows of Hkv heads, in the context's dtype (bf16 for MXFP4); lse NULL or fp32 "rows of one
  * element" as in baklava_prompt_attn.  fp32 accumulation; softmax weights of bf16 rows enter the second product as bf16.
+ * out must not share memory with q, k or v.
  * workspace DEVICE, baklava_tree_workspace_bytes(ctx, layer_count, N) bytes, 256-byte aligned, free again once the stream has
  * passed the call; its contents do not matter.
  * Live lengths are read on the device.  Enqueues two kernels on `stream`; deterministic.

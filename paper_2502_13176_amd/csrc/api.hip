@@ -1224,7 +1224,7 @@ extern "C" int baklava_append_accepted(baklava_ctx* ctx, int32_t layer_begin, in
   if (track) {
     p.q = tree_rows(q, N, es, 1);
     p.lse = tree_rows(lse, N, 4, 1);
-    p.table = reinterpret_cast<int2*>(ctx->ws + ctx->plan.accept);
+    p.table = reinterpret_cast<int2*>(ctx->ws + ctx->plan.accept) + (int64_t)layer_begin * ctx->cpl;
   }
   p.k_plane = ctx->d.k; p.v_plane = ctx->d.v;
   p.kv_scale = reinterpret_cast<uint8_t*>(ctx->d.kv_scale);

@@ -95,9 +95,10 @@ __device__ __forceinline__ double exponent_scale(const VerifyParams& p, int b) {
   return t > 0.f ? 1.4426950408889634 / (double)t : 0.0;
 }
 
-// Sums over the workgroup, in an order that does not change.
+// Sums over the workgroup, in an order that does not change.  (Loops that a workgroup runs through once stay loops here and below: its
+// instructions come from memory, and take longer than the work.)
 __device__ __forceinline__ double sum_threads(double x, double* lds) {
-#pragma unroll
+#pragma unroll 1
   for (int i = 32; i >= 1; i /= 2) x += __shfl_xor(x, i);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
@@ -114,7 +115,7 @@ struct Top {
 };
 __device__ __forceinline__ Top higher(Top a, Top b) { return b.x > a.x || (b.x == a.x && b.first < a.first) ? b : a; }
 __device__ __forceinline__ Top top_of_threads(Top t, Top* lds) {
-#pragma unroll
+#pragma unroll 1
   for (int i = 32; i >= 1; i /= 2) t = higher(t, Top{__shfl_xor(t.x, i), __shfl_xor(t.first, i)});
   __syncthreads();
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = t;
@@ -252,15 +253,17 @@ struct Walk {
   VerifyStat target[kMostNodes], drafts[kMostNodes];
   float u[kMostNodes];
   double sums[kWaves];
+  unsigned long long stands[kMostNodes / 64];  // bits of nodes that are accepted if they are tried
+  int32_t n_tried;
 };
 
-// The walk, by all threads of a workgroup together; write: its path goes out.  n > 0.
+// Nodes of a sequence into LDS, with what the rows of those that have children say (rows: and the draft rows), and the probabilities
+// of each node's token.  Returns node threadIdx.x's parent, or -1.
 template <bool F32>
-__device__ __forceinline__ VerifyEnd take_walk(const VerifyParams& p, int b, int n, double c, Walk& w, bool write) {
+__device__ __forceinline__ int load_nodes(const VerifyParams& p, int b, int n, double c, bool rows, Walk& w) {
   static_assert(kMostNodes == kThreads, "a thread for every node");
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int tid = threadIdx.x;
   const int64_t node0 = (int64_t)b * p.N;
-  const bool rows = p.draft && c > 0.0;
   int up = -1, mine = -1;
   if (tid < n) {
     w.u[tid] = p.u[node0 + tid];
@@ -280,15 +283,13 @@ __device__ __forceinline__ VerifyEnd take_walk(const VerifyParams& p, int b, int
     if (rows) y = load1<F32>(row_at<F32>(p.draft, (node0 + tid) * p.draft_row), mine);
   }
   __syncthreads();
-  for (int i = tid / 16; i < n; i += kThreads / 16) {
-    if (w.tried[i]) {
-      const VerifyStat s = merged(p.stat + (node0 + i) * p.parts, p.parts, c);
-      if (tid % 16 == 0) w.target[i] = s;
-    }
-    if (rows && w.parent[i] >= 0) {
-      const VerifyStat s = merged(p.stat + ((int64_t)p.n_seq * p.N + node0 + i) * p.parts, p.parts, c);
-      if (tid % 16 == 0) w.drafts[i] = s;
-    }
+#pragma unroll 1
+  for (int k = tid / 16; k < (rows ? 2 * n : n); k += kThreads / 16) {  // target rows, then draft rows
+    const bool draft = k >= n;
+    const int i = draft ? k - n : k;
+    if (!draft ? w.tried[i] == 0 : w.parent[i] < 0) continue;
+    const VerifyStat s = merged(p.stat + ((draft ? (int64_t)p.n_seq * p.N : 0) + node0 + i) * p.parts, p.parts, c);
+    if (tid % 16 == 0) (draft ? w.drafts : w.target)[i] = s;
   }
   __syncthreads();
   double pr = 0.0, q = 1.0;
@@ -304,21 +305,81 @@ __device__ __forceinline__ VerifyEnd take_walk(const VerifyParams& p, int b, int
   w.prob[tid] = pr;
   w.from[tid] = q;
   __syncthreads();
-  int cur = 0, n_path = 1, n_tried = 0;
-  double off = 0.0;                           // what the point masses of those tried have taken off
+  return up;
+}
+
+__device__ __forceinline__ void write_path(const VerifyParams& p, int64_t node0, int b, int n_path) {
+  const int tid = threadIdx.x;
+  if (tid >= n_path && tid < p.N) p.path[node0 + tid] = -1;
+  if (tid == 0) p.n_path[b] = n_path;
+}
+
+// The walk where drafted tokens are point masses, by a workgroup together; write: its path goes out.  n > 0.  What those tried before
+// a node have taken off follows from its siblings, so whether a node would be accepted is known without the walk.
+template <bool F32>
+__device__ __forceinline__ VerifyEnd walk_points(const VerifyParams& p, int b, int n, double c, Walk& w, bool write) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int64_t node0 = (int64_t)b * p.N;
+  const int up = load_nodes<F32>(p, b, n, c, false, w);
+  const int mine = w.token[tid];
+  const double pr = w.prob[tid];
+  bool again = false;                         // a sibling before has taken this token off already
+#pragma unroll 1
+  for (int j = up + 1; j < tid && up >= 0; ++j) again = again || (w.parent[j] == up && w.token[j] == mine);
+  w.from[tid] = again ? 0.0 : pr;
+  if (tid < 4) w.stands[tid] = 0;
+  if (tid == 0) w.n_tried = 0;
+  __syncthreads();
+  // (a token without weight takes nothing off, and one that has all that is left leaves it as it is)
+  double off = 0.0;
+#pragma unroll 1
+  for (int j = up + 1; j < tid && up >= 0; ++j) {
+    const double q = w.parent[j] == up ? w.from[j] : 0.0;
+    if (q > 0.0 && 1.0 - off - q > 0.0) off += q;
+  }
+  const bool stands = up >= 0 && mine >= 0 && (double)w.u[tid] < (again ? 0.0 : pr / (1.0 - off));
+  const unsigned long long these = __ballot(stands);
+  if (lane == 0) w.stands[tid / 64] = these;
+  __syncthreads();
+  int cur = 0, n_path = 1;
   if (write && tid == 0) p.path[node0] = 0;
+#pragma unroll 1
+  for (int g = 0; g * 64 < n;) {              // the children of cur among nodes 64 g .. + 63, the same in all wavefronts
+    const unsigned long long hit = __ballot(w.parent[g * 64 + lane] == cur) & w.stands[g];
+    if (hit == 0) {
+      ++g;
+      continue;
+    }
+    cur = g * 64 + __builtin_ctzll(hit);
+    if (write && tid == 0) p.path[node0 + n_path] = cur;
+    n_path += 1;
+  }
+  if (up == cur && !again && pr > 0.0 && 1.0 - off - pr > 0.0) w.tried[atomicAdd(&w.n_tried, 1)] = tid;
+  __syncthreads();
+  if (write) write_path(p, node0, b, n_path);
+  return VerifyEnd{cur, w.n_tried};
+}
+
+// The walk where they were drawn from the draft rows, one child after the other.
+template <bool F32>
+__device__ __forceinline__ VerifyEnd walk_rows(const VerifyParams& p, int b, int n, double c, Walk& w, bool write) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int64_t node0 = (int64_t)b * p.N;
+  load_nodes<F32>(p, b, n, c, true, w);
+  int cur = 0, n_path = 1, n_tried = 0;
+  if (write && tid == 0) p.path[node0] = 0;
+#pragma unroll 1
   for (int g = 0; g * 64 < n;) {              // the children of cur among nodes 64 g .. + 63
-    const int j = g * 64 + lane;
-    unsigned long long todo = __ballot(j > cur && j < n && w.parent[j < n ? j : 0] == cur);
+    unsigned long long todo = __ballot(w.parent[g * 64 + lane] == cur);
     bool moved = false;
+#pragma unroll 1
     while (todo) {
       const int i = g * 64 + __builtin_ctzll(todo);
       todo &= todo - 1;
       const int t = w.token[i];
       if (t < 0) continue;
       double r = w.prob[i];
-      bool again = false;                     // a point mass on this token has been taken off already
-      if (rows && n_tried > 0) {              // the sum that the child before has left
+      if (n_tried > 0) {                      // the sum that the child before has left
         const VerifyStat s = w.target[cur];
         const void* row = row_at<F32>(p.logits, (node0 + cur) * p.row);
         double z = 0.0;
@@ -339,34 +400,23 @@ __device__ __forceinline__ VerifyEnd take_walk(const VerifyParams& p, int b, int
         }
         __syncthreads();
         if (n_tried > 0) r = rest_of_one<F32>(p, node0, s, w.drafts, t, row, w.tried, w.left, n_tried, c);
-      } else if (!rows) {
-        for (int k = 0; k < n_tried; ++k) again = again || w.token[w.tried[k]] == t;
-        r = again ? 0.0 : r / (1.0 - off);
       }
       if ((double)w.u[i] * w.from[i] < r) {
         cur = i;
         if (write && tid == 0) p.path[node0 + n_path] = i;
         n_path += 1;
         n_tried = 0;
-        off = 0.0;
         moved = true;
         break;
       }
-      // (a token without weight takes nothing off, and one that has all of it leaves it as it is)
-      if (rows || (!again && r > 0.0 && 1.0 - off - w.prob[i] > 0.0)) {
-        off += w.prob[i];
-        __syncthreads();                      // (tried has been read)
-        if (tid == 0) w.tried[n_tried] = i;
-        n_tried += 1;
-        __syncthreads();
-      }
+      __syncthreads();                        // (tried has been read)
+      if (tid == 0) w.tried[n_tried] = i;
+      n_tried += 1;
+      __syncthreads();
     }
     g = moved ? cur / 64 : g + 1;
   }
-  if (write) {
-    if (tid >= n_path && tid < p.N) p.path[node0 + tid] = -1;
-    if (tid == 0) p.n_path[b] = n_path;
-  }
+  if (write) write_path(p, node0, b, n_path);
   return VerifyEnd{cur, n_tried};
 }
 
@@ -391,7 +441,7 @@ __global__ __launch_bounds__(kThreads) void verify_walk_kernel(VerifyParams p) {
     if (part == 0) no_walk(p, b);
     return;
   }
-  const VerifyEnd e = take_walk<F32>(p, b, n, c, w, part == 0);
+  const VerifyEnd e = c > 0.0 ? walk_rows<F32>(p, b, n, c, w, part == 0) : walk_points<F32>(p, b, n, c, w, part == 0);
   const int64_t node0 = (int64_t)b * p.N;
   if (part == 0) {
     if (tid < e.n_tried) {
@@ -423,12 +473,13 @@ __global__ __launch_bounds__(kThreads) void verify_walk_kernel(VerifyParams p) {
 
 // Weights of the last node's row, a part of kPick elements each; the last workgroup of a sequence to end picks the token.  WALK: each
 // workgroup takes the walk itself first (there are no draft rows).
-constexpr int kPick = kVerifyPick;
+constexpr int kPick = kVerifyPick, kHeldParts = 256;
 static_assert(kPick == kThreads * 8, "eight elements a thread");
 template <bool F32, bool WALK>
 __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyParams p) {
   __shared__ Walk w;
   __shared__ Top tops[kWaves];
+  __shared__ VerifyMass held[kHeldParts];
   __shared__ int found, is_last;
   const int part = (uint32_t)blockIdx.x % (uint32_t)p.picks, b = (uint32_t)blockIdx.x / (uint32_t)p.picks;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -440,7 +491,7 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyParams p) {
   }
   const int64_t node0 = (int64_t)b * p.N;
   VerifyEnd e;
-  if (WALK) e = take_walk<F32>(p, b, n, c, w, part == 0);
+  if (WALK) e = walk_points<F32>(p, b, n, c, w, part == 0);
   else e = p.end[b];
   const bool rows = !WALK && c > 0.0 && e.n_tried > 0;
   if (rows) {
@@ -467,133 +518,145 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyParams p) {
         for (int i = 0; i < 8; ++i) x[i] = at == i ? kNegInf : x[i];
       }
   };
-  float x[8];
-  const int v0 = part * kPick + tid * 8;
-  load(x, v0);
-  Top t{kNegInf, INT32_MAX};
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (x[i] > t.x) t = Top{x[i], v0 + i};
-  t = top_of_threads(t, tops);
-  double all = 0.0, without = 0.0;
-  if (rows) {
-    double r[8], before[8];
-    rest_of<F32>(r, before, p, node0, w.target[e.last], w.drafts, x, v0, w.tried, w.left, e.n_tried, c);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      all += r[i];
-      without += before[i];
-    }
-    without = sum_threads(without, w.sums);
-  } else if (c > 0.0) {  // relative to the part's largest logit, so that the whole row's is not needed
-#pragma unroll
-    for (int i = 0; i < 8; ++i) all += weight(x[i], t.x, c);
-  }
-  if (c > 0.0) all = sum_threads(all, w.sums);
   // What other workgroups read is written and read past the caches that the chip's parts do not share.
   VerifyMass* const parts = p.mass + (int64_t)b * p.picks;
-  if (tid == 0) {
-    __hip_atomic_store(&parts[part].all, all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __hip_atomic_store(&parts[part].without, without, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __hip_atomic_store(&parts[part].top, t.x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __hip_atomic_store(&parts[part].first, t.first, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    is_last = __hip_atomic_fetch_add(p.ticket + b, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == p.picks - 1;
-    found = INT32_MAX;
-  }
-  __syncthreads();
-  if (!is_last) return;
-  auto top_of_part = [&](int i) { return __hip_atomic_load(&parts[i].top, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
-  t = Top{kNegInf, INT32_MAX};
-  for (int i = tid; i < p.picks; i += kThreads) t = higher(t, Top{top_of_part(i), __hip_atomic_load(&parts[i].first, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)});
-  t = top_of_threads(t, tops);
-  if (t.x == kNegInf || c == 0.0) {
-    if (tid == 0) p.next[b] = t.x == kNegInf ? -1 : t.first;
-    return;
-  }
-  // The part, by every wavefront for itself.
-  auto mass_of = [&](int i, int which) {
-    if (i >= p.picks) return 0.0;
-    const double m = __hip_atomic_load(which ? &parts[i].without : &parts[i].all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return rows ? m : m * weight(top_of_part(i), t.x, c);
-  };
   auto scan = [&](double y) {
-#pragma unroll
+#pragma unroll 1
     for (int i = 1; i < 64; i *= 2) {
       const double z = __shfl_up(y, i);
       y += lane >= i ? z : 0.0;
     }
     return y;
   };
-  auto total_of = [&](int which) {
-    double s = 0.0;
-    for (int i = lane; i < p.picks; i += 64) s += mass_of(i, which);
+  int at = part, which = 0;
+  double want = 0.0, before = 0.0;
+  Top t;
+  // First its own part; the last workgroup then goes over the part that holds the token.
+#pragma unroll 1
+  for (int pass = 0;; ++pass) {
+    float x[8];
+    const int v = at * kPick + tid * 8;
+    load(x, v);
+    if (pass == 0) {
+      t = Top{kNegInf, INT32_MAX};
 #pragma unroll
-    for (int i = 32; i >= 1; i /= 2) s += __shfl_xor(s, i);
-    return s;
-  };
-  double total = total_of(0);
-  int which = 0;
-  if (rows && !(total > 0.0)) {  // nothing was left by the last child that was tried: as it was before
-    which = 1;
-    total = total_of(1);
-  }
-  const double want = fmin(fmax((double)(WALK ? w.u[0] : p.u[node0]), 0.0), 1.0) * total;
-  int at = -1;
-  double before = 0.0, c0 = 0.0;
-  for (int i0 = 0; i0 < p.picks; i0 += 64) {
-    const double m = mass_of(i0 + lane, which), s = c0 + scan(m);
-    const unsigned long long over = __ballot(m > 0.0 && s > want), some = __ballot(m > 0.0);
-    if (over | some) {
-      const int l = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some);  // (without one: the last that has any weight)
-      at = i0 + l;
-      before = __shfl(s - m, l);
+      for (int i = 0; i < 8; ++i)
+        if (x[i] > t.x) t = Top{x[i], v + i};
+      t = top_of_threads(t, tops);
     }
-    if (over) break;
-    c0 = __shfl(s, 63);
-  }
-  if (at < 0) {
-    if (tid == 0) p.next[b] = -1;
-    return;
-  }
-  const int v = at * kPick + tid * 8;
-  double y[8];
-  load(x, v);
-  if (rows) {
-    double prev[8];
-    rest_of<F32>(y, prev, p, node0, w.target[e.last], w.drafts, x, v, w.tried, w.left, e.n_tried, c);
+    double y[8], prev[8], sum = 0.0, sum_prev = 0.0;
+    if (rows) {
+      rest_of<F32>(y, prev, p, node0, w.target[e.last], w.drafts, x, v, w.tried, w.left, e.n_tried, c);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = which ? prev[i] : y[i];
-  } else {
+      for (int i = 0; i < 8; ++i) {
+        sum_prev += prev[i];
+        y[i] = which ? prev[i] : y[i];
+      }
+    } else if (c > 0.0) {  // relative to the part's largest logit at first, so that the whole row's is not needed
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = weight(x[i], t.x, c);
-  }
-  double sum = 0.0;
+      for (int i = 0; i < 8; ++i) y[i] = weight(x[i], t.x, c);
+    }
+    if (c > 0.0) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) sum += y[i];
-  double end = scan(sum);
-  if (lane == 63) w.sums[wave] = end;
-  __syncthreads();
-  for (int i = 0; i < wave; ++i) end += w.sums[i];
-  // The first element whose sum exceeds; where rounding leaves none, the last one that has any weight.
-  double s = before + end - sum;
-  int last = -1, hit = -1;
+      for (int i = 0; i < 8; ++i) sum += y[i];
+    }
+    if (pass == 1) {
+      double end = scan(sum);
+      if (lane == 63) w.sums[wave] = end;
+      __syncthreads();
+      for (int i = 0; i < wave; ++i) end += w.sums[i];
+      // The first element whose sum exceeds; where rounding leaves none, the last one that has any weight.
+      double s = before + end - sum;
+      int last = -1, hit = -1;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    s += y[i];
-    if (y[i] > 0.0) last = v + i;
-    if (hit < 0 && y[i] > 0.0 && s > want) hit = v + i;
-  }
-  if (hit >= 0) atomicMin(&found, hit);
-  __syncthreads();
-  const bool none = found == INT32_MAX;
-  __syncthreads();
-  if (none) {
-    if (tid == 0) found = -1;
+      for (int i = 0; i < 8; ++i) {
+        s += y[i];
+        if (y[i] > 0.0) last = v + i;
+        if (hit < 0 && y[i] > 0.0 && s > want) hit = v + i;
+      }
+      if (hit >= 0) atomicMin(&found, hit);
+      __syncthreads();
+      const bool none = found == INT32_MAX;
+      __syncthreads();
+      if (none) {
+        if (tid == 0) found = -1;
+        __syncthreads();
+        if (last >= 0) atomicMax(&found, last);
+        __syncthreads();
+      }
+      if (tid == 0) p.next[b] = found;
+      return;
+    }
+    if (c > 0.0) sum = sum_threads(sum, w.sums);
+    if (rows) sum_prev = sum_threads(sum_prev, w.sums);
+    if (tid == 0) {
+      __hip_atomic_store(&parts[part].all, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(&parts[part].without, sum_prev, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(&parts[part].top, t.x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(&parts[part].first, t.first, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      // The four have arrived before the ticket is drawn.  (They go past the caches as they are: an ordering of the atomic's own
+      // would write back and empty the L2 of a whole part of the chip, for every workgroup.)
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      is_last = __hip_atomic_fetch_add(p.ticket + b, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == p.picks - 1;
+      found = INT32_MAX;
+    }
     __syncthreads();
-    if (last >= 0) atomicMax(&found, last);
-    __syncthreads();
+    if (!is_last) return;
+    // Parts as far as they fit into LDS are fetched once.
+    auto fetch = [&](int i) {
+      VerifyMass m;
+      m.all = __hip_atomic_load(&parts[i].all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      m.without = __hip_atomic_load(&parts[i].without, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      m.top = __hip_atomic_load(&parts[i].top, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      m.first = __hip_atomic_load(&parts[i].first, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      return m;
+    };
+    t = Top{kNegInf, INT32_MAX};
+    for (int i = tid; i < p.picks; i += kThreads) {
+      const VerifyMass m = fetch(i);
+      if (i < kHeldParts) held[i] = m;
+      t = higher(t, Top{m.top, m.first});
+    }
+    t = top_of_threads(t, tops);  // (its barriers also stand between the writes and the reads of `held`)
+    if (t.x == kNegInf || c == 0.0) {
+      if (tid == 0) p.next[b] = t.x == kNegInf ? -1 : t.first;
+      return;
+    }
+    // The part, by every wavefront for itself.
+    auto mass_of = [&](int i) {
+      if (i >= p.picks) return 0.0;
+      const VerifyMass m = i < kHeldParts ? held[i] : fetch(i);
+      const double y = which ? m.without : m.all;
+      return rows ? y : y * weight(m.top, t.x, c);
+    };
+    double total = 0.0;
+#pragma unroll 1
+    for (which = 0;; which = 1) {
+      for (int i = lane; i < p.picks; i += 64) total += mass_of(i);
+#pragma unroll
+      for (int i = 32; i >= 1; i /= 2) total += __shfl_xor(total, i);
+      if (total > 0.0 || !rows || which == 1) break;  // (nothing was left by the last child that was tried: as it was before)
+      total = 0.0;
+    }
+    want = fmin(fmax((double)(WALK ? w.u[0] : p.u[node0]), 0.0), 1.0) * total;
+    at = -1;
+    double c0 = 0.0;
+    for (int i0 = 0; i0 < p.picks; i0 += 64) {
+      const double m = mass_of(i0 + lane), s = c0 + scan(m);
+      const unsigned long long over = __ballot(m > 0.0 && s > want), some = __ballot(m > 0.0);
+      if (over | some) {
+        const int l = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some);  // (without one: the last that has any weight)
+        at = i0 + l;
+        before = __shfl(s - m, l);
+      }
+      if (over) break;
+      c0 = __shfl(s, 63);
+    }
+    if (at < 0) {
+      if (tid == 0) p.next[b] = -1;
+      return;
+    }
   }
-  if (tid == 0) p.next[b] = found;
 }
 
 template <bool F32>

@@ -289,3 +289,97 @@ def test_another_stream_while_the_current_one_is_busy():
     assert all(torch.equal(x, y) for x, y in zip(got, want)) and all(torch.equal(x, y) for x, y in zip((path, n_path, nxt), told))
     assert a.lengths().tolist() == [500 + int(n_path[0]), 300 + int(n_path[0])]
     torch.cuda.synchronize()
+
+
+def test_refusals():
+    a, K, V = make("bf16", 128, 2, 2, 1, 2, [10] * 4, room=20, track=True)
+    g = torch.Generator().manual_seed(1)
+    q, k, v = (nodes("packed", 2, 5, h, 128, torch.bfloat16, g) for h in (4, 2, 2))
+    lse = torch.full((4, 10), 9.0).cuda()
+    path, n = torch.zeros((1, 5), dtype=torch.int32).cuda(), torch.ones(1, dtype=torch.int32).cuda()
+    with pytest.raises(B.BaklavaError) as e:  # scores are tracked
+        a.append_accepted(0, 2, k, v, path, n, n)
+    assert e.value.status == B.EINVAL
+    good = dict(k=k, v=v, path=path, n_path=n, pos0=n, q=q, lse=lse)
+    for bad in (dict(path=path.long()), dict(path=path[0]), dict(path=path.cpu()), dict(n_path=torch.ones(2, dtype=torch.int32).cuda()), dict(pos0=n.float()),
+                dict(q=None), dict(lse=None), dict(k=k.float()), dict(v=v[:-1]), dict(q=q[:, :2]), dict(lse=lse.double()), dict(lse=lse[:, :9])):
+        with pytest.raises(ValueError):
+            a.append_accepted(0, 2, **(good | bad))
+    for first, count in ((0, 3), (-1, 1), (2, 1)):
+        with pytest.raises((B.BaklavaError, ValueError)):
+            a.append_accepted(first, count, **good)
+    a.sync_lengths()
+    assert a.lengths().tolist() == [10] * 4
+    a.set_option(B.OPT_TRACK_SCORES, 0)  # paused: they are not looked at
+    before = a.score.clone()
+    a.append_accepted(0, 2, k, v, path, n, n)
+    a.sync_lengths()
+    for c in range(4):
+        o = int(a.off_host[c])
+        assert torch.equal(a.score[o:o + 10], before[o:o + 10])
+    assert a.lengths().tolist() == [11] * 4
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "mxfp4"])
+def test_pending_calls_and_accepted_paths_add_up(dtype):
+    """Tracked steps that are still on record, a path behind them, steps behind that: the scores an eviction finds hold all of them."""
+    L, Hkv, G, D, N = 1, 2, 4, 128, 5
+    a, K, V = make(dtype, D, G, Hkv, 1, L, [200, 77], room=40, seed=1, track=True)
+    g = torch.Generator().manual_seed(4)
+    steps = [[nodes("packed", 1, 1, h, D, torch.bfloat16, g) for h in (G * Hkv, Hkv, Hkv)] for _ in range(7)]
+    q, k, v = (nodes("packed", 1, N, h, D, torch.bfloat16, g) for h in (G * Hkv, Hkv, Hkv))
+    out = torch.empty((1, G * Hkv, D), device="cuda")
+    for t, (qs, ks, vs) in enumerate(steps[:3]):
+        a.append_decode_attn(0, 1, ks, vs, t, qs, out)
+    parent = torch.from_numpy(parents("chain", 1, N)).cuda()
+    _, lse = a.tree_attn(0, 1, k, v, parent, q, want_lse=True)
+    path, n, pos = torch.arange(N, dtype=torch.int32).view(1, N).cuda(), torch.tensor([N], dtype=torch.int32).cuda(), torch.tensor([3], dtype=torch.int32).cuda()
+    a.append_accepted(0, 1, k, v, path, n, pos, q=q, lse=lse)
+    a.sync_lengths()
+    for t, (qs, ks, vs) in enumerate(steps[3:]):
+        a.append_decode_attn(0, 1, ks, vs, 3 + N + t, qs, out)
+    a.flush_scores(0, 1)
+    for c, n0 in enumerate((200, 77)):
+        o, total = int(a.off_host[c]), n0 + 7 + N
+        score = a.score[o:o + total].double().cpu()
+        # every query's weights add up to 1 a head: 2^-10 of it is far more than fp32 loses
+        assert abs(float(score.sum()) - G * (7 + N)) <= 2.0 ** -10 * G * (7 + N)
+        rows = [stored(ks, dtype)[0, c] for _, ks, _ in steps[:3]] + [stored(k, dtype)[i, c] for i in range(N)] + [stored(ks, dtype)[0, c] for _, ks, _ in steps[3:]]
+        all_k = np.concatenate([K[o:o + n0], np.stack(rows)])
+        qd = [s[0][0, c * G:(c + 1) * G] for s in steps[:3]] + [q[i, c * G:(c + 1) * G] for i in range(N)] + [s[0][0, c * G:(c + 1) * G] for s in steps[3:]]
+        want = np.zeros(total)
+        for t, x in enumerate(qd):
+            for y in x.double().cpu().numpy():
+                s = all_k[:n0 + t + 1] @ y / np.sqrt(D)
+                e = np.exp(s - s.max())
+                want[:n0 + t + 1] += e / e.sum()
+        assert np.abs(score.numpy() - want).max() <= 2e-3 * max(1.0, want.max())
+
+
+def test_many_caches_and_a_long_one():
+    """720 caches of which some take no path, and one of 40000 rows, in one call."""
+    L, batch, Hkv, G, D, N = 5, 9, 16, 2, 64, 6
+    rng = np.random.default_rng(1)
+    lens = rng.integers(0, 90, (L, batch, Hkv))
+    lens[2, 4, 3] = 40000
+    a, K, V = make("bf16", D, G, Hkv, batch, L, lens.reshape(-1).tolist(), room=N, seed=2, track=True)
+    g = torch.Generator().manual_seed(3)
+    q, k, v = (nodes("packed", L * batch, N, h, D, torch.bfloat16, g) for h in (G * Hkv, Hkv, Hkv))
+    parent = torch.from_numpy(parents("chain", batch, N)).cuda()
+    _, lse = a.tree_attn(0, L, k, v, parent, q, want_lse=True)
+    n_path = rng.integers(0, N + 1, batch)
+    n_path[4] = 5
+    path = np.full((batch, N), -1, dtype=np.int32)
+    for b in range(batch):
+        path[b, :n_path[b]] = np.arange(n_path[b])
+    n = torch.from_numpy(n_path).int().cuda()
+    a.append_accepted(0, L, k, v, torch.from_numpy(path).cuda(), n, n, q=q, lse=lse)
+    a.sync_lengths()
+    assert a.lengths().tolist() == (lens + n_path.reshape(1, -1, 1)).reshape(-1).tolist()
+    score, kd, qd, ln = a.score.double().cpu().numpy(), stored(k, "bf16"), q.double().cpu().numpy(), lse.double().cpu().numpy()
+    flat = lens.reshape(-1)
+    for c in sorted({(2 * batch + 4) * Hkv + 3} | set(rng.choice(a.n_caches, 60, replace=False).tolist())):
+        P, o = int(n_path[c // Hkv % batch]), int(a.off_host[c])
+        add, e = expected_scores(K, flat, kd, qd, ln, path, n_path, c, Hkv, batch, N, G, D, o)
+        got = score[o:o + flat[c] + P]
+        assert (np.abs(got - add[:len(got)]) <= e * add[:len(got)] + add[:len(got)] * 2.0 ** -23).all(), c

@@ -268,3 +268,88 @@ def test_offsets_beyond_32_bits():
         assert (out[3 + i].double() - want).abs().max() <= 2.0 ** -7 * want + 1e-30
         wl = np.log2(n + i + 1) + 128 * 0.125 / np.sqrt(128) * np.log2(np.e)
         assert (lse[:, 3 + i].double() - wl).abs().max() <= 1e-4  # (sums of 2^24 terms: within 2^-14)
+
+
+@pytest.mark.parametrize("dtype,G,N", [("bf16", 7, 50), ("bf16", 16, 40), ("f32", 8, 30), ("mxfp4", 4, 31), ("mxfp4", 8, 100)])
+def test_many_query_rows_behind_long_caches(dtype, G, N):
+    """Several workgroups for the query rows of a work item, several work items for a cache, trees of different sizes."""
+    lens = [9000, 40, 3000, 129]
+    a, K, V = make(dtype, 128, G, 2, 2, 1, lens, seed=N)
+    g = torch.Generator().manual_seed(N)
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    q, k, v = (nodes("packed", 2, N, h, 128, dt, g) for h in (2 * G, 2, 2))
+    parent, count = parents("tree", 2, N, 7), (N, N // 3)
+    out, lse = torch.zeros_like(q), torch.zeros((2 * G, 2 * N), device="cuda")
+    a.tree_attn(0, 1, k, v, torch.from_numpy(parent).cuda(), q, n_nodes=torch.tensor(count, dtype=torch.int32).cuda(), out=out, lse=lse)
+    check(a, K, V, k, v, q, parent, count, out, lse, (0, 1), dtype)
+
+
+@pytest.mark.parametrize("dtype,N", [("bf16", 3), ("bf16", 40), ("f32", 2), ("mxfp4", 5)])
+@pytest.mark.parametrize("L,batch,Hkv", [(3, 8, 4), (5, 9, 16)])
+def test_more_caches_than_a_workgroup_has_threads(dtype, N, L, batch, Hkv):
+    """96 caches, and 720, some of them long, some empty, sequences without nodes among them."""
+    rng = np.random.default_rng(L)
+    lens = rng.integers(0, 150, (L, batch, Hkv))
+    lens[1, 2, :] = 0
+    lens[0, 1, 1], lens[L - 1, batch - 1, Hkv - 1] = 5000, 2500
+    a, K, V = make(dtype, 64, 2, Hkv, batch, L, lens.reshape(-1).tolist(), seed=9)
+    g = torch.Generator().manual_seed(L)
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    q, k, v = (nodes("packed", L * batch, N, h, 64, dt, g) for h in (2 * Hkv, Hkv, Hkv))
+    parent = parents("tree", batch, N, 2)
+    count = rng.integers(0, N + 1, batch)
+    count[2], count[3] = N, 0
+    out, lse = torch.zeros_like(q), torch.zeros((2 * Hkv, L * batch * N), device="cuda")
+    a.tree_attn(0, L, k, v, torch.from_numpy(parent).cuda(), q, n_nodes=torch.from_numpy(count).int().cuda(), out=out, lse=lse)
+    some = sorted({1 * Hkv + 1, a.n_caches - 1} | set(rng.choice(a.n_caches, 40, replace=False).tolist()))
+    check(a, K, V, k, v, q, parent, count, out, lse, (0, L), dtype, only=some)
+
+
+def test_refusals():
+    a, K, V = make("bf16", 128, 2, 2, 2, 2, [10] * 8, track=True)
+    g = torch.Generator().manual_seed(1)
+    N = 4
+    q, k, v = (nodes("packed", 4, N, h, 128, torch.bfloat16, g) for h in (4, 2, 2))
+    p = torch.from_numpy(parents("chain", 2, N)).cuda()
+    n = torch.tensor([1, 2], dtype=torch.int32).cuda()
+    a.tree_attn(0, 2, k, v, p, q)
+    for bad in (dict(parent=p.long()), dict(parent=p[:1]), dict(parent=p.cpu()), dict(parent=p[:, ::2]), dict(n_nodes=n[:1]), dict(n_nodes=n.float()),
+                dict(n_nodes=n.cpu()), dict(q=q.float()), dict(q=q[:-1]), dict(k=k[:, :1]), dict(v=v[..., :64]), dict(q=q.cpu()), dict(out=q.float()),
+                dict(lse=torch.zeros((4, 4 * N), device="cuda").half()), dict(lse=torch.zeros((3, 4 * N), device="cuda")), dict(q=q.clone().requires_grad_())):
+        with pytest.raises(ValueError):
+            a.tree_attn(0, 2, **(dict(k=k, v=v, parent=p, q=q) | bad))
+    for first, count in ((0, 3), (-1, 1), (2, 1), (1, 0)):
+        with pytest.raises((B.BaklavaError, ValueError)):
+            a.tree_attn(first, count, k, v, p, q)
+    big = torch.zeros((2, 257), dtype=torch.int32).cuda()
+    wide = [torch.zeros((4 * 257, h, 128), dtype=torch.bfloat16, device="cuda") for h in (2, 2, 4)]
+    with pytest.raises(B.BaklavaError) as e:
+        a.tree_attn(0, 2, wide[0], wide[1], big, wide[2])
+    assert e.value.status == B.EINVAL
+    # misaligned rows, outputs that overlap, a workspace that is too small
+    odd = torch.zeros(4 * N * 4 * 128 + 8, dtype=torch.bfloat16, device="cuda")[4:4 + 4 * N * 4 * 128].view(4 * N, 4, 128)
+    for bad in (dict(q=odd), dict(out=odd), dict(out=q[:1].expand(4 * N, 4, 128))):
+        with pytest.raises(B.BaklavaError) as e:
+            a.tree_attn(0, 2, **(dict(k=k, v=v, parent=p, q=q) | bad))
+        assert e.value.status == B.EINVAL
+    lib, rows = B.lib(), B._Rows(torch)
+    at = [rows.add(t, "t", 4, 4 * N, N, t.shape[1], 128, torch.bfloat16) for t in (q, k, v)]
+    need = lib.baklava_tree_workspace_bytes(a.ctx, 2, N)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    call = lambda nbytes, at_ws: lib.baklava_tree_attn(a.ctx, 0, 2, at[1], at[2], N, p.data_ptr(), None, at[0], at[0], None, at_ws, nbytes, None)
+    assert call(need - 1, ws.data_ptr()) == B.ECAPACITY and call(need, ws.data_ptr() + 64) == B.EINVAL and call(need, None) == B.EINVAL
+    assert lib.baklava_tree_workspace_bytes(a.ctx, 3, N) == lib.baklava_tree_workspace_bytes(a.ctx, 0, N) == lib.baklava_tree_workspace_bytes(a.ctx, 1, 257) == 0
+
+
+def test_two_calls_at_once():
+    """Calls on two streams over the same caches, each with outputs and a workspace of its own."""
+    a, K, V = make("bf16", 128, 4, 2, 2, 1, [4000, 300, 2000, 9000])
+    g = torch.Generator().manual_seed(5)
+    sets = [[nodes("packed", 2, N, h, 128, torch.bfloat16, g) for h in (8, 2, 2)] + [torch.from_numpy(parents("tree", 2, N)).cuda()] for N in (5, 40)]
+    want = [a.tree_attn(0, 1, k, v, p, q, want_lse=True) for q, k, v, p in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(5):
+        got = [a.tree_attn(0, 1, k, v, p, q, want_lse=True, stream=s) for (q, k, v, p), s in zip(sets, streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for gs, ws in zip(got, want) for x, y in zip(gs, ws))

@@ -175,3 +175,57 @@ def test_drawn_tokens_follow_the_target():
     behind_root = np.where(count.numpy() > 1, token[:, 1], nxt.numpy())
     got = np.bincount(behind_root, minlength=V)
     assert (np.abs(got - n * p) <= 4 * np.sqrt(n * p * (1 - p))).all(), (got, n * p)
+
+
+def test_vocabularies_of_more_parts_than_are_held():
+    V = 3 * (1 << 18) + 5
+    for drafts in (False, True):
+        t = inputs(2, 3, V, "chain", "bf16", False, 3)
+        if drafts:
+            t["draft_logits"] = (t["logits"].float().roll(1, 1) + 0.5 * torch.randn(t["logits"].shape, generator=torch.Generator().manual_seed(1))).bfloat16()
+        for u0 in (0.0, 0.37, 1 - 2.0 ** -24):
+            t["u"][:, 0] = u0
+            same(run(t), expect(t))
+
+
+def test_two_calls_at_once_and_other_streams():
+    sets = [inputs(4, 12, 5000, "tree", "f32", False, 1), inputs(6, 5, 20000, "chain", "bf16", True, 2)]
+    sets = [{n: x.cuda() if isinstance(x, torch.Tensor) else x for n, x in t.items()} for t in sets]
+    want = [B.verify_draft(**t) for t in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda._sleep(5_000_000)
+    for _ in range(5):
+        got = [B.verify_draft(**t, stream=s) for t, s in zip(sets, streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for gs, ws in zip(got, want) for x, y in zip(gs, ws))
+
+
+def test_captured_and_replayed():
+    for drafts in (False, True):
+        t = {n: x.cuda() if isinstance(x, torch.Tensor) else x for n, x in inputs(3, 9, 4000, "tree", "bf16", drafts, 7).items()}
+        B.verify_draft(**t)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            res = B.verify_draft(**t)
+        for seed in range(4):
+            new = inputs(3, 9, 4000, "tree", "bf16", drafts, 20 + seed)
+            for n, x in new.items():
+                if isinstance(x, torch.Tensor):
+                    t[n].copy_(x)
+            graph.replay()
+            torch.cuda.synchronize()
+            same([x.cpu() for x in res], expect(new))
+            torch.randn((500, 500), device="cuda").sum().item()
+
+
+def test_refusals_on_the_gpu():
+    t = {n: x.cuda() if isinstance(x, torch.Tensor) else x for n, x in inputs(2, 3, 50, "chain", "f32", False, 1).items()}
+    f = torch.zeros((2, 3, 50), device="cuda")
+    for bad in (dict(logits=f.double()), dict(logits=f[:, :2]), dict(logits=f.cpu()), dict(logits=f.transpose(0, 1).contiguous().transpose(0, 1)),
+                dict(logits=torch.zeros((2, 3, 100), device="cuda")[..., ::2]), dict(draft_logits=f.bfloat16()), dict(draft_logits=f[..., :49]),
+                dict(temperature=torch.ones(3, device="cuda")), dict(temperature=torch.ones(2, device="cuda").double()), dict(n_nodes=torch.ones(2, device="cuda")),
+                dict(u=t["u"].cpu()), dict(u=t["u"].double())):
+        with pytest.raises(ValueError):
+            B.verify_draft(**(t | bad))
