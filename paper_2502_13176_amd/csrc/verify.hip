@@ -95,11 +95,48 @@ __device__ __forceinline__ double exponent_scale(const VerifyParams& p, int b) {
   return t > 0.f ? 1.4426950408889634 / (double)t : 0.0;
 }
 
-// Sums over the workgroup, in an order that does not change.  (Loops that a workgroup runs through once stay loops here and below: its
-// instructions come from memory, and take longer than the work.)
+// x of the lane ROR further on in its row of 16.
+template <int ROR>
+__device__ __forceinline__ int row_turn(int x) { return __builtin_amdgcn_update_dpp(0, x, 0x120 + ROR, 0xf, 0xf, true); }
+template <int ROR>
+__device__ __forceinline__ float row_turn(float x) { return __int_as_float(row_turn<ROR>(__float_as_int(x))); }
+template <int ROR>
+__device__ __forceinline__ double row_turn(double x) {
+  return __hiloint2double(row_turn<ROR>(__double2hiint(x)), row_turn<ROR>(__double2loint(x)));
+}
+__device__ __forceinline__ double of_lane(double x, int lane) {
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(x), lane), __builtin_amdgcn_readlane(__double2loint(x), lane));
+}
+// Sum over a row of 16 lanes, in each of them.  (Lanes l and l + 8 first: whichever a lane starts from, the same pairs are added.)
+__device__ __forceinline__ double sum_row(double x) {
+  x += row_turn<8>(x);
+  x += row_turn<4>(x);
+  x += row_turn<2>(x);
+  x += row_turn<1>(x);
+  return x;
+}
+__device__ __forceinline__ double sum_wave(double x) {
+  x = sum_row(x);
+  return of_lane(x, 0) + of_lane(x, 16) + of_lane(x, 32) + of_lane(x, 48);
+}
+// Sum over the wavefront's lanes up to and with the calling one.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double shifted(double x) {  // 0 where there is no lane to come from
+  return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(x), CTRL, ROWS, 0xf, false),
+                          __builtin_amdgcn_update_dpp(0, __double2loint(x), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ double scan_wave(double x) {
+  x += shifted<0x111, 0xf>(x);  // row_shr:1
+  x += shifted<0x112, 0xf>(x);
+  x += shifted<0x114, 0xf>(x);
+  x += shifted<0x118, 0xf>(x);
+  x += shifted<0x142, 0xa>(x);  // row_bcast:15 into rows 1 and 3
+  x += shifted<0x143, 0xc>(x);  // row_bcast:31 into rows 2 and 3
+  return x;
+}
+// Sums over the workgroup, in an order that does not change.
 __device__ __forceinline__ double sum_threads(double x, double* lds) {
-#pragma unroll 1
-  for (int i = 32; i >= 1; i /= 2) x += __shfl_xor(x, i);
+  x = sum_wave(x);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
   __syncthreads();
@@ -114,9 +151,20 @@ struct Top {
   int first;
 };
 __device__ __forceinline__ Top higher(Top a, Top b) { return b.x > a.x || (b.x == a.x && b.first < a.first) ? b : a; }
+template <int ROR>
+__device__ __forceinline__ Top row_turn(Top t) { return Top{row_turn<ROR>(t.x), row_turn<ROR>(t.first)}; }
+__device__ __forceinline__ Top top_row(Top t) {
+  t = higher(t, row_turn<8>(t));
+  t = higher(t, row_turn<4>(t));
+  t = higher(t, row_turn<2>(t));
+  return higher(t, row_turn<1>(t));
+}
+__device__ __forceinline__ Top of_lane(Top t, int lane) {
+  return Top{__int_as_float(__builtin_amdgcn_readlane(__float_as_int(t.x), lane)), __builtin_amdgcn_readlane(t.first, lane)};
+}
 __device__ __forceinline__ Top top_of_threads(Top t, Top* lds) {
-#pragma unroll 1
-  for (int i = 32; i >= 1; i /= 2) t = higher(t, Top{__shfl_xor(t.x, i), __shfl_xor(t.first, i)});
+  t = top_row(t);
+  t = higher(higher(of_lane(t, 0), of_lane(t, 16)), higher(of_lane(t, 32), of_lane(t, 48)));
   __syncthreads();
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = t;
   __syncthreads();
@@ -195,13 +243,11 @@ __device__ __forceinline__ VerifyStat merged(const VerifyStat* s, int parts, dou
   const int l = threadIdx.x & 15;
   Top t{kNegInf, INT32_MAX};
   for (int i = l; i < parts; i += 16) t = higher(t, Top{s[i].top, s[i].first});
-#pragma unroll
-  for (int i = 8; i >= 1; i /= 2) t = higher(t, Top{__shfl_xor(t.x, i), __shfl_xor(t.first, i)});
+  t = top_row(t);
   double sum = 0.0;
   if (c > 0.0) {
     for (int i = l; i < parts; i += 16) sum += s[i].sum * weight(s[i].top, t.x, c);
-#pragma unroll
-    for (int i = 8; i >= 1; i /= 2) sum += __shfl_xor(sum, i);
+    sum = sum_row(sum);
   }
   return VerifyStat{sum, t.x, t.first};
 }
@@ -247,7 +293,8 @@ __device__ __forceinline__ double rest_of_one(const VerifyParams& p, int64_t nod
 
 // What the walk of a sequence leaves.
 struct Walk {
-  int32_t parent[kMostNodes], token[kMostNodes], tried[kMostNodes];  // tried: children of the last node that have had an effect
+  // tried: children of the last node that have had an effect (walk_points: their tokens)
+  int32_t parent[kMostNodes], token[kMostNodes], tried[kMostNodes];
   double prob[kMostNodes], from[kMostNodes];  // of node i's token: under its parent's row, under its own draft row
   double left[kMostNodes];                    // what is left by tried[k], before it is divided
   VerifyStat target[kMostNodes], drafts[kMostNodes];
@@ -321,21 +368,33 @@ __device__ __forceinline__ VerifyEnd walk_points(const VerifyParams& p, int b, i
   const int tid = threadIdx.x, lane = tid & 63;
   const int64_t node0 = (int64_t)b * p.N;
   const int up = load_nodes<F32>(p, b, n, c, false, w);
-  const int mine = w.token[tid];
+  const int mine = w.token[tid], wave = tid >> 6;
   const double pr = w.prob[tid];
-  bool again = false;                         // a sibling before has taken this token off already
-#pragma unroll 1
-  for (int j = up + 1; j < tid && up >= 0; ++j) again = again || (w.parent[j] == up && w.token[j] == mine);
-  w.from[tid] = again ? 0.0 : pr;
   if (tid < 4) w.stands[tid] = 0;
   if (tid == 0) w.n_tried = 0;
-  __syncthreads();
-  // (a token without weight takes nothing off, and one that has all that is left leaves it as it is)
-  double off = 0.0;
+  bool again = false;                         // a sibling before has taken this token off already
+  double off = 0.0;                           // what siblings before have taken off
+  // Node j against all behind it.  (A token without weight takes nothing off, and one that has all that is left leaves it as it is.)
+  auto against = [&](int j, int its_up, int its_token, double its_weight) {
+    if (its_up < 0 || its_up != up || j >= tid) return;
+    again = again || its_token == mine;
+    if (its_weight > 0.0 && 1.0 - off - its_weight > 0.0) off += its_weight;
+  };
 #pragma unroll 1
-  for (int j = up + 1; j < tid && up >= 0; ++j) {
-    const double q = w.parent[j] == up ? w.from[j] : 0.0;
-    if (q > 0.0 && 1.0 - off - q > 0.0) off += q;
+  for (int g = 0; g * 64 < n; ++g) {
+    if (wave == g) {                          // inside a wavefront: node j's is known when its turn comes
+#pragma unroll 1
+      for (int j = 0; j < min(64, n - g * 64); ++j) {
+        const double x = again ? 0.0 : pr;
+        against(g * 64 + j, __builtin_amdgcn_readlane(up, j), __builtin_amdgcn_readlane(mine, j),
+                __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(x), j), __builtin_amdgcn_readlane(__double2loint(x), j)));
+      }
+      w.from[tid] = again ? 0.0 : pr;
+    }
+    __syncthreads();
+    if (wave > g && wave * 64 < n)
+#pragma unroll 1
+      for (int j = g * 64; j < g * 64 + 64; ++j) against(j, w.parent[j], w.token[j], w.from[j]);
   }
   const bool stands = up >= 0 && mine >= 0 && (double)w.u[tid] < (again ? 0.0 : pr / (1.0 - off));
   const unsigned long long these = __ballot(stands);
@@ -354,7 +413,7 @@ __device__ __forceinline__ VerifyEnd walk_points(const VerifyParams& p, int b, i
     if (write && tid == 0) p.path[node0 + n_path] = cur;
     n_path += 1;
   }
-  if (up == cur && !again && pr > 0.0 && 1.0 - off - pr > 0.0) w.tried[atomicAdd(&w.n_tried, 1)] = tid;
+  if (up == cur && !again && pr > 0.0 && 1.0 - off - pr > 0.0) w.tried[atomicAdd(&w.n_tried, 1)] = mine;  // (its token)
   __syncthreads();
   if (write) write_path(p, node0, b, n_path);
   return VerifyEnd{cur, w.n_tried};
@@ -513,21 +572,13 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyParams p) {
     load8<F32>(x, row, v, p.V);
     if (WALK && c > 0.0)
       for (int j = 0; j < e.n_tried; ++j) {
-        const int at = w.token[w.tried[j]] - v;
+        const int at = w.tried[j] - v;
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = at == i ? kNegInf : x[i];
       }
   };
   // What other workgroups read is written and read past the caches that the chip's parts do not share.
   VerifyMass* const parts = p.mass + (int64_t)b * p.picks;
-  auto scan = [&](double y) {
-#pragma unroll 1
-    for (int i = 1; i < 64; i *= 2) {
-      const double z = __shfl_up(y, i);
-      y += lane >= i ? z : 0.0;
-    }
-    return y;
-  };
   int at = part, which = 0;
   double want = 0.0, before = 0.0;
   Top t;
@@ -561,7 +612,7 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyParams p) {
       for (int i = 0; i < 8; ++i) sum += y[i];
     }
     if (pass == 1) {
-      double end = scan(sum);
+      double end = scan_wave(sum);
       if (lane == 63) w.sums[wave] = end;
       __syncthreads();
       for (int i = 0; i < wave; ++i) end += w.sums[i];
@@ -633,8 +684,7 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyParams p) {
 #pragma unroll 1
     for (which = 0;; which = 1) {
       for (int i = lane; i < p.picks; i += 64) total += mass_of(i);
-#pragma unroll
-      for (int i = 32; i >= 1; i /= 2) total += __shfl_xor(total, i);
+      total = sum_wave(total);
       if (total > 0.0 || !rows || which == 1) break;  // (nothing was left by the last child that was tried: as it was before)
       total = 0.0;
     }
@@ -642,15 +692,15 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyParams p) {
     at = -1;
     double c0 = 0.0;
     for (int i0 = 0; i0 < p.picks; i0 += 64) {
-      const double m = mass_of(i0 + lane), s = c0 + scan(m);
+      const double m = mass_of(i0 + lane), s = c0 + scan_wave(m);
       const unsigned long long over = __ballot(m > 0.0 && s > want), some = __ballot(m > 0.0);
       if (over | some) {
         const int l = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some);  // (without one: the last that has any weight)
         at = i0 + l;
-        before = __shfl(s - m, l);
+        before = of_lane(s - m, l);
       }
       if (over) break;
-      c0 = __shfl(s, 63);
+      c0 = of_lane(s, 63);
     }
     if (at < 0) {
       if (tid == 0) p.next[b] = -1;
