@@ -367,13 +367,6 @@ class Arena:
         _hold_until_stream_passes((k, v), stream)
         return k, v
 
-    def _nodes(self, rows, parent, n_nodes) -> int:
-        """Nodes of a tree, from its tensor of parents."""
-        _expect_ints(rows, parent, "parent", (self.batch, None))
-        if n_nodes is not None:
-            _expect_ints(rows, n_nodes, "n_nodes", (self.batch,))
-        return parent.shape[1]
-
     def tree_attn(self, layer_begin: int, layer_count: int, k, v, parent, q, n_nodes=None, out=None, lse=None,
                   want_lse: bool = False, stream=None):
         """baklava_tree_attn: parent int32 [batch, N], n_nodes int32 [batch] or None (N); q [tokens, Hq, D], k and v [tokens,
@@ -386,20 +379,22 @@ class Arena:
         rows = _Rows(torch)
         if rows.device != self.gpu:
             raise ValueError("the arena's GPU must be the current one")
-        N = self._nodes(rows, parent, n_nodes)
-        n_seq = layer_count * self.batch
+        N, n_seq = _per_node(parent, "parent"), layer_count * self.batch
+        _expect(rows, parent, torch.int32, "parent", (self.batch, N))
+        if n_nodes is not None:
+            _expect(rows, n_nodes, torch.int32, "n_nodes", (self.batch,))
         dt = torch.float32 if self.dtype not in ("bf16", "mxfp4") else torch.bfloat16
         k_at = rows.add(k, "k", n_seq, n_seq * N, N, self.Hkv, self.D, dt)
         v_at = rows.add(v, "v", n_seq, n_seq * N, N, self.Hkv, self.D, dt)
         q_at = rows.add(q, "q", n_seq, n_seq * N, N, self.Hq, self.D, dt)
-        nbytes = lib().baklava_tree_workspace_bytes(self.ctx, int(layer_count), N)
         if out is None:
-            out = _empty_on(stream, q.new_empty, q.shape)
+            out = q.new_empty(q.shape) if stream is None else _empty_on(stream, q.new_empty, q.shape)
         if lse is None and want_lse:
             lse = _empty_on(stream, q.new_empty, (self.Hq, q.shape[0]) if q.dim() == 3 else q.shape[:3], dtype=torch.float32)
         out_at = rows.add(out, "out", n_seq, n_seq * N, N, self.Hq, self.D, dt)
         lse_at = rows.add_values(lse, "lse", n_seq, n_seq * N, N, self.Hq) if lse is not None else None
-        ws = _empty_on(stream, torch.empty, (max(nbytes, 256),), dtype=torch.uint8, device=q.device)
+        nbytes = lib().baklava_tree_workspace_bytes(self.ctx, int(layer_count), N)
+        ws = _empty_on(stream, parent.new_empty, max(nbytes, 256), dtype=torch.uint8)
         _check(lib().baklava_tree_attn(self.ctx, int(layer_begin), int(layer_count), k_at, v_at, N, parent.data_ptr(),
                                        n_nodes.data_ptr() if n_nodes is not None else None, q_at, out_at, lse_at, ws.data_ptr(),
                                        nbytes, _stream_ptr(stream)), "baklava_tree_attn")
@@ -414,12 +409,12 @@ class Arena:
         rows = _Rows(torch)
         if rows.device != self.gpu:
             raise ValueError("the arena's GPU must be the current one")
-        _expect_ints(rows, path, "path", (self.batch, None))
-        _expect_ints(rows, n_path, "n_path", (self.batch,))
-        _expect_ints(rows, pos0, "pos0", (self.batch,))
+        N, n_seq = _per_node(path, "path"), layer_count * self.batch
+        _expect(rows, path, torch.int32, "path", (self.batch, N))
+        _expect(rows, n_path, torch.int32, "n_path", (self.batch,))
+        _expect(rows, pos0, torch.int32, "pos0", (self.batch,))
         if (q is None) != (lse is None):
             raise ValueError("q and lse go together")
-        N, n_seq = path.shape[1], layer_count * self.batch
         dt = torch.float32 if self.dtype not in ("bf16", "mxfp4") else torch.bfloat16
         k_at = rows.add(k, "k", n_seq, n_seq * N, N, self.Hkv, self.D, dt)
         v_at = rows.add(v, "v", n_seq, n_seq * N, N, self.Hkv, self.D, dt)
@@ -678,13 +673,19 @@ class _Rows:
         return self._put(t, seq, tok, head)
 
 
-def _expect_ints(rows: _Rows, t, name: str, shape) -> None:
-    """int32 [shape] (None: any size of at least one) on the current GPU, contiguous."""
-    import torch
-    if t.dtype is not torch.int32 or not t.is_contiguous() or t.dim() != len(shape) or any(
-            n < 1 if want is None else n != want for n, want in zip(t.shape, shape)):
-        raise ValueError(f"{name} must be a contiguous int32 tensor [{', '.join('N' if x is None else str(x) for x in shape)}]")
-    rows.on_device(t, name)
+def _expect(rows: _Rows, t, dtype, name: str, shape) -> None:
+    """A contiguous tensor of that type and shape on the current GPU."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)}")
+    if not t.is_cuda or t.get_device() != rows.device:
+        raise ValueError(f"{name} must be on the current GPU")
+
+
+def _per_node(t, name: str) -> int:
+    """Nodes of a tree, from a tensor [sequences, nodes]."""
+    if t.dim() != 2 or t.shape[1] < 1:
+        raise ValueError(f"{name} must be [sequences, nodes], of at least one node")
+    return t.shape[1]
 
 
 def verify_draft(logits, token, parent, u, draft_logits=None, temperature=None, n_nodes=None, stream=None):
@@ -693,16 +694,16 @@ def verify_draft(logits, token, parent, u, draft_logits=None, temperature=None, 
     [batch] or None (N).  Returns (path [batch, N], n_path [batch], next_token [batch]), int32."""
     import torch
     rows = _Rows(torch)
-    _expect_ints(rows, parent, "parent", (None, None))
-    batch, N = parent.shape
-    _expect_ints(rows, token, "token", (batch, N))
+    N, batch = _per_node(parent, "parent"), parent.shape[0]
+    if batch < 1:
+        raise ValueError("at least one sequence expected")
+    _expect(rows, parent, torch.int32, "parent", (batch, N))
+    _expect(rows, token, torch.int32, "token", (batch, N))
+    _expect(rows, u, torch.float32, "u", (batch, N))
     if n_nodes is not None:
-        _expect_ints(rows, n_nodes, "n_nodes", (batch,))
-    for t, name, shape in ((u, "u", (batch, N)), (temperature, "temperature", (batch,))):
-        if t is not None:
-            if t.dtype is not torch.float32 or not t.is_contiguous() or t.shape != shape:
-                raise ValueError(f"{name} must be a contiguous fp32 tensor {list(shape)}")
-            rows.on_device(t, name)
+        _expect(rows, n_nodes, torch.int32, "n_nodes", (batch,))
+    if temperature is not None:
+        _expect(rows, temperature, torch.float32, "temperature", (batch,))
     dt, V = logits.dtype, logits.shape[-1]
     if dt is not torch.bfloat16 and dt is not torch.float32:
         raise ValueError("bf16 or fp32 logits expected")
@@ -719,9 +720,11 @@ def verify_draft(logits, token, parent, u, draft_logits=None, temperature=None, 
         rows.on_device(t, name)
         at.append((t.data_ptr(), t.stride(0) if len(shape) == 2 or N == 1 else t.stride(1)))
     nbytes = lib().baklava_verify_workspace_bytes(batch, N, V, int(draft_logits is not None))
-    path = _empty_on(stream, parent.new_empty, (batch, N))
-    n_path, token_out = (_empty_on(stream, parent.new_empty, (batch,)) for _ in range(2))
-    ws = _empty_on(stream, torch.empty, (max(nbytes, 256),), dtype=torch.uint8, device=logits.device)
+    if stream is None:
+        path, n_path, token_out = parent.new_empty((batch, N)), parent.new_empty(batch), parent.new_empty(batch)
+    else:
+        path, n_path, token_out = (_empty_on(stream, parent.new_empty, n) for n in ((batch, N), batch, batch))
+    ws = _empty_on(stream, parent.new_empty, max(nbytes, 256), dtype=torch.uint8)
     _check(lib().baklava_verify_draft(at[0][0], at[0][1], at[1][0], at[1][1], BF16 if dt is torch.bfloat16 else F32, batch, N, V,
                                       token.data_ptr(), parent.data_ptr(), n_nodes.data_ptr() if n_nodes is not None else None,
                                       temperature.data_ptr() if temperature is not None else None, u.data_ptr(), path.data_ptr(),

@@ -15,6 +15,13 @@
 // One pass over the keys with the running maximum and sum of every row in fp32.  The keys of all caches of a launch are cut into
 // work items of equal length, as the lengths on the device are (so a replayed launch is balanced too); each workgroup finds its
 // item by a scan over the lengths.  Caches of several items are merged by a kernel of their own.
+//
+// A workgroup of four wavefronts, two of them to a compute unit, owns 128 query rows (64 where pairs share their rows) and shares
+// tiles of 64 keys in LDS.  16 caches of 39321 bf16 rows, 448 query rows: 188 us of which 110 are the products at the rate of a library
+// product (1306 TFLOP/s); the matrix cores are busy 41% of the cycles, at 1.8 GHz: start and end take some 15 us, one wavefront in eight
+// has no rows of the last workgroup, and a step of 2.2 us ends with a wait for the tiles asked for at its start.  64 caches of 8200 rows,
+// 64 query rows on average: 53 us (271 MB, 39 at 7 TB/s), and 12 for the merge of their partials.  128 caches of 9830 4-bit rows, 52
+// query rows: 66 us (155 MB, 22): conversions, exponentials and LDS, none of them saturated.
 #include "common.h"
 #include "mxfp4.h"
 #include "tree.h"
@@ -603,9 +610,14 @@ hipError_t launch(const TreeParams& p, int ks, unsigned grid, hipStream_t s) {
 
 }  // namespace
 
+// The streaming kernel takes up to 64 query rows, up to 32 where two blocks of them cost it too many registers.  us a call, it / this
+// one with pairs of wavefronts, 64 caches of 10240 rows: bf16, D = 128, 64 rows 61.8 / 65.9, D = 64 36.4 / 40.7, 1 row 59.0 / 69.2; 4-bit
+// rows, 32 rows 29.7 / 41.9, D = 64 22.0 / 34.3, 52 rows (128 caches of 9830) 130 / 73; fp32, 32 caches of 4096 rows, D = 64, 64 rows
+// 43.0 / 42.1, D = 128 78.4 / 65.5, 32 rows 47.2 / 59.9.  Here up to 64 rows are taken by pairs of wavefronts, each with half of a
+// tile's keys: the 52 rows of 4 bits 73, without pairs 92.
 TreeLaunch tree_launch(int type, int D, int rows, int n_cus) {
   TreeLaunch t;
-  if (rows <= (type == 2 ? kStreamRows / 2 : kStreamRows)) {  // (4-bit rows: two blocks take more registers than there are)
+  if (rows <= (type == 2 || (type == 1 && D == 128) ? kStreamRows / 2 : kStreamRows)) {
     t.ks = 0;
     t.row_tiles = 1;
     t.target = n_cus < kMostTreeItems ? n_cus : kMostTreeItems;

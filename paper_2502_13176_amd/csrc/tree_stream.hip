@@ -1,5 +1,5 @@
-// Attention of a tree of drafted tokens over ragged caches, few query rows (nodes times query heads of a KV head): up to 64, of 4-bit
-// rows up to 32.
+// Attention of a tree of drafted tokens over ragged caches, few query rows (nodes times query heads of a KV head): up to 64, or 32
+// (rule at tree_launch).
 //
 // Products, layouts and work items are those of tree.hip.  Here every wavefront takes all query rows, in one or two blocks of 32, and
 // streams slabs of 32 keys of its own, without a barrier: the K rows of its next slab are requested as soon as the first product
@@ -7,6 +7,10 @@
 // wavefronts' do not come and go together.  bf16 and fp32 rows are copied straight to LDS.  Of 4-bit rows a lane takes half a row's
 // codes, which are an operand of the first product once the head dimension is numbered that way; V's values pass through LDS to
 // be transposed.  At the end the wavefronts' outputs are added up in LDS and leave as whole rows.
+//
+// HBM bounds it from some 100 MB on: 64 caches of 10240 bf16 rows, one query row, 59 us with the merge (335 MB, 47 at 7.1 TB/s).  Small
+// calls are bound by their start: 8 caches of 4096 rows, 16 query rows, 11 us, of 64 rows 9: lengths, scan, first rows, drafted rows
+// and the way out are a chain of memory latencies, and the code itself (some 10 KB, run through once) comes from memory too.
 #include "common.h"
 #include "mxfp4.h"
 #include "tree.h"
@@ -469,8 +473,9 @@ __global__ __launch_bounds__(64 * stream_waves(TYPE, D), stream_waves(TYPE, D) /
 
 template <int TYPE, int D>
 hipError_t launch(const TreeParams& p, unsigned grid, hipStream_t s) {
-  if (TYPE == 2 || p.rows <= 32) tree_stream_kernel<TYPE, D, 1><<<dim3(grid), dim3(Shape<TYPE, D, 1>::kThreads), 0, s>>>(p);
-  else if constexpr (TYPE != 2) tree_stream_kernel<TYPE, D, 2><<<dim3(grid), dim3(Shape<TYPE, D, 2>::kThreads), 0, s>>>(p);
+  constexpr bool kOne = TYPE == 2 || (TYPE == 1 && D == 128);
+  if (kOne || p.rows <= 32) tree_stream_kernel<TYPE, D, 1><<<dim3(grid), dim3(Shape<TYPE, D, 1>::kThreads), 0, s>>>(p);
+  else if constexpr (!kOne) tree_stream_kernel<TYPE, D, 2><<<dim3(grid), dim3(Shape<TYPE, D, 2>::kThreads), 0, s>>>(p);
   return hipGetLastError();
 }
 

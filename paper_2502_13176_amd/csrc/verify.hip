@@ -17,6 +17,11 @@
 // none); the walk, and the weights of parts of the last node's row, of which the last workgroup to end takes the token.  With
 // draft rows what is left of a distribution is a difference, so the walk is a launch of its own that also sums up the rows it
 // ends with in 64 bits.
+//
+// Latency bounds it: chains of memory reads, and code that is run through once and comes from memory itself (192 cycles for 64 bytes),
+// which is why loops are kept as loops.  Chain of 5, 32000 tokens, greedy: 12 us (4.7 and 7.6); 8 trees of up to 32 nodes, 131072
+// tokens: 30 us (11 for 16 MB of rows that may be visited, 18); 16 chains of 6 with draft rows, 100003 tokens in fp32: 54 us (20 for 77
+// MB, 14, 19).
 #include "common.h"
 
 namespace baklava {
