@@ -141,199 +141,199 @@ __global__ __launch_bounds__(64 * score_waves(TYPE, D), score_waves(TYPE, D) / 4
   float* const mine = ring + wave * S::kRing * kSlab;
 
   for (;; ++c_rel, tile = 0) {  // the caches it has a part of
-  const int2 t = p.table[c_rel];
-  const int n_old = __builtin_amdgcn_readfirstlane(t.x), n_path = __builtin_amdgcn_readfirstlane(t.y);
-  if (n_path == 0) continue;  // (tiles are left, so there is another cache)
-  const int64_t row0 = uniform(p.off[p.cache0 + c_rel]);
-  const int n = n_old + n_path, n_rows = n_path * p.G, n_blocks = (n_rows + 31) / 32;
-  const int tile_end = min(tile + left, (n + kTile - 1) / kTile);
-  left -= tile_end - tile;
-  const int slab_end = min(tile_end * kWaves, (n + kSlab - 1) / kSlab);
-  // Rows, scores and scales of a slab, straight to LDS.  (Codes are read with the ordinary hint: a cache line of theirs is asked for
-  // by two instructions, and is fetched twice without a stay in the cache, 53 / 58 us.)
-  auto request = [&](int buf, int slab) {
-    const uint32_t most = n - 1 - slab * kSlab;  // rows past the last repeat it
-    const int64_t first = row0 + (int64_t)slab * kSlab;
-    const uint32_t at = wave * S::kAhead + buf;
-    const uint32_t dst = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds + at * S::kStage;
-    const uint32_t dst_score = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float*)lds_score + at * 256;
-    const unsigned char* src = Kp + first * S::kStored;
-    const float* src_score = p.score + first;
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (what lay there has been read)
+    const int2 t = p.table[c_rel];
+    const int n_old = __builtin_amdgcn_readfirstlane(t.x), n_path = __builtin_amdgcn_readfirstlane(t.y);
+    if (n_path == 0) continue;  // (tiles are left, so there is another cache)
+    const int64_t row0 = uniform(p.off[p.cache0 + c_rel]);
+    const int n = n_old + n_path, n_rows = n_path * p.G, n_blocks = (n_rows + 31) / 32;
+    const int tile_end = min(tile + left, (n + kTile - 1) / kTile);
+    left -= tile_end - tile;
+    const int slab_end = min(tile_end * kWaves, (n + kSlab - 1) / kSlab);
+    // Rows, scores and scales of a slab, straight to LDS.  (Codes are read with the ordinary hint: a cache line of theirs is asked for
+    // by two instructions, and is fetched twice without a stay in the cache, 53 / 58 us.)
+    auto request = [&](int buf, int slab) {
+      const uint32_t most = n - 1 - slab * kSlab;  // rows past the last repeat it
+      const int64_t first = row0 + (int64_t)slab * kSlab;
+      const uint32_t at = wave * S::kAhead + buf;
+      const uint32_t dst = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds + at * S::kStage;
+      const uint32_t dst_score = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float*)lds_score + at * 256;
+      const unsigned char* src = Kp + first * S::kStored;
+      const float* src_score = p.score + first;
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (what lay there has been read)
 #pragma unroll
-    for (int i = 0; i < S::kCopies; ++i) {
-      const uint32_t from = min(c_row[i], most) * (uint32_t)S::kStored + off[i];
-      if constexpr (S::kMx)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst + i * 1024), "v"(from), "s"(src) : "memory", "m0");
-      else
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "s"(dst + i * 1024), "v"(from), "s"(src) : "memory", "m0");
-    }
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
-                 :: "s"(dst_score), "v"(min((uint32_t)n32, most) * 4), "s"(src_score) : "memory", "m0");
-    if constexpr (S::kMx) {  // a row's D / 16 scale bytes: two words or one
-      const uint8_t* src_scale = p.kv_scale + first * (D / 16);
-      const uint32_t dst_scale = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint32_t*)lds_scale + at * 256;
-      const uint32_t r = D == 128 ? lane / 2 : n32, from = min(r, most) * (D / 16) + (D == 128 ? lane % 2 * 4 : 0);
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" :: "s"(dst_scale), "v"(from), "s"(src_scale) : "memory", "m0");
-    }
-  };
-  int slab = tile * kWaves + wave;
+      for (int i = 0; i < S::kCopies; ++i) {
+        const uint32_t from = min(c_row[i], most) * (uint32_t)S::kStored + off[i];
+        if constexpr (S::kMx)
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(dst + i * 1024), "v"(from), "s"(src) : "memory", "m0");
+        else
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "s"(dst + i * 1024), "v"(from), "s"(src) : "memory", "m0");
+      }
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+                   :: "s"(dst_score), "v"(min((uint32_t)n32, most) * 4), "s"(src_score) : "memory", "m0");
+      if constexpr (S::kMx) {  // a row's D / 16 scale bytes: two words or one
+        const uint8_t* src_scale = p.kv_scale + first * (D / 16);
+        const uint32_t dst_scale = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint32_t*)lds_scale + at * 256;
+        const uint32_t r = D == 128 ? lane / 2 : n32, from = min(r, most) * (D / 16) + (D == 128 ? lane % 2 * 4 : 0);
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" :: "s"(dst_scale), "v"(from), "s"(src_scale) : "memory", "m0");
+      }
+    };
+    int slab = tile * kWaves + wave;
 #pragma unroll
-  for (int a = 0; a < S::kAhead; ++a)
-    if (slab + a * kWaves < slab_end) request(a, slab + a * kWaves);
+    for (int a = 0; a < S::kAhead; ++a)
+      if (slab + a * kWaves < slab_end) request(a, slab + a * kWaves);
 
-  // Query row r of the path; rows past the last repeat it and weigh nothing.
-  const int h = (uint32_t)c_rel % (uint32_t)p.Hkv, s_rel = (uint32_t)c_rel / (uint32_t)p.Hkv, b = (uint32_t)s_rel % (uint32_t)p.batch;
-  const int32_t* const path = p.path + (int64_t)b * p.N;
-  auto load_q = [&](u32x4_t (&qa)[S::kChunks], int r0) {
-    const uint32_t at = min(r0 + n32, n_rows - 1);
-    const unsigned char* src = row_of(p.q, s_rel, path[at / (uint32_t)p.G], h * p.G + at % (uint32_t)p.G);
+    // Query row r of the path; rows past the last repeat it and weigh nothing.
+    const int h = (uint32_t)c_rel % (uint32_t)p.Hkv, s_rel = (uint32_t)c_rel / (uint32_t)p.Hkv, b = (uint32_t)s_rel % (uint32_t)p.batch;
+    const int32_t* const path = p.path + (int64_t)b * p.N;
+    auto load_q = [&](u32x4_t (&qa)[S::kChunks], int r0) {
+      const uint32_t at = min(r0 + n32, n_rows - 1);
+      const unsigned char* src = row_of(p.q, s_rel, path[at / (uint32_t)p.G], h * p.G + at % (uint32_t)p.G);
 #pragma unroll
-    for (int c = 0; c < S::kChunks; ++c) qa[c] = *reinterpret_cast<const u32x4_t*>(src + S::piece(c, jh) * 16);
-  };
-  auto lse_of = [&](int r) {
-    return r < n_rows ? *reinterpret_cast<const float*>(row_of(p.lse, s_rel, path[(uint32_t)r / (uint32_t)p.G], h * p.G + (uint32_t)r % (uint32_t)p.G))
-                      : __builtin_huge_valf();
-  };
-  u32x4_t qa[S::kQueriesInLds ? 1 : 2][S::kChunks];
-  if constexpr (!S::kQueriesInLds) {
-    load_q(qa[0], 0);
-    if (n_blocks > 1) load_q(qa[1], 32);
-  }
-  __syncthreads();  // (what the cache before needed has been read)
-  if (tid < 64) lse[tid] = lse_of(tid);
-  if constexpr (S::kQueriesInLds) {
-    for (int x = tid; x < min(n_blocks, 2) * 32 * S::kPieces; x += S::kThreads) {  // (rows past the last repeat it)
-      const uint32_t r = x / S::kPieces, piece = x % S::kPieces, at = min(r, (uint32_t)n_rows - 1);
-      *reinterpret_cast<u32x4_t*>(lds_q + r * S::kRow + S::q_slot(r, piece) * 16) =
-          *reinterpret_cast<const u32x4_t*>(row_of(p.q, s_rel, path[at / (uint32_t)p.G], h * p.G + at % (uint32_t)p.G) + piece * 16);
+      for (int c = 0; c < S::kChunks; ++c) qa[c] = *reinterpret_cast<const u32x4_t*>(src + S::piece(c, jh) * 16);
+    };
+    auto lse_of = [&](int r) {
+      return r < n_rows ? *reinterpret_cast<const float*>(row_of(p.lse, s_rel, path[(uint32_t)r / (uint32_t)p.G], h * p.G + (uint32_t)r % (uint32_t)p.G))
+                        : __builtin_huge_valf();
+    };
+    u32x4_t qa[S::kQueriesInLds ? 1 : 2][S::kChunks];
+    if constexpr (!S::kQueriesInLds) {
+      load_q(qa[0], 0);
+      if (n_blocks > 1) load_q(qa[1], 32);
     }
-  }
-  __syncthreads();
-  // register i of a block's logits: row 32 blk + 8 (i / 4) + 4 h + i % 4; a path's row j is seen by its nodes from j on
-  auto product = [&](floatx16_t& s, const u32x4_t& q, const u32x4_t& k, bool first) {
-    const floatx16_t zero = {};
-    if constexpr (S::kF32) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(q[e]), __uint_as_float(k[e]), first && e == 0 ? zero : s, 0, 0, 0);
-    } else {
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, q), __builtin_bit_cast(bf16x8_t, k), first ? zero : s, 0, 0, 0);
-    }
-  };
-  auto weights = [&](const floatx16_t& s, int blk, int slab, float& sum) {
-    const float* z = lse + blk * 32 + 4 * jh;
-    const bool fresh = (slab + 1) * kSlab > n_old;  // new rows among them
-    const int first_row = fresh ? (slab * kSlab + n32 - n_old) * p.G - blk * 32 - 4 * jh : INT32_MIN;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if (blk * 32 + 8 * q >= n_rows) break;
-      const floatx4_t y = *reinterpret_cast<const floatx4_t*>(z + 8 * q);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float w = fast_exp2(fmaf(s[4 * q + i], cs, -y[i]));
-        sum += 8 * q + i >= first_row ? w : 0.f;
+    __syncthreads();  // (what the cache before needed has been read)
+    if (tid < 64) lse[tid] = lse_of(tid);
+    if constexpr (S::kQueriesInLds) {
+      for (int x = tid; x < min(n_blocks, 2) * 32 * S::kPieces; x += S::kThreads) {  // (rows past the last repeat it)
+        const uint32_t r = x / S::kPieces, piece = x % S::kPieces, at = min(r, (uint32_t)n_rows - 1);
+        *reinterpret_cast<u32x4_t*>(lds_q + r * S::kRow + S::q_slot(r, piece) * 16) =
+            *reinterpret_cast<const u32x4_t*>(row_of(p.q, s_rel, path[at / (uint32_t)p.G], h * p.G + at % (uint32_t)p.G) + piece * 16);
       }
     }
-  };
-  // Blocks beyond those two, of long paths: their rows and normalisers come from memory, again for every slab.
-  auto weights_of_far_rows = [&](const floatx16_t& s, int blk, int slab, float& sum) {
-    const int first_row = (slab * kSlab + n32 - n_old) * p.G - blk * 32 - 4 * jh;
+    __syncthreads();
+    // register i of a block's logits: row 32 blk + 8 (i / 4) + 4 h + i % 4; a path's row j is seen by its nodes from j on
+    auto product = [&](floatx16_t& s, const u32x4_t& q, const u32x4_t& k, bool first) {
+      const floatx16_t zero = {};
+      if constexpr (S::kF32) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int r = 8 * (i / 4) + i % 4;
-      const float w = fast_exp2(fmaf(s[i], cs, -lse_of(blk * 32 + 4 * jh + r)));
-      sum += r >= first_row ? w : 0.f;
-    }
-  };
-  // New scores are stored several slabs at a time: whoever waits for a load also waits for the stores in front of it.
-  int waiting = 0;
-  auto store = [&](int first) {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    for (int i = lane; i < waiting * kSlab; i += 64) {
-      const int row = (first + i / kSlab * kWaves) * kSlab + i % kSlab;
-      if (row < n) p.score[row0 + row] = mine[i];
-    }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();  // (the ring may be written again)
-    waiting = 0;
-  };
-  for (int buf = 0; slab < slab_end; slab += kWaves) {
-    // (loads come back in order: with as many outstanding as have been asked for behind them, stores among them or not, this slab's
-    // are there)
-    if (slab + (S::kAhead - 1) * kWaves < slab_end) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(S::kRequests * (S::kAhead - 1)) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    const int at = wave * S::kAhead + buf;
-    const unsigned char* src = lds + at * S::kStage + n32 * S::kStored;
-    u32x4_t codes[S::kMx ? S::kWords / 4 : 1];  // half a row's
-    uint32_t bytes = 0;
-    if constexpr (S::kMx) {
-#pragma unroll
-      for (int i = 0; i < S::kWords / 4; ++i) codes[i] = *reinterpret_cast<const u32x4_t*>(src + S::slot(n32, jh * (S::kWords / 4) + i) * 16);
-      bytes = D == 128 ? lds_scale[at * 64 + n32 * 2] >> (16 * jh) : lds_scale[at * 64 + n32] >> (8 * jh);
-    }
-    auto key = [&](int c) {  // chunk c of row n32 of the slab
-      if constexpr (S::kMx) {
-        const uint4 x = mx_values(codes[c / 4][c % 4], mx_scale(bytes >> (8 * (c / 4)) & 255));
-        return u32x4_t{x.x, x.y, x.z, x.w};
+        for (int e = 0; e < 4; ++e)
+          s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(q[e]), __uint_as_float(k[e]), first && e == 0 ? zero : s, 0, 0, 0);
       } else {
-        return *reinterpret_cast<const u32x4_t*>(src + S::slot(n32, 2 * c + jh) * 16);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, q), __builtin_bit_cast(bf16x8_t, k), first ? zero : s, 0, 0, 0);
       }
     };
-    const float before = lds_score[at * 64 + n32];
-    float sum = 0.f;
-    floatx16_t s0;
-    auto far_rows = [&]() {
-#pragma unroll 1
-      for (int blk = 2; blk < n_blocks; ++blk) {
-        u32x4_t q[S::kChunks];
-        load_q(q, blk * 32);
+    auto weights = [&](const floatx16_t& s, int blk, int slab, float& sum) {
+      const float* z = lse + blk * 32 + 4 * jh;
+      const bool fresh = (slab + 1) * kSlab > n_old;  // new rows among them
+      const int first_row = fresh ? (slab * kSlab + n32 - n_old) * p.G - blk * 32 - 4 * jh : INT32_MIN;
 #pragma unroll
-        for (int c = 0; c < S::kChunks; ++c) product(s0, q[c], key(c), c == 0);
-        weights_of_far_rows(s0, blk, slab, sum);
-      }
-    };
-    const int ahead = slab + S::kAhead * kWaves;
-    if constexpr (S::kQueriesInLds) {  // (the codes are in registers)
-      if (ahead < slab_end) request(buf, ahead);
-#pragma unroll 1
-      for (int blk = 0; blk < min(n_blocks, 2); ++blk) {
+      for (int q = 0; q < 4; ++q) {
+        if (blk * 32 + 8 * q >= n_rows) break;
+        const floatx4_t y = *reinterpret_cast<const floatx4_t*>(z + 8 * q);
 #pragma unroll
-        for (int c = 0; c < S::kChunks; ++c)
-          product(s0, *reinterpret_cast<const u32x4_t*>(lds_q + (blk * 32 + n32) * S::kRow + S::q_slot(n32, S::piece(c, jh)) * 16), key(c), c == 0);
-        weights(s0, blk, slab, sum);
-      }
-      far_rows();
-    } else {
-      floatx16_t s1;
-      if (n_blocks == 1) {
-#pragma unroll
-        for (int c = 0; c < S::kChunks; ++c) product(s0, qa[0][c], key(c), c == 0);
-      } else {
-#pragma unroll
-        for (int c = 0; c < S::kChunks; ++c) {
-          const u32x4_t k = key(c);
-          product(s0, qa[0][c], k, c == 0);
-          product(s1, qa[1][c], k, c == 0);
+        for (int i = 0; i < 4; ++i) {
+          const float w = fast_exp2(fmaf(s[4 * q + i], cs, -y[i]));
+          sum += 8 * q + i >= first_row ? w : 0.f;
         }
       }
-      if (n_blocks <= 2 && ahead < slab_end) request(buf, ahead);
-      weights(s0, 0, slab, sum);
-      if (n_blocks > 1) weights(s1, 1, slab, sum);
-      if (n_blocks > 2) {
-        far_rows();
-        if (ahead < slab_end) request(buf, ahead);
+    };
+    // Blocks beyond those two, of long paths: their rows and normalisers come from memory, again for every slab.
+    auto weights_of_far_rows = [&](const floatx16_t& s, int blk, int slab, float& sum) {
+      const int first_row = max(slab * kSlab + n32 - n_old, 0) * p.G - blk * 32 - 4 * jh;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int r = 8 * (i / 4) + i % 4;
+        const float w = fast_exp2(fmaf(s[i], cs, -lse_of(blk * 32 + 4 * jh + r)));
+        sum += r >= first_row ? w : 0.f;
       }
+    };
+    // New scores are stored several slabs at a time: whoever waits for a load also waits for the stores in front of it.
+    int waiting = 0;
+    auto store = [&](int first) {
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      for (int i = lane; i < waiting * kSlab; i += 64) {
+        const int row = (first + i / kSlab * kWaves) * kSlab + i % kSlab;
+        if (row < n) p.score[row0 + row] = mine[i];
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();  // (the ring may be written again)
+      waiting = 0;
+    };
+    for (int buf = 0; slab < slab_end; slab += kWaves) {
+      // (loads come back in order: with as many outstanding as have been asked for behind them, stores among them or not, this slab's
+      // are there)
+      if (slab + (S::kAhead - 1) * kWaves < slab_end) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(S::kRequests * (S::kAhead - 1)) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      const int at = wave * S::kAhead + buf;
+      const unsigned char* src = lds + at * S::kStage + n32 * S::kStored;
+      u32x4_t codes[S::kMx ? S::kWords / 4 : 1];  // half a row's
+      uint32_t bytes = 0;
+      if constexpr (S::kMx) {
+#pragma unroll
+        for (int i = 0; i < S::kWords / 4; ++i) codes[i] = *reinterpret_cast<const u32x4_t*>(src + S::slot(n32, jh * (S::kWords / 4) + i) * 16);
+        bytes = D == 128 ? lds_scale[at * 64 + n32 * 2] >> (16 * jh) : lds_scale[at * 64 + n32] >> (8 * jh);
+      }
+      auto key = [&](int c) {  // chunk c of row n32 of the slab
+        if constexpr (S::kMx) {
+          const uint4 x = mx_values(codes[c / 4][c % 4], mx_scale(bytes >> (8 * (c / 4)) & 255));
+          return u32x4_t{x.x, x.y, x.z, x.w};
+        } else {
+          return *reinterpret_cast<const u32x4_t*>(src + S::slot(n32, 2 * c + jh) * 16);
+        }
+      };
+      const float before = lds_score[at * 64 + n32];
+      float sum = 0.f;
+      floatx16_t s0;
+      auto far_rows = [&]() {
+#pragma unroll 1
+        for (int blk = 2; blk < n_blocks; ++blk) {
+          u32x4_t q[S::kChunks];
+          load_q(q, blk * 32);
+#pragma unroll
+          for (int c = 0; c < S::kChunks; ++c) product(s0, q[c], key(c), c == 0);
+          weights_of_far_rows(s0, blk, slab, sum);
+        }
+      };
+      const int ahead = slab + S::kAhead * kWaves;
+      if constexpr (S::kQueriesInLds) {  // (the codes are in registers)
+        if (ahead < slab_end) request(buf, ahead);
+#pragma unroll 1
+        for (int blk = 0; blk < min(n_blocks, 2); ++blk) {
+#pragma unroll
+          for (int c = 0; c < S::kChunks; ++c)
+            product(s0, *reinterpret_cast<const u32x4_t*>(lds_q + (blk * 32 + n32) * S::kRow + S::q_slot(n32, S::piece(c, jh)) * 16), key(c), c == 0);
+          weights(s0, blk, slab, sum);
+        }
+        far_rows();
+      } else {
+        floatx16_t s1;
+        if (n_blocks == 1) {
+#pragma unroll
+          for (int c = 0; c < S::kChunks; ++c) product(s0, qa[0][c], key(c), c == 0);
+        } else {
+#pragma unroll
+          for (int c = 0; c < S::kChunks; ++c) {
+            const u32x4_t k = key(c);
+            product(s0, qa[0][c], k, c == 0);
+            product(s1, qa[1][c], k, c == 0);
+          }
+        }
+        if (n_blocks <= 2 && ahead < slab_end) request(buf, ahead);
+        weights(s0, 0, slab, sum);
+        if (n_blocks > 1) weights(s1, 1, slab, sum);
+        if (n_blocks > 2) {
+          far_rows();
+          if (ahead < slab_end) request(buf, ahead);
+        }
+      }
+      buf = buf + 1 == S::kAhead ? 0 : buf + 1;
+      sum += __shfl_xor(sum, 32);
+      if (jh == 0) mine[waiting * kSlab + n32] = before + sum;
+      if (++waiting == S::kRing) store(slab - (S::kRing - 1) * kWaves);
     }
-    buf = buf + 1 == S::kAhead ? 0 : buf + 1;
-    sum += __shfl_xor(sum, 32);
-    if (jh == 0) mine[waiting * kSlab + n32] = before + sum;
-    if (++waiting == S::kRing) store(slab - (S::kRing - 1) * kWaves);
-  }
-  if (waiting > 0) store(slab - waiting * kWaves);
-  if (left == 0) break;
+    if (waiting > 0) store(slab - waiting * kWaves);
+    if (left == 0) break;
   }
 }
 

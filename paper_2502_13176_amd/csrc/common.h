@@ -258,7 +258,6 @@ struct TreeLaunch {
 constexpr int kMostTreeItems = 512;   // work items of a launch that are aimed at, and therefore of a cache, at most
 constexpr int kStreamRows = 64;       // query rows that the streaming kernel takes
 
-constexpr int kAcceptRows = kMostNodes * 16;  // query rows of a path
 struct AcceptParams {
   Rows k, v;                // strides in 16-byte pieces; sequences as in TreeParams
   Rows q, lse;              // in bytes (tracking only)

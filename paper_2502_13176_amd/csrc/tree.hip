@@ -337,6 +337,11 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attn_kernel(TreeParams p) {
     }
     for (; kt < live_end; ++kt) {
       if constexpr (!S::kMx) ask(ck, cv, kt);
+      if ((kt + 1) * kTile > n_live) {  // (a weight of zero times an infinity of the row that was repeated would be NaN)
+        for (int x = (n_live - kt * kTile) * S::kPieces + tid; x < kTile * S::kPieces; x += kThreads)
+          *reinterpret_cast<u32x4_t*>(lds_v[kt & 1] + x * 16) = u32x4_t{};
+        __syncthreads();
+      }
       if (!idle) {
         if ((kt + 1) * kTile > n_live) {
 #pragma unroll
@@ -610,14 +615,14 @@ hipError_t launch(const TreeParams& p, int ks, unsigned grid, hipStream_t s) {
 
 }  // namespace
 
-// The streaming kernel takes up to 64 query rows, up to 32 where two blocks of them cost it too many registers.  us a call, it / this
-// one with pairs of wavefronts, 64 caches of 10240 rows: bf16, D = 128, 64 rows 61.8 / 65.9, D = 64 36.4 / 40.7, 1 row 59.0 / 69.2; 4-bit
-// rows, 32 rows 29.7 / 41.9, D = 64 22.0 / 34.3, 52 rows (128 caches of 9830) 130 / 73; fp32, 32 caches of 4096 rows, D = 64, 64 rows
-// 43.0 / 42.1, D = 128 78.4 / 65.5, 32 rows 47.2 / 59.9.  Here up to 64 rows are taken by pairs of wavefronts, each with half of a
-// tile's keys: the 52 rows of 4 bits 73, without pairs 92.
+// The streaming kernel takes up to 64 query rows over bf16 caches, up to 32 over the others, where two blocks of them cost it too many
+// registers.  us a call, it / this one with pairs of wavefronts, 64 caches of 10240 rows: bf16, D = 128, 64 rows 61.8 / 65.9, D = 64
+// 36.4 / 40.7, 1 row 59.0 / 69.2; 4-bit rows, 32 rows 29.7 / 41.9, D = 64 22.0 / 34.3, 52 rows (128 caches of 9830) 130 / 73; fp32, 32
+// caches of 4096 rows, D = 64, 64 rows 43.0 / 42.1, D = 128 78.4 / 65.5, 32 rows 47.2 / 59.9.  Here up to 64 rows are taken by pairs of
+// wavefronts, each with half of a tile's keys: the 52 rows of 4 bits 73, without pairs 92.
 TreeLaunch tree_launch(int type, int D, int rows, int n_cus) {
   TreeLaunch t;
-  if (rows <= (type == 2 || (type == 1 && D == 128) ? kStreamRows / 2 : kStreamRows)) {
+  if (rows <= (type == 0 ? kStreamRows : kStreamRows / 2)) {
     t.ks = 0;
     t.row_tiles = 1;
     t.target = n_cus < kMostTreeItems ? n_cus : kMostTreeItems;

@@ -1,7 +1,7 @@
 // Attention of a tree of drafted tokens over ragged caches, few query rows (nodes times query heads of a KV head): up to 64, or 32
 // (rule at tree_launch).
 //
-// Products, layouts and work items are those of tree.hip.  Here every wavefront takes all query rows, in one or two blocks of 32, and
+// Products, layouts and work items are those of tree.hip.  Here every wavefront takes all query rows, in one or (bf16) two blocks of 32, and
 // streams slabs of 32 keys of its own, without a barrier: the K rows of its next slab are requested as soon as the first product
 // has read the last ones, the V rows as soon as the second one has, so that its requests follow each other at any time and the
 // wavefronts' do not come and go together.  bf16 and fp32 rows are copied straight to LDS.  Of 4-bit rows a lane takes half a row's
@@ -49,8 +49,8 @@ struct Shape {
   static constexpr int kLds = kWaves * (kArea > kOut ? kArea : kOut);
   static constexpr int kCopyRows = 64 / kPieces, kCopies = kSlab / kCopyRows;
   static constexpr int kWords = D / 16;                       // 4-bit rows: words of codes in half a row
-  static constexpr int kAhead = kMx && RB == 1 ? 2 : 1;       // slabs on the way
-  static constexpr bool kQueriesInLds = RB == 2 && !kF32;     // (registers run out)
+  static constexpr int kAhead = kMx ? 2 : 1;                  // slabs on the way
+  static constexpr bool kQueriesInLds = RB == 2;              // (registers run out)
   // piece of a row that lane half h takes as chunk c of the first product
   static __device__ __forceinline__ int piece(int c, int h) { return kMx ? h * kChunks + c : 2 * c + h; }
   // where piece x of row r lies in LDS
@@ -313,6 +313,15 @@ __global__ __launch_bounds__(64 * stream_waves(TYPE, D), stream_waves(TYPE, D) /
     weigh(s);
     put_v(cv);
     wait(more);
+    if ((slab + 1) * kSlab > n_live) {  // (a weight of zero times an infinity of the row that was repeated would be NaN)
+      if (slab * kSlab + n32 >= n_live) {
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) *reinterpret_cast<u32x4_t*>(my_v + n32 * kRow + (jh * kChunks + c) * 16) = u32x4_t{};
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
     outputs(s, false);
     if (more) request(cv, 1, ahead);
     slab += kWaves;
@@ -473,7 +482,7 @@ __global__ __launch_bounds__(64 * stream_waves(TYPE, D), stream_waves(TYPE, D) /
 
 template <int TYPE, int D>
 hipError_t launch(const TreeParams& p, unsigned grid, hipStream_t s) {
-  constexpr bool kOne = TYPE == 2 || (TYPE == 1 && D == 128);
+  constexpr bool kOne = TYPE != 0;  // (rule at tree_launch)
   if (kOne || p.rows <= 32) tree_stream_kernel<TYPE, D, 1><<<dim3(grid), dim3(Shape<TYPE, D, 1>::kThreads), 0, s>>>(p);
   else if constexpr (!kOne) tree_stream_kernel<TYPE, D, 2><<<dim3(grid), dim3(Shape<TYPE, D, 2>::kThreads), 0, s>>>(p);
   return hipGetLastError();

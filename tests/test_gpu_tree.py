@@ -203,6 +203,23 @@ def test_infinite_and_nan_rows_of_nodes_that_are_not_seen(dtype, D):
             assert got[sees7].isnan().all()
 
 
+@pytest.mark.parametrize("dtype,D,G,N", [("bf16", 128, 4, 6), ("bf16", 128, 8, 8), ("bf16", 128, 4, 40), ("bf16", 64, 1, 1), ("bf16", 64, 3, 90),
+                                         ("f32", 128, 2, 3), ("f32", 128, 2, 20), ("f32", 64, 4, 16), ("f32", 64, 4, 60)])
+def test_infinite_values_of_the_last_live_row(dtype, D, G, N):
+    """An infinity in the last row of a cache, anywhere in a tile, is one in that element of every output, and nothing else changes."""
+    a, K, V = make(dtype, D, G, 2, 3, 1, (1, 31, 33, 70, 128, 600), seed=3)
+    last = [int(a.off_host[c]) + int(a.len[c]) - 1 for c in range(6)]
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    g = torch.Generator().manual_seed(4)
+    k, v = (nodes("packed", 3, N, 2, D, dt, g) for _ in range(2))
+    q, parent = nodes("packed", 3, N, 2 * G, D, dt, g), torch.from_numpy(parents("tree", 3, N)).cuda()
+    want, lse = a.tree_attn(0, 1, k, v, parent, q, want_lse=True)
+    a.v[last, 5], a.v[last, D - 1] = float("inf"), float("-inf")
+    got, again = a.tree_attn(0, 1, k, v, parent, q, want_lse=True)
+    want[..., 5], want[..., D - 1] = float("inf"), float("-inf")
+    assert torch.equal(got, want) and torch.equal(again, lse)
+
+
 def test_logits_far_apart():
     """Queries whose logits spread over thousands: one key takes everything, in any tile, and the running maximum follows."""
     for dtype in ("bf16", "f32", "mxfp4"):
