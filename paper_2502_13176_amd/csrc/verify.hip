@@ -76,7 +76,7 @@ __device__ __forceinline__ const void* row_at(const void* data, int64_t row) {
   return reinterpret_cast<const char*>(data) + row * (F32 ? 4 : 2);
 }
 
-// 2^((x - top) c) for x <= top, 0 where x is -inf (top may be, too); c = log2(e) / temperature.  The fraction f of the exponent, at most
+// 2^((x - top) c) for x <= top, 0 where x is -inf (top may be, too: y is NaN); c = log2(e) / temperature.  The fraction f of the exponent, at most
 // 1/2, goes into the series sum (f ln 2)^k / k!, whose next term is below 2^-47 of it; equal logits give exactly 1.
 __device__ __forceinline__ double weight(float x, float top, double c) {
   const double y = ((double)x - (double)top) * c, n = __builtin_rint(y), f = y - n;
@@ -91,13 +91,13 @@ __device__ __forceinline__ double weight(float x, float top, double c) {
   s = __builtin_fma(s, f, 2.4022650695910071e-1);
   s = __builtin_fma(s, f, 6.9314718055994531e-1);
   s = __builtin_fma(s, f, 1.0);
-  return x > kNegInf ? __builtin_amdgcn_ldexp(s, (int)__builtin_fmax(n, -2000.0)) : 0.0;
+  return y > -1080.0 ? __builtin_amdgcn_ldexp(s, (int)n) : 0.0;  // (far below, f is the product's rounding and s anything)
 }
 
 __device__ __forceinline__ int nodes_of(const VerifyParams& p, int b) { return p.n_nodes ? min(max(p.n_nodes[b], 0), p.N) : p.N; }
 __device__ __forceinline__ double exponent_scale(const VerifyParams& p, int b) {  // log2(e) / temperature; 0: greedy
   const float t = p.temp ? p.temp[b] : 1.f;
-  return t > 0.f ? 1.4426950408889634 / (double)t : 0.0;
+  return t > 0.f ? __builtin_fmax(1.4426950408889634 / (double)t, 1e-300) : 0.0;  // (of an infinite one no more than a sign is left)
 }
 
 // x of the lane ROR further on in its row of 16.
@@ -179,11 +179,12 @@ __device__ __forceinline__ Top top_of_threads(Top t, Top* lds) {
   return t;
 }
 
-// The same by the hardware's exponential: c = hi + lo, and what the product with the difference lacks goes in behind it.
+// The same by the hardware's exponential: c = hi + lo, and what the product with the difference lacks goes in behind it.  Below 2^-150,
+// where a logit is the type's lowest value too and the product -inf (or NaN: x is -inf), it is 0.
 __device__ __forceinline__ float quick_weight(float x, float top, float hi, float lo) {
   const float d = x - top, y = d * hi, rest = fmaf(d, lo, fmaf(d, hi, -y));
   const float w = __builtin_amdgcn_exp2f(y);
-  return x > kNegInf ? fmaf(w, rest * 0.69314718f, w) : 0.f;
+  return y > -150.f ? fmaf(w, rest * 0.69314718f, w) : 0.f;
 }
 
 // One part of one row: workgroups over the parts first, then the nodes, then target and draft rows.
@@ -233,7 +234,7 @@ __global__ __launch_bounds__(kThreads) void verify_stat_kernel(VerifyParams p) {
       for (int e = 0; e < 8; ++e) s += weight(x[k][e], t.x, c);
     s = sum_threads(s, sums);
   } else if (c > 0.0) {
-    const float hi = (float)c, lo = (float)(c - (double)hi);
+    const float hi = (float)__builtin_fmin(c, 1e38), lo = c > 1e38 ? 0.f : (float)(c - (double)hi);
 #pragma unroll
     for (int k = 0; k < kPer / 8; ++k)
 #pragma unroll

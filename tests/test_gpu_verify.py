@@ -120,6 +120,26 @@ def test_values_that_are_not_finite():
     same(run(t), expect(t))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("drafts", [False, True])
+@pytest.mark.parametrize("temp", [None, 0.7, 1e-3, 1e-30, 1e-42, 1e30, float("inf")])
+def test_lowest_and_largest_values_beside_ordinary_ones(dtype, drafts, temp):
+    """Tokens masked with the type's lowest value, rows with an infinity, temperatures at the ends of their range."""
+    B_, N, V = 6, 7, 300
+    for tree in ("chain", "tree"):
+        t = inputs(B_, N, V, tree, dtype, drafts, 11)
+        low = torch.finfo(t["logits"].dtype).min
+        keep = torch.rand((B_, N, V), generator=torch.Generator().manual_seed(5)) < 0.6
+        for b in range(B_):
+            for i in range(1, N):
+                keep[b, max(int(t["parent"][b, i]), 0), int(t["token"][b, i])] = True
+        t["logits"] = t["logits"].masked_fill(~keep, low)
+        if temp is None or temp < 1e30:
+            t["logits"][4, 0, 17] = float("inf")
+            t["logits"][5, 1, 3], t["logits"][5, 1, 5] = -low, -low
+        same(run(t, temperature=None if temp is None else torch.full((B_,), temp)), expect(t, None if temp is None else torch.full((B_,), temp)))
+
+
 def test_tokens_that_are_none_and_parents_that_are_none():
     t = inputs(4, 8, 50, "star", "f32", False, 1)
     want = expect(t)
