@@ -20,8 +20,8 @@
 //
 // Latency bounds it: chains of memory reads, and code that is run through once and comes from memory itself (192 cycles for 64 bytes),
 // which is why loops are kept as loops.  Chain of 5, 32000 tokens, greedy: 12 us (4.7 and 7.6); 8 trees of up to 32 nodes, 131072
-// tokens: 30 us (11 for 16 MB of rows that may be visited, 18); 16 chains of 6 with draft rows, 100003 tokens in fp32: 54 us (20 for 77
-// MB, 14, 19).
+// tokens: 29 us (11 for 16 MB of rows that may be visited, 18); 16 chains of 6 with draft rows, 100003 tokens in fp32: 51 us (20 for 77
+// MB, 12.5, 18.5).
 #include "common.h"
 
 namespace baklava {
