@@ -579,8 +579,9 @@ int baklava_tree_attn(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count
  * temperature DEVICE fp32 [n_seq] or NULL (1); u DEVICE fp32 [n_seq, N], 0 <= u < 1.  path_out DEVICE int32 [n_seq, N],
  * n_path_out, next_token_out DEVICE int32 [n_seq].  V 1 .. 2^30, rows times parts of 8192 elements below 2^21.
  * workspace DEVICE, baklava_verify_workspace_bytes(n_seq, N, V, draft_logits != NULL) bytes, 256-byte aligned, as above.
- * Sums are in 64 bits; so are the exponentials, but for those of a sum that only an acceptance test divides by (to about
- * 1e-8).  A rejected node of a sequence with draft_logits that has a later sibling costs a pass of one workgroup over the
+ * Sums are in 64 bits; so are the exponentials, but for those of a row that a single drafted token is tested against: its
+ * probability may be off by 1e-8 or so there, 2e-7 at most.  What rejected tokens leave of a distribution is summed up from what is
+ * left, however little that is: a row with a logit above -inf always has a next token.  A rejected node of a sequence with draft_logits that has a later sibling costs a pass of one workgroup over the
  * target row and the draft rows rejected before it, its own among them. Enqueues kernels on `stream`; deterministic.
  * Errors: EINVAL (null, misaligned, bad shape, stride or dtype), ECAPACITY (workspace too small), EHIP.
  */

@@ -10,8 +10,10 @@
 // are distributed as if the target had been sampled one by one.
 //
 // What decides between tokens next to each other is held in 64 bits: a vocabulary has 1e5 borders, and an error of 1e-7 in the sums
-// would hand one draw in a hundred to a neighbour.  A probability that is only compared with a random number may be off by some
-// 1e-8: sums of the rows that may be visited take the hardware's exponential, with what its argument lacks put back.
+// would hand one draw in a hundred to a neighbour.  So are the sums of nodes with several children, of whose rows little may be left
+// when a child's turn comes.  The one probability that a single child is tested against may be off by some 1e-8 (2e-7 at most: a
+// quarter of the sum's error, 2^-22 of the exponentials and up to 9 * 2^-24 of rounded differences of fp32 logits): its sum takes the
+// hardware's exponential, with what its argument lacks put back.
 //
 // Launches: the largest logit and the sum of exponentials of parts of the rows that a decision can need (a node without children is
 // none); the walk, and the weights of parts of the last node's row, of which the last workgroup to end takes the token.  With
@@ -20,7 +22,7 @@
 //
 // Latency bounds it: chains of memory reads, and code that is run through once and comes from memory itself (192 cycles for 64 bytes),
 // which is why loops are kept as loops.  Chain of 5, 32000 tokens, greedy: 12 us (4.7 and 7.6); 8 trees of up to 32 nodes, 131072
-// tokens: 29 us (11 for 16 MB of rows that may be visited, 18); 16 chains of 6 with draft rows, 100003 tokens in fp32: 51 us (20 for 77
+// tokens: 31 us (28 with sums by the hardware's exponential there, too); 16 chains of 6 with draft rows, 100003 tokens in fp32: 51 us (20 for 77
 // MB, 12.5, 18.5).
 #include "common.h"
 
@@ -193,6 +195,8 @@ __global__ __launch_bounds__(kThreads) void verify_stat_kernel(VerifyParams p) {
   __shared__ double sums[kWaves];
   __shared__ Top tops[kWaves];
   __shared__ int32_t children[kMostNodes];
+  __shared__ uint32_t taken[kThreads];        // bits of the part's elements that are a child's token
+  static_assert(kVerifyPart == 32 * kThreads, "a word for every thread");
   const int part = (uint32_t)blockIdx.x % (uint32_t)p.parts, r = (uint32_t)blockIdx.x / (uint32_t)p.parts;
   const bool draft = r >= p.n_seq * p.N;
   const int at = draft ? r - p.n_seq * p.N : r, b = (uint32_t)at / (uint32_t)p.N, i = (uint32_t)at % (uint32_t)p.N;
@@ -201,24 +205,41 @@ __global__ __launch_bounds__(kThreads) void verify_stat_kernel(VerifyParams p) {
   if (!draft && i == 0 && part == 0 && tid == 0) p.ticket[b] = 0;
   if (i >= n) return;
   children[tid] = 0;
-  int up = -1;
-  if (tid < n) up = p.parent[(int64_t)b * p.N + tid];
+  taken[tid] = 0;
+  // Drafted tokens that are point masses: what the children of a node leave of its row is added up from what is left, never a
+  // difference, so their tokens are no part of its sum.
+  const bool apart = !p.draft && c > 0.0;
+  int up = -1, mine = -1;
+  if (tid < n) {
+    up = p.parent[(int64_t)b * p.N + tid];
+    if (apart) mine = p.token[(int64_t)b * p.N + tid];
+  }
   if (up < 0 || up >= tid) up = -1;
   __syncthreads();
   if (up >= 0) atomicAdd(&children[up], 1);
+  if (up == i && mine >= 0 && mine / kVerifyPart == part) atomicOr(&taken[mine % kVerifyPart / 32], 1u << (mine & 31));
   if (draft) {
     if (!__syncthreads_or(tid == i && up >= 0) || c == 0.0) return;
   } else {
     __syncthreads();
     if (children[i] == 0) return;
   }
-  // Draft rows and nodes with several children: what they leave of a distribution is divided by its sum in the walk.
-  const bool precise = p.draft && __syncthreads_or(children[tid] > 1);
+  // Nodes with several children: what rejected ones leave of a distribution is a part of it, as small as 2^-24 of it each time, and
+  // decides what becomes of the next one.  (Draft rows: with any such node of the sequence.)
+  const bool precise = c > 0.0 && (p.draft ? __syncthreads_or(children[tid] > 1) : children[i] > 1);
   const void* row = row_at<F32>(draft ? p.draft : p.logits, at * (draft ? p.draft_row : p.row));
   const int v0 = part * kVerifyPart + tid * 8;
   float x[kPer / 8][8];
 #pragma unroll
   for (int k = 0; k < kPer / 8; ++k) load8<F32>(x[k], row, v0 + k * kThreads * 8, p.V);
+  if (apart) {
+#pragma unroll
+    for (int k = 0; k < kPer / 8; ++k) {
+      const uint32_t bits = reinterpret_cast<const uint8_t*>(taken)[k * kThreads + tid];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[k][e] = bits >> e & 1 ? kNegInf : x[k][e];
+    }
+  }
   Top t{kNegInf, INT32_MAX};
 #pragma unroll
   for (int k = 0; k < kPer / 8; ++k)
@@ -301,14 +322,20 @@ __device__ __forceinline__ double rest_of_one(const VerifyParams& p, int64_t nod
 struct Walk {
   // tried: children of the last node that have had an effect (walk_points: their tokens)
   int32_t parent[kMostNodes], token[kMostNodes], tried[kMostNodes];
-  double prob[kMostNodes], from[kMostNodes];  // of node i's token: under its parent's row, under its own draft row
+  // of node i's token: under its parent's row, under its own draft row.  Point masses: weight of the token in its parent's row, and of all
+  // those in it that no child has drafted, relative to the row's largest logit; at T = 0 the probability, and 0.
+  double prob[kMostNodes], from[kMostNodes];
   double left[kMostNodes];                    // what is left by tried[k], before it is divided
   VerifyStat target[kMostNodes], drafts[kMostNodes];
+  int32_t peak[kMostNodes];                   // point masses: the largest logit that a child has drafted, ordered as whole numbers are
   float u[kMostNodes];
   double sums[kWaves];
   unsigned long long stands[kMostNodes / 64];  // bits of nodes that are accepted if they are tried
   int32_t n_tried;
 };
+
+// Logits as whole numbers of the same order, and back.
+__device__ __forceinline__ int ordered(int x) { return x ^ (x >> 31 & 0x7fffffff); }
 
 // Nodes of a sequence into LDS, with what the rows of those that have children say (rows: and the draft rows), and the probabilities
 // of each node's token.  Returns node threadIdx.x's parent, or -1.
@@ -327,13 +354,15 @@ __device__ __forceinline__ int load_nodes(const VerifyParams& p, int b, int n, d
   if (mine < 0 || mine >= p.V) mine = -1;     // (never accepted, and takes nothing off)
   w.parent[tid] = up;
   w.token[tid] = mine;
-  w.tried[tid] = 0;                           // (for now: whether node tid has children)
+  w.tried[tid] = 0;                           // (for now: the children of node tid)
+  w.peak[tid] = INT32_MIN;
   __syncthreads();
-  if (up >= 0) w.tried[up] = 1;
+  if (up >= 0) atomicAdd(&w.tried[up], 1);
   float x = 0.f, y = 0.f;                     // logits of the node's token
   if (up >= 0 && mine >= 0) {
     x = load1<F32>(row_at<F32>(p.logits, (node0 + up) * p.row), mine);
     if (rows) y = load1<F32>(row_at<F32>(p.draft, (node0 + tid) * p.draft_row), mine);
+    else atomicMax(&w.peak[up], ordered(__float_as_int(x)));
   }
   __syncthreads();
 #pragma unroll 1
@@ -345,14 +374,19 @@ __device__ __forceinline__ int load_nodes(const VerifyParams& p, int b, int n, d
     if (tid % 16 == 0) (draft ? w.drafts : w.target)[i] = s;
   }
   __syncthreads();
-  double pr = 0.0, q = 1.0;
+  double pr = 0.0, q = 0.0;
   if (up >= 0 && mine >= 0) {
     const VerifyStat s = w.target[up];
-    if (c == 0.0) pr = s.top > kNegInf && s.first == mine ? 1.0 : 0.0;
-    else if (s.sum > 0.0) pr = weight(x, s.top, c) * (1.0 / s.sum);
-    if (rows) {
+    if (c == 0.0) {
+      pr = s.top > kNegInf && s.first == mine ? 1.0 : 0.0;
+    } else if (rows) {
+      if (s.sum > 0.0) pr = weight(x, s.top, c) * (1.0 / s.sum);
       const VerifyStat d = w.drafts[tid];
       q = d.sum > 0.0 ? weight(y, d.top, c) * (1.0 / d.sum) : 0.0;
+    } else {
+      const float top = fmaxf(s.top, __int_as_float(ordered(w.peak[up])));
+      pr = weight(x, top, c);
+      q = s.sum * weight(s.top, top, c);
     }
   }
   w.prob[tid] = pr;
@@ -368,41 +402,42 @@ __device__ __forceinline__ void write_path(const VerifyParams& p, int64_t node0,
 }
 
 // The walk where drafted tokens are point masses, by a workgroup together; write: its path goes out.  n > 0.  What those tried before
-// a node have taken off follows from its siblings, so whether a node would be accepted is known without the walk.
+// a node have left follows from its siblings, so whether a node would be accepted is known without the walk:
+//   r(token) = its weight / (weights of the tokens that no sibling has drafted + of those of siblings from it on),
+// a sum of what is left, whose error stays relative to it however little that is.
 template <bool F32>
 __device__ __forceinline__ VerifyEnd walk_points(const VerifyParams& p, int b, int n, double c, Walk& w, bool write) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int64_t node0 = (int64_t)b * p.N;
   const int up = load_nodes<F32>(p, b, n, c, false, w);
   const int mine = w.token[tid], wave = tid >> 6;
-  const double pr = w.prob[tid];
   if (tid < 4) w.stands[tid] = 0;
   if (tid == 0) w.n_tried = 0;
-  bool again = false;                         // a sibling before has taken this token off already
-  double off = 0.0;                           // what siblings before have taken off
-  // Node j against all behind it.  (A token without weight takes nothing off, and one that has all that is left leaves it as it is.)
-  auto against = [&](int j, int its_up, int its_token, double its_weight) {
-    if (its_up < 0 || its_up != up || j >= tid) return;
-    again = again || its_token == mine;
-    if (its_weight > 0.0 && 1.0 - off - its_weight > 0.0) off += its_weight;
-  };
+  // Nodes that have siblings, one after the other against all of a wavefront.
+  auto siblings = [&](auto&& against) {
+    if (wave * 64 >= n) return;
 #pragma unroll 1
-  for (int g = 0; g * 64 < n; ++g) {
-    if (wave == g) {                          // inside a wavefront: node j's is known when its turn comes
+    for (int g = 0; g * 64 < n; ++g) {
+      const int at = g * 64 + lane, its_up = w.parent[at], its_token = w.token[at];
+      const double its_weight = w.prob[at];
+      unsigned long long todo = __ballot(its_up >= 0 && w.tried[its_up < 0 ? 0 : its_up] > 1);
 #pragma unroll 1
-      for (int j = 0; j < min(64, n - g * 64); ++j) {
-        const double x = again ? 0.0 : pr;
-        against(g * 64 + j, __builtin_amdgcn_readlane(up, j), __builtin_amdgcn_readlane(mine, j),
-                __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(x), j), __builtin_amdgcn_readlane(__double2loint(x), j)));
+      while (todo) {
+        const int j = __builtin_ctzll(todo);
+        todo &= todo - 1;
+        against(g * 64 + j, __builtin_amdgcn_readlane(its_up, j) == up, __builtin_amdgcn_readlane(its_token, j), of_lane(its_weight, j));
       }
-      w.from[tid] = again ? 0.0 : pr;
     }
-    __syncthreads();
-    if (wave > g && wave * 64 < n)
-#pragma unroll 1
-      for (int j = g * 64; j < g * 64 + 64; ++j) against(j, w.parent[j], w.token[j], w.from[j]);
-  }
-  const bool stands = up >= 0 && mine >= 0 && (double)w.u[tid] < (again ? 0.0 : pr / (1.0 - off));
+  };
+  bool again = false;                         // a sibling before has this token, which is then gone already
+  siblings([&](int j, bool mine_too, int its_token, double) { again = again || (mine_too && j < tid && its_token == mine); });
+  __syncthreads();
+  if (again) w.prob[tid] = 0.0;
+  __syncthreads();
+  const double own = w.prob[tid];
+  double after = w.from[tid];                 // what is left behind this node
+  siblings([&](int j, bool mine_too, int, double its_weight) { after += mine_too && j > tid ? its_weight : 0.0; });
+  const bool stands = up >= 0 && own > 0.0 && (double)w.u[tid] < own / (after + own);
   const unsigned long long these = __ballot(stands);
   if (lane == 0) w.stands[tid / 64] = these;
   __syncthreads();
@@ -419,7 +454,8 @@ __device__ __forceinline__ VerifyEnd walk_points(const VerifyParams& p, int b, i
     if (write && tid == 0) p.path[node0 + n_path] = cur;
     n_path += 1;
   }
-  if (up == cur && !again && pr > 0.0 && 1.0 - off - pr > 0.0) w.tried[atomicAdd(&w.n_tried, 1)] = mine;  // (its token)
+  // (a token without weight takes nothing off, and one that has all that is left leaves it as it is)
+  if (up == cur && own > 0.0 && after > 0.0) w.tried[atomicAdd(&w.n_tried, 1)] = mine;  // (its token)
   __syncthreads();
   if (write) write_path(p, node0, b, n_path);
   return VerifyEnd{cur, w.n_tried};
