@@ -181,10 +181,11 @@ __device__ __forceinline__ Top top_of_threads(Top t, Top* lds) {
   return t;
 }
 
-// The same by the hardware's exponential: c = hi + lo, and what the product with the difference lacks goes in behind it.  Below 2^-150,
-// where a logit is the type's lowest value too and the product -inf (or NaN: x is -inf), it is 0.
-__device__ __forceinline__ float quick_weight(float x, float top, float hi, float lo) {
-  const float d = x - top, y = d * hi, rest = fmaf(d, lo, fmaf(d, hi, -y));
+// The same by the hardware's exponential: c = (hi + lo) unit, and what the product with the difference lacks goes in behind it.  unit
+// is 1, or, where a difference beyond fp32 may weigh something (c < 2^-100), 2^-64: what the difference loses then at its lower end
+// is nothing to the exponent.  Below 2^-150, where the product may be -inf too (or NaN: x is -inf), it is 0.
+__device__ __forceinline__ float quick_weight(float x, float top, float unit, float hi, float lo) {
+  const float d = fmaf(x, unit, -top * unit), y = d * hi, rest = fmaf(d, lo, fmaf(d, hi, -y));
   const float w = __builtin_amdgcn_exp2f(y);
   return y > -150.f ? fmaf(w, rest * 0.69314718f, w) : 0.f;
 }
@@ -255,11 +256,13 @@ __global__ __launch_bounds__(kThreads) void verify_stat_kernel(VerifyParams p) {
       for (int e = 0; e < 8; ++e) s += weight(x[k][e], t.x, c);
     s = sum_threads(s, sums);
   } else if (c > 0.0) {
-    const float hi = (float)__builtin_fmin(c, 1e38), lo = c > 1e38 ? 0.f : (float)(c - (double)hi);
+    const float unit = c < 0x1p-100 ? 0x1p-64f : 1.f;
+    const double scale = c / (double)unit;
+    const float hi = (float)__builtin_fmin(scale, 1e38), lo = scale > 1e38 ? 0.f : (float)(scale - (double)hi);
 #pragma unroll
     for (int k = 0; k < kPer / 8; ++k)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s += (double)quick_weight(x[k][e], t.x, hi, lo);
+      for (int e = 0; e < 8; ++e) s += (double)quick_weight(x[k][e], t.x, unit, hi, lo);
     s = sum_threads(s, sums);
   }
   if (tid == 0) p.stat[(int64_t)r * p.parts + part] = VerifyStat{s, t.x, t.first};
