@@ -170,6 +170,14 @@ __global__ __launch_bounds__(64 * stream_waves(TYPE, D), stream_waves(TYPE, D) /
     }
   };
 
+  // What lanes of the wavefront have written to LDS, or read there, before others read it or write there.  (LDS serves a wavefront in
+  // order: this only keeps the compiler from moving accesses of different lanes past each other.)
+  auto exchange = [&]() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
+
   // ---- one slab ----------------------------------------------------------------------------------
   floatx16_t o[RB][kBlocks];  // lane (row, h), register i of block x: O[row][32 x + 8 (i / 4) + 4 h + i % 4]
   // Reference maximum of the exponent, log2 units.  It starts at the lowest finite value, so that a masked logit weighs 2^-inf = 0.
@@ -313,16 +321,16 @@ __global__ __launch_bounds__(64 * stream_waves(TYPE, D), stream_waves(TYPE, D) /
     weigh(s);
     put_v(cv);
     wait(more);
+    if constexpr (S::kMx) exchange();
     if ((slab + 1) * kSlab > n_live) {  // (a weight of zero times an infinity of the row that was repeated would be NaN)
       if (slab * kSlab + n32 >= n_live) {
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) *reinterpret_cast<u32x4_t*>(my_v + n32 * kRow + (jh * kChunks + c) * 16) = u32x4_t{};
       }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      exchange();
     }
     outputs(s, false);
+    if constexpr (S::kMx) exchange();  // (the next slab's values go there)
     if (more) request(cv, 1, ahead);
     slab += kWaves;
   };
@@ -375,9 +383,7 @@ __global__ __launch_bounds__(64 * stream_waves(TYPE, D), stream_waves(TYPE, D) /
           }
         }
       }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      exchange();
       floatx16_t s[RB];
       logits(s, codes[0]);
       uint32_t seen[RB];
@@ -415,8 +421,7 @@ __global__ __launch_bounds__(64 * stream_waves(TYPE, D), stream_waves(TYPE, D) /
               }
           }
       }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();  // (the area may be written again)
+      exchange();  // (the area may be written again)
     }
   }
 
