@@ -577,7 +577,7 @@ int baklava_tree_attn(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count
  * logits, draft_logits DEVICE [n_seq * N] rows of V elements of `dtype` (BAKLAVA_BF16 or BAKLAVA_F32), contiguous, aligned to an
  * element; draft_logits NULL or with its own row stride (strides in elements, >= 0).  token, parent DEVICE int32 [n_seq, N];
  * temperature DEVICE fp32 [n_seq] or NULL (1); u DEVICE fp32 [n_seq, N], 0 <= u < 1.  path_out DEVICE int32 [n_seq, N],
- * n_path_out, next_token_out DEVICE int32 [n_seq].  V 1 .. 2^30, rows times parts of 8192 elements below 2^21.
+ * n_path_out, next_token_out DEVICE int32 [n_seq].  V 1 .. 2^30, n_seq * N times the parts of 8192 elements of a row below 2^21.
  * workspace DEVICE, baklava_verify_workspace_bytes(n_seq, N, V, draft_logits != NULL) bytes, 256-byte aligned, as above.
  * Sums are in 64 bits; so are the exponentials, but for those of a row that a single drafted token is tested against: its
  * probability may be off by 1e-8 or so there, 2e-7 at most.  What rejected tokens leave of a distribution is summed up from what is

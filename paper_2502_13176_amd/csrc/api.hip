@@ -35,6 +35,7 @@ constexpr int32_t kMostPromptTokens = 1 << 29;      // of a sequence
 constexpr int32_t kMostRopeTokens = 1 << 26;        // of a sequence
 constexpr int64_t kMostTokenStride = 1 << 24;       // offsets inside a tile of rows stay below 2^32 bytes
 constexpr int32_t kMostVocabulary = 1 << 30;
+constexpr int64_t kMostVerifyParts = 1 << 21;       // rows of logits times parts of them
 constexpr int kMaxChunk = 1 << 22; // row offsets inside a work item stay below 2^32 bytes
 inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
@@ -1260,16 +1261,19 @@ VerifySpace verify_space(int32_t n_seq, int32_t N, int32_t V, bool draft) {
   return w;
 }
 
-bool verify_shape_ok(int32_t n_seq, int32_t N, int32_t V, bool draft) {
+// As many rows times parts as give each launch fewer than 2^31 threads: with draft rows twice as many workgroups, over the parts of the
+// last node's row at most four times.
+bool verify_shape_ok(int32_t n_seq, int32_t N, int32_t V) {
+  static_assert(kVerifyPart / kVerifyPick <= 4, "workgroups for a part");
   if (n_seq < 1 || N < 1 || N > kMostNodes || V < 1 || V > kMostVocabulary) return false;
   const int64_t parts = ((int64_t)V + kVerifyPart - 1) / kVerifyPart;
-  return (int64_t)n_seq * N <= INT32_MAX / 1024 && (int64_t)n_seq * N * (draft ? 2 : 1) * parts <= INT32_MAX / 1024 && (int64_t)n_seq * parts * (kVerifyPart / kVerifyPick) <= INT32_MAX / 1024;
+  return (int64_t)n_seq * N < kMostVerifyParts && (int64_t)n_seq * N * parts < kMostVerifyParts;
 }
 
 }  // namespace
 
 extern "C" size_t baklava_verify_workspace_bytes(int32_t n_seq, int32_t N, int32_t V, int32_t with_draft_logits) {
-  if (!verify_shape_ok(n_seq, N, V, with_draft_logits != 0)) return 0;
+  if (!verify_shape_ok(n_seq, N, V)) return 0;
   return verify_space(n_seq, N, V, with_draft_logits != 0).total;
 }
 
@@ -1280,7 +1284,7 @@ extern "C" int baklava_verify_draft(const void* logits, int64_t row_stride, cons
                                     size_t workspace_bytes, void* stream) {
   if (!logits || !token || !parent || !u || !path || !n_path || !next_token || !workspace) return BAKLAVA_EINVAL;
   if (dtype != BAKLAVA_BF16 && dtype != BAKLAVA_F32) return BAKLAVA_EINVAL;
-  if (!verify_shape_ok(n_seq, N, V, draft_logits != nullptr)) return BAKLAVA_EINVAL;
+  if (!verify_shape_ok(n_seq, N, V)) return BAKLAVA_EINVAL;
   const uintptr_t es = dtype == BAKLAVA_F32 ? 4 : 2;
   if (((uintptr_t)logits | (uintptr_t)draft_logits) & (es - 1)) return BAKLAVA_EINVAL;
   if (((uintptr_t)token | (uintptr_t)parent | (uintptr_t)n_nodes | (uintptr_t)temperature | (uintptr_t)u | (uintptr_t)path |
