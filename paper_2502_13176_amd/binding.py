@@ -404,8 +404,9 @@ class Arena:
     def append_accepted(self, layer_begin: int, layer_count: int, k, v, path, n_path, pos0, q=None, lse=None, stream=None) -> None:
         """baklava_append_accepted: path int32 [batch, N], n_path and pos0 int32 [batch]; k, v (and q, lse, which an arena that
         tracks scores needs) as tree_attn took and gave them.  sync_lengths comes before the next call that takes its position
-        by value."""
+        by value.  No gradient: tensors that require one are refused outside torch.no_grad()."""
         torch = self.torch
+        _refuse_grad(torch, k, v, q, lse)
         rows = _Rows(torch)
         if rows.device != self.gpu:
             raise ValueError("the arena's GPU must be the current one")
@@ -691,7 +692,8 @@ def _per_node(t, name: str) -> int:
 def verify_draft(logits, token, parent, u, draft_logits=None, temperature=None, n_nodes=None, stream=None):
     """baklava_verify_draft: logits (and draft_logits) [batch, N, V] or [batch * N, V] bf16 or fp32, rows of any one stride with
     contiguous elements; token and parent int32 [batch, N], u fp32 [batch, N], temperature fp32 [batch] or None (1), n_nodes int32
-    [batch] or None (N).  Returns (path [batch, N], n_path [batch], next_token [batch]), int32."""
+    [batch] or None (N).  Returns (path [batch, N], n_path [batch], next_token [batch]), int32: whole numbers, which no gradient goes
+    through, whatever the logits require."""
     import torch
     rows = _Rows(torch)
     N, batch = _per_node(parent, "parent"), parent.shape[0]
