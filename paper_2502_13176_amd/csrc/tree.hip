@@ -607,8 +607,13 @@ __global__ __launch_bounds__(kThreads) void tree_merge_kernel(TreeParams p) {
 
 template <int TYPE, int D>
 hipError_t launch(const TreeParams& p, int ks, unsigned grid, hipStream_t s) {
-  if (ks == 2) tree_attn_kernel<TYPE, D, 2, true><<<dim3(grid), dim3(kThreads), 0, s>>>(p);
-  else if (p.row_tiles == 1) tree_attn_kernel<TYPE, D, 1, true><<<dim3(grid), dim3(kThreads), 0, s>>>(p);
+  if constexpr (TYPE != 0) {  // (bf16 launches of as few rows are the streaming kernel's: rule at tree_launch)
+    if (ks == 2) {
+      tree_attn_kernel<TYPE, D, 2, true><<<dim3(grid), dim3(kThreads), 0, s>>>(p);
+      return hipGetLastError();
+    }
+  }
+  if (p.row_tiles == 1) tree_attn_kernel<TYPE, D, 1, true><<<dim3(grid), dim3(kThreads), 0, s>>>(p);
   else tree_attn_kernel<TYPE, D, 1, false><<<dim3(grid), dim3(kThreads), 0, s>>>(p);
   return hipGetLastError();
 }
