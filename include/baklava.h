@@ -546,8 +546,9 @@ int baklava_read_rows(baklava_ctx* ctx, int32_t layer_begin, int32_t layer_count
  * Attention of the nodes of every sequence's tree over the caches of a layer range: node i sees all live rows of a cache and,
  * of the drafted rows k, v, those of its ancestors and its own:
  *   out[i][hq] = softmax(q[i][hq] . [K_c; k of those]^T / sqrt(D)) [V_c; v of those],  c = the cache of KV head hq / G.
- * A node on a path from the root gets what baklava_append_decode_attn gives when the path's tokens are appended one by one;
- * for MXFP4 caches the drafted rows are rounded to 4 bits first, as an append does.  Nothing is appended, scores stay.  Caches may
+ * A node on a path from the root gets what baklava_append_decode_attn gives when the path's tokens are appended one by one, within
+ * the rounding of this call's weights and outputs (bf16, or fp32 over fp32 caches; that call's are fp32); for MXFP4 caches the
+ * drafted rows are rounded to 4 bits first, as an append does.  Nothing is appended, scores stay.  Caches may
  * be empty.
  * q, out rows of Hq heads, k, v rows of Hkv heads, in the context's dtype (bf16 for MXFP4); lse NULL or fp32 "rows of one
  * element" as in baklava_prompt_attn.  fp32 accumulation; softmax weights of bf16 rows enter the second product as bf16.

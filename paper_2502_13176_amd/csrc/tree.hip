@@ -18,7 +18,7 @@
 //
 // A workgroup of four wavefronts, two of them to a compute unit, owns 128 query rows (64 where pairs share their rows) and shares
 // tiles of 64 keys in LDS.  16 caches of 39321 bf16 rows, 448 query rows: 188 us of which 110 are the products at the rate of a library
-// product (1306 TFLOP/s); the matrix cores are busy 41% of the cycles, at 1.8 GHz: start and end take some 15 us, one wavefront in eight
+// product (1306 TFLOP/s); the matrix cores are busy 47% of the cycles, at 1.7 GHz: start and end take some 15 us, one wavefront in eight
 // has no rows of the last workgroup, and a step of 2.2 us ends with a wait for the tiles asked for at its start.  64 caches of 8200 rows,
 // 64 query rows on average: 53 us (271 MB, 39 at 7 TB/s), and 12 for the merge of their partials.  128 caches of 9830 4-bit rows, 52
 // query rows: 66 us (155 MB, 22): conversions, exponentials and LDS, none of them saturated.

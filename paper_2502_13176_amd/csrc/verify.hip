@@ -16,14 +16,15 @@
 // hardware's exponential, with what its argument lacks put back.
 //
 // Launches: the largest logit and the sum of exponentials of parts of the rows that a decision can need (a node without children is
-// none); the walk, and the weights of parts of the last node's row, of which the last workgroup to end takes the token.  With
+// none; point masses: without the tokens that its children drafted); the walk, and the weights of parts of the last node's row, of which the last workgroup to end takes the token.  With
 // draft rows what is left of a distribution is a difference, so the walk is a launch of its own that also sums up the rows it
 // ends with in 64 bits.
 //
-// Latency bounds it: chains of memory reads, and code that is run through once and comes from memory itself (192 cycles for 64 bytes),
-// which is why loops are kept as loops.  Chain of 5, 32000 tokens, greedy: 12 us (4.7 and 7.6); 8 trees of up to 32 nodes, 131072
+// Latency bounds it: chains of memory reads, and code that is run through once and comes from memory itself (a launch of 16 KB
+// of straight-line code takes 8 us, of 32 KB 29), which is why loops are kept as loops.  Chain of 5, 32000 tokens, greedy: 12 us (4.7 and 7.6); 8 trees of up to 32 nodes, 131072
 // tokens: 31 us (28 with sums by the hardware's exponential there, too); 16 chains of 6 with draft rows, 100003 tokens in fp32: 51 us (20 for 77
-// MB, 12.5, 18.5).
+// MB, 12.5, 19).  Siblings with draft rows are the costly ones, by how many fail: 8 trees of 16 nodes, 131072 tokens in bf16, 56 us; of 32
+// nodes, paths of 2 to 5, 510.
 #include "common.h"
 
 namespace baklava {
